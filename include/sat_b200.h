@@ -512,6 +512,49 @@ sat_status sat_codec_decode(sat_ctx *ctx, const uint8_t *in, int64_t in_bytes, c
                             int32_t precision, float *x, int32_t ld);
 sat_status sat_cache_requantise(sat_ctx *ctx, int32_t layer, int32_t age, int32_t precision, int64_t *bytes);
 
+/* ---------------------------------------------------------------------------------------
+ * Microscaled matrices: storage in 8 or 4 bits that contractions read as it lies (the paper has no counterpart; its "Data Compression"
+ * supplement compresses stored embeddings, and these formats do the same for what the layers keep and multiply).
+ *
+ * A row of d elements is cut into groups of 32 consecutive elements (the last one may be short).  Group G has one scale 2^e and every
+ * element x of it a small floating-point number q, standing for q 2^e:
+ *     SAT_MX8   q in e4m3 (1 sign, 4 exponent, 3 fraction bits, bias 7, largest 448)       SAT_MX4   q in e2m1 (0 .5 1 1.5 2 3 4 6)
+ *     e = the smallest integer >= -127 with max_{x in G} |x| <= largest 2^e,      q = x 2^-e rounded to nearest, ties to even.
+ * Nothing saturates, so an element is off by at most 2^-4 |x| (SAT_MX8) or 2^-2 |x| (SAT_MX4) or half the format's least step times 2^e
+ * (2^-10 or 2^-2), whichever is more.  A group with an infinity or a NaN has the scale byte 255 and reads as NaN throughout.
+ *   codes    DEVICE, row r at byte r * ld_codes: one byte per element (SAT_MX8) or two elements a byte, the even one in the low half
+ *            (SAT_MX4), the last group filled up with zeros.  16-byte aligned, ld_codes a multiple of 16 and >= 32 (16) bytes a group
+ *   scales   DEVICE, row r at byte r * ld_scales: e + 127 per group.  4-byte aligned, ld_scales a multiple of 4 and >= the groups
+ * Bytes between a row's end and the next row are neither read nor written.  The structure is HOST and not kept.
+ * ------------------------------------------------------------------------------------- */
+enum { SAT_MX8 = 8, SAT_MX4 = 4 };
+typedef struct sat_mx_matrix {
+    uint8_t *codes, *scales;
+    int64_t rows;                /* up to 2^31 - 1 */
+    int32_t d, ld_codes, ld_scales;
+    int32_t format;              /* SAT_MX8 or SAT_MX4 */
+} sat_mx_matrix;
+/* x [q.rows x ld] fp32 -> q, and back (the value nearest to q 2^e, which is itself).  Every finite fp32 value is taken, subnormal ones too. */
+sat_status sat_mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q);
+sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int32_t ld);
+/* Contractions with microscaled operands, fp32 results (a hat marks what the codes stand for):
+ *   sat_mx_dense_nt  C[m x n] = A^[m x k] W^[n x k]^T + bias: both operands in 4 bits, the transform of a layer with a row of W per output.
+ *                    A is fp32 [m x lda] and quantised on the way in, and where Aq is given kept there (for sat_mx_dense_tn); or A is NULL
+ *                    and the rows come from Aq.  bias DEVICE [n] or NULL.  W and Aq: SAT_MX4.
+ *   sat_mx_dense_nn  C[m x W.d] = A[m x W.rows] W^: fp32 rows on stored weights of either format; with A = the gradient with respect to
+ *                    C of the product above this is the gradient with respect to A^.
+ *   sat_mx_dense_tn  C[A.d x n] (+)= A^^T B[A.rows x n], colsum[n] (+)= 1^T B: weight and bias gradient from a stored input.  C is
+ *                    dense row-major, colsum may be NULL; accumulate = 1 adds to both.
+ * sat_mx_dense_nt multiplies 4-bit codes exactly and adds in fp32; the other two split fp32 operands into terms that carry all of
+ * their 24 bits.  An infinity or a NaN in an fp32 operand makes NaN of every result that it reaches.  Results are bit-reproducible.
+ * Empty sums (no rows, W without rows) are zero, or the bias.  Calls on one context share its workspaces like all calls of this
+ * header: two captured graphs with calls of one context must not run at the same time, and the first call of a size may allocate (make
+ * it before a capture). */
+sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias,
+                           float *C, int32_t ldc);
+sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc);
+sat_status sat_mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate);
+
 /* Bounds-checking debug build (libsat_b200_dbg.so: the same sources compiled with -DSAT_DEBUG_BOUNDS; the paper has no
  * counterpart).  Every index the graph kernels (SpMM, halo-row products, row gather / scatter, per-slot sums) load from an
  * index array is compared with the extent of the matrix it addresses; an index outside it raises a bit of the device status
@@ -535,7 +578,7 @@ sat_status sat_launch_count(sat_ctx *ctx, int64_t *count);
  * so that a timed run can carry the events of one family only. */
 enum { SAT_PROF_SPMM_FWD = 0, SAT_PROF_SPMM_BWD, SAT_PROF_SPMM_HROW, SAT_PROF_GEMM_NN, SAT_PROF_GEMM_NT,
        SAT_PROF_GEMM_TN, SAT_PROF_LSTM_CELL, SAT_PROF_GATHER, SAT_PROF_SCATTER, SAT_PROF_LOSS, SAT_PROF_MASK,
-       SAT_PROF_GEMM_SIDE, SAT_PROF_CODEC, SAT_PROF_PRED_TRAIN, SAT_PROF_GAT };
+       SAT_PROF_GEMM_SIDE, SAT_PROF_CODEC, SAT_PROF_PRED_TRAIN, SAT_PROF_GAT, SAT_PROF_MX };
 int32_t sat_profile_families(void);
 sat_status sat_profile_enable(sat_ctx *ctx, int enable);
 sat_status sat_profile_select(sat_ctx *ctx, uint64_t family_mask);

@@ -43,6 +43,13 @@ class sat_pred_params(C.Structure):
                 ("h", C.c_int32), ("cell", C.c_int32), ("version", C.c_uint64)]
 
 
+class sat_mx_matrix(C.Structure):
+    """A microscaled matrix (groups of 32 elements of a row with one power of two); `_keep` holds the tensors behind the pointers."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("d", C.c_int32), ("ld_codes", C.c_int32),
+                ("ld_scales", C.c_int32), ("format", C.c_int32)]
+
+
+SAT_MX8, SAT_MX4 = 8, 4
 SAT_CELL_LSTM, SAT_CELL_GRU = 0, 1
 SAT_EPOCH_GRAD_HISTORY, SAT_EPOCH_COMMIT, SAT_EPOCH_STEP, SAT_EPOCH_CONTINUE = 1, 2, 4, 8
 
@@ -76,7 +83,7 @@ EXPORTS = [
     "sat_predict_state", "sat_layer_fwd", "sat_layer_bwd", "sat_cache_update", "sat_cache_commit", "sat_cache_state",
     "sat_cache_read", "sat_cache_export", "sat_cache_import", "sat_cache_set_state", "sat_loss_grad", "sat_sgd_step", "sat_sgd_steps",
     "sat_dense_nn", "sat_dense_nt", "sat_dense_tn", "sat_dense_tn_static", "sat_launch_count", "sat_profile_families", "sat_profile_enable", "sat_profile_select", "sat_profile_read",
-    "sat_epoch", "sat_codec_plan", "sat_codec_encode", "sat_codec_decode", "sat_cache_requantise", "sat_staleness", "sat_pred_grad", "sat_grad_history_read", "sat_grad_history_write", "sat_gat_fwd", "sat_gat_bwd", "sat_gat_scores", "sat_profile_l2_rates", "sat_debug_poke_index", "sat_spmm_plan",
+    "sat_epoch", "sat_codec_plan", "sat_codec_encode", "sat_codec_decode", "sat_cache_requantise", "sat_mx_quantise", "sat_mx_dequantise", "sat_mx_dense_nt", "sat_mx_dense_nn", "sat_mx_dense_tn", "sat_staleness", "sat_pred_grad", "sat_grad_history_read", "sat_grad_history_write", "sat_gat_fwd", "sat_gat_bwd", "sat_gat_scores", "sat_profile_l2_rates", "sat_debug_poke_index", "sat_spmm_plan",
 ]
 
 
@@ -444,6 +451,67 @@ def sat_cache_requantise(ctx, layer: int, age: int, precision: int) -> int:
     total = C.c_int64(0)
     _check(ctx, _lib.sat_cache_requantise(ctx, C.c_int32(layer), C.c_int32(age), C.c_int32(precision), C.byref(total)))
     return int(total.value)
+
+
+def make_mx(codes, scales, d: int, fmt: int) -> sat_mx_matrix:
+    """Describes a microscaled matrix of d columns: codes CUDA uint8 [rows, >= 32 (SAT_MX8) or 16 (SAT_MX4) bytes per group of 32 columns], row
+    stride a multiple of 16; scales CUDA uint8 [rows, >= groups], row stride a multiple of 4."""
+    import torch
+    groups = (d + 31) // 32
+    assert d > 0 and fmt in (SAT_MX8, SAT_MX4)
+    for t, width in ((codes, groups * 32 * fmt // 8), (scales, groups)):
+        assert t.is_cuda and t.dtype == torch.uint8 and t.dim() == 2 and t.stride(1) == 1 and t.shape[1] >= width and t.shape[0] == codes.shape[0]
+    q = sat_mx_matrix(codes.data_ptr(), scales.data_ptr(), codes.shape[0], d, _ld(codes), _ld(scales), fmt)
+    q._keep = (codes, scales)
+    return q
+
+
+def new_mx(rows: int, d: int, fmt: int, device=None) -> sat_mx_matrix:
+    """An uninitialised microscaled matrix on `device` (default: the current CUDA device)."""
+    import torch
+    groups = (d + 31) // 32
+    device = torch.device("cuda") if device is None else device
+    codes = torch.empty((rows, (groups * 32 * fmt // 8 + 15) & ~15), dtype=torch.uint8, device=device)
+    return make_mx(codes, torch.empty((rows, (groups + 3) & ~3), dtype=torch.uint8, device=device), d, fmt)
+
+
+def sat_mx_quantise(ctx, x, q: sat_mx_matrix):
+    """q <- x (CUDA fp32 [rows, d])"""
+    assert tuple(x.shape) == (q.rows, q.d)
+    _check(ctx, _lib.sat_mx_quantise(ctx, _dev(x), C.c_int32(_ld(x)), C.byref(q)))
+
+
+def sat_mx_dequantise(ctx, q: sat_mx_matrix, x):
+    """x (CUDA fp32 [rows, d]) <- what q stands for"""
+    assert tuple(x.shape) == (q.rows, q.d)
+    _check(ctx, _lib.sat_mx_dequantise(ctx, C.byref(q), _dev(x), C.c_int32(_ld(x))))
+
+
+def sat_mx_dense_nt(ctx, A, W: sat_mx_matrix, bias, out, kept: sat_mx_matrix | None = None):
+    """out[m, n] = A^[m, k] W^[n, k]^T + bias, both operands in 4 bits.  A: CUDA fp32, quantised on the way in (and kept in `kept`, if given), or a
+    sat_mx_matrix."""
+    stored = isinstance(A, sat_mx_matrix)
+    assert not (stored and kept is not None)
+    m, k = (int(A.rows), int(A.d)) if stored else map(int, A.shape)
+    q = A if stored else kept
+    assert k == W.d and tuple(out.shape) == (m, W.rows) and (q is None or (q.rows, q.d) == (m, k))
+    assert bias is None or (bias.is_contiguous() and bias.numel() == W.rows)
+    _check(ctx, _lib.sat_mx_dense_nt(ctx, C.c_int64(m), None if stored else _dev(A), C.c_int32(0 if stored else _ld(A)), None if q is None else C.byref(q),
+                                     C.byref(W), _dev(bias), _dev(out), C.c_int32(_ld(out))))
+
+
+def sat_mx_dense_nn(ctx, A, W: sat_mx_matrix, out):
+    """out[m, W.d] = A[m, W.rows] W^"""
+    assert A.shape[1] == W.rows and tuple(out.shape) == (A.shape[0], W.d)
+    _check(ctx, _lib.sat_mx_dense_nn(ctx, C.c_int64(A.shape[0]), _dev(A), C.c_int32(_ld(A)), C.byref(W), _dev(out), C.c_int32(_ld(out))))
+
+
+def sat_mx_dense_tn(ctx, A: sat_mx_matrix, Bm, out, colsum=None, accumulate: bool = False):
+    """out[A.d, n] (+)= A^^T Bm[A.rows, n], colsum[n] (+)= column sums of Bm (out dense)"""
+    assert out.is_contiguous() and Bm.shape[0] == A.rows and tuple(out.shape) == (A.d, Bm.shape[1])
+    assert colsum is None or (colsum.is_contiguous() and colsum.numel() == Bm.shape[1])
+    _check(ctx, _lib.sat_mx_dense_tn(ctx, C.byref(A), C.c_int32(Bm.shape[1]), _dev(Bm), C.c_int32(_ld(Bm)), _dev(out), _dev(colsum),
+                                     C.c_int(1 if accumulate else 0)))
 
 
 def sat_dense_tn_static(stream: int, A, Bm, out):

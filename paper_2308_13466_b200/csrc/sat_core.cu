@@ -208,6 +208,7 @@ extern "C" sat_status sat_destroy(sat_ctx *ctx)
     sat_free_buf(ctx->buf_lstm_w);
     sat_free_buf(ctx->buf_pred_a);
     sat_free_buf(ctx->buf_misc);
+    sat_free_buf(ctx->buf_mx);
     sat_free_buf(ctx->buf_colsum);
     sat_free_buf(ctx->buf_dmask);
     sat_free_buf(ctx->buf_wsplit);
@@ -282,7 +283,7 @@ extern "C" sat_status sat_launch_count(sat_ctx *ctx, int64_t *count)
 // per-family device timing
 // =====================================================================================
 static const char *k_family_names[SATK_COUNT] = {"spmm_fwd", "spmm_bwd", "spmm_hrow", "gemm_nn", "gemm_nt", "gemm_tn",
-                                                 "lstm_cell", "gather", "scatter", "loss", "mask", "gemm_side", "codec", "pred_train", "gat"};
+                                                 "lstm_cell", "gather", "scatter", "loss", "mask", "gemm_side", "codec", "pred_train", "gat", "mx"};
 
 static void prof_clear(sat_ctx *ctx)
 {

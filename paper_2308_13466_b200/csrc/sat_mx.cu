@@ -1,0 +1,369 @@
+// Microscaled matrices: quantisation to and from groups of 32 elements with one power of two, and the contractions that read them.
+//     group G of a row:  x ~ q 2^e,  e = least integer >= -127 with max |x| <= largest 2^e,  q = rne(x 2^-e) in e4m3 or e2m1
+//   sat_mx_dense_nt   C = A^ W^^T + bias    both operands 4-bit
+//   sat_mx_dense_nn   C = A W^              A fp32
+//   sat_mx_dense_tn   C (+)= A^^T B         B fp32, split over the rows
+#include "sat_internal.h"
+#include "sat_ptx.h"
+
+#include <algorithm>
+
+#define MX_GROUP 32
+
+static inline int32_t mx_groups(int32_t d) { return (d + MX_GROUP - 1) / MX_GROUP; }
+// bytes of codes in a row, the last group filled up
+static inline int32_t mx_row_bytes(const sat_mx_matrix *q) { return mx_groups(q->d) * (q->format == SAT_MX8 ? 32 : 16); }
+
+// The matrix as kernels take it
+struct MxView {
+    uint8_t *codes, *scales;
+    int64_t ld_codes, ld_scales;
+};
+static inline MxView mx_view(const sat_mx_matrix *q) { return MxView{q->codes, q->scales, q->ld_codes, q->ld_scales}; }
+
+static sat_status mx_check(sat_ctx *ctx, const sat_mx_matrix *q, const char *who)
+{
+    if (!q || (q->format != SAT_MX8 && q->format != SAT_MX4) || q->rows < 0 || q->rows > INT32_MAX || q->d <= 0 || q->d > INT32_MAX - 63)
+        return sat_fail(ctx, SAT_EINVAL, "%s: no microscaled matrix, or one of bad format or shape", who);
+    if (q->rows > 0 && (!q->codes || !q->scales || !aligned16(q->codes) || ((uintptr_t)q->scales & 3)))
+        return sat_fail(ctx, SAT_EINVAL, "%s: null or misaligned codes / scales", who);
+    if (q->ld_codes < mx_row_bytes(q) || (q->ld_codes & 15) || q->ld_scales < mx_groups(q->d) || (q->ld_scales & 3))
+        return sat_fail(ctx, SAT_EINVAL, "%s: bad row stride of codes or scales", who);
+    return SAT_OK;
+}
+
+// =====================================================================================
+// the two formats
+// =====================================================================================
+// Scale byte of a group from the bits of its largest magnitude: the exponent that brings it to [largest / 2, largest], rounded up from the
+// fraction's compare with 1.75 (448 = 1.75 2^8) or 1.5 (6 = 1.5 2^2) by a carry; 255 where that magnitude is no finite number.
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax)
+{
+    if (amax >= 0x7F800000u) return 255u;
+    const int32_t e = (int32_t)((amax + (FMT == SAT_MX8 ? 0x1FFFFFu : 0x3FFFFFu)) >> 23) - (FMT == SAT_MX8 ? 8 : 2);
+    return e > 0 ? (uint32_t)e : 0u;
+}
+// 2^(127 - byte), which is never subnormal: bytes go up to 253, and NaN's comes out as 0.  (x 2^-e is rounded only where it is below
+// 2^-126, far under half a step of either format.)
+__device__ __forceinline__ float mx_inverse(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }
+// 2^(byte - 127); byte 0 is a subnormal number, 255 stands for NaN
+__device__ __forceinline__ float mx_power(uint32_t byte)
+{
+    return byte == 255u ? __uint_as_float(0x7FFFFFFFu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+}
+// four elements -> four bytes (SAT_MX8) or two (SAT_MX4), the first element lowest
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_encode4(float a, float b, float c, float d)
+{
+    uint32_t r;
+    if (FMT == SAT_MX8)
+        asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+            : "=r"(r)
+            : "f"(a), "f"(b), "f"(c), "f"(d));
+    else
+        asm("{\n\t.reg .b8 l, h, z;\n\tcvt.rn.satfinite.e2m1x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h, l, h};\n\t}"
+            : "=r"(r)
+            : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
+}
+// two elements as a pair of halves, without the scale
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_decode2(uint32_t code)
+{
+    uint32_t r;
+    if (FMT == SAT_MX8)
+        asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(r) : "r"(code));
+    else
+        asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(r) : "r"(code));
+    return r;
+}
+__device__ __forceinline__ float2 mx_unpack(uint32_t halves)
+{
+    float2 f;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(halves));
+    return f;
+}
+// element (r, c)
+template <int FMT>
+__device__ __forceinline__ float mx_element(const MxView &q, int64_t r, int32_t c)
+{
+    const float s = mx_power(__ldg(q.scales + r * q.ld_scales + (c >> 5)));
+    if (FMT == SAT_MX8) return mx_unpack(mx_decode2<FMT>(__ldg(q.codes + r * q.ld_codes + c))).x * s;
+    const float2 p = mx_unpack(mx_decode2<FMT>(__ldg(q.codes + r * q.ld_codes + (c >> 1))));
+    return ((c & 1) ? p.y : p.x) * s;
+}
+
+// =====================================================================================
+// quantisation and back
+// =====================================================================================
+#define MX_UNROLL 4
+// Eight lanes per group, four elements each.  One pass over the data; bound by memory.
+template <int FMT>
+__global__ void __launch_bounds__(256)
+k_mx_quantise(const float *__restrict__ x, int64_t ld, int64_t total, int32_t groups, int32_t d, MxView q)
+{
+    sat_grid_wait();
+    const int sub = threadIdx.x & 7;
+    const int64_t step = (int64_t)gridDim.x * 32, first = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
+    for (int64_t g0 = first - (threadIdx.x >> 3); g0 < total; g0 += MX_UNROLL * step) {   // (the same for the whole block: the lanes meet below)
+        float4 v[MX_UNROLL];
+        int64_t row[MX_UNROLL];
+        int32_t col[MX_UNROLL];
+#pragma unroll
+        for (int u = 0; u < MX_UNROLL; ++u) {
+            const int64_t g = g0 + (threadIdx.x >> 3) + u * step;
+            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            row[u] = -1;
+            if (g < total) {
+                row[u] = sat_div(g, groups);
+                col[u] = (int32_t)(g - row[u] * groups) * MX_GROUP + 4 * sub;
+                if (col[u] < d) v[u] = __ldg(reinterpret_cast<const float4 *>(x + row[u] * ld + col[u]));
+                if (col[u] + 1 >= d) v[u].y = 0.f;   // what lies behind the row's end is not part of it
+                if (col[u] + 2 >= d) v[u].z = 0.f;
+                if (col[u] + 3 >= d) v[u].w = 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < MX_UNROLL; ++u) {
+            uint32_t amax = max(max(__float_as_uint(v[u].x) & 0x7FFFFFFFu, __float_as_uint(v[u].y) & 0x7FFFFFFFu),
+                                max(__float_as_uint(v[u].z) & 0x7FFFFFFFu, __float_as_uint(v[u].w) & 0x7FFFFFFFu));
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            if (row[u] < 0) continue;
+            const uint32_t byte = mx_scale_byte<FMT>(amax);
+            const float s = mx_inverse(byte);
+            const uint32_t c = byte == 255u ? 0u : mx_encode4<FMT>(v[u].x * s, v[u].y * s, v[u].z * s, v[u].w * s);
+            if (FMT == SAT_MX8) *reinterpret_cast<uint32_t *>(q.codes + row[u] * q.ld_codes + col[u]) = c;
+            else *reinterpret_cast<uint16_t *>(q.codes + row[u] * q.ld_codes + col[u] / 2) = (uint16_t)c;
+            if (sub == 0) q.scales[row[u] * q.ld_scales + (col[u] >> 5)] = (uint8_t)byte;
+        }
+    }
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(256)
+k_mx_dequantise(MxView q, int64_t total, int32_t groups, int32_t d, float *__restrict__ x, int64_t ld)
+{
+    sat_grid_wait();
+    const int sub = threadIdx.x & 7;
+    const int64_t step = (int64_t)gridDim.x * 32;
+    for (int64_t g0 = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); g0 < total; g0 += MX_UNROLL * step) {
+        uint32_t code[MX_UNROLL], byte[MX_UNROLL];
+        int64_t row[MX_UNROLL];
+        int32_t col[MX_UNROLL];
+#pragma unroll
+        for (int u = 0; u < MX_UNROLL; ++u) {
+            const int64_t g = g0 + u * step;
+            row[u] = -1;
+            if (g < total) {
+                row[u] = sat_div(g, groups);
+                col[u] = (int32_t)(g - row[u] * groups) * MX_GROUP + 4 * sub;
+                if (FMT == SAT_MX8) code[u] = __ldg(reinterpret_cast<const uint32_t *>(q.codes + row[u] * q.ld_codes + col[u]));
+                else code[u] = __ldg(reinterpret_cast<const uint16_t *>(q.codes + row[u] * q.ld_codes + col[u] / 2));
+                byte[u] = __ldg(q.scales + row[u] * q.ld_scales + (col[u] >> 5));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < MX_UNROLL; ++u) {
+            if (row[u] < 0 || col[u] >= d) continue;
+            const float s = mx_power(byte[u]);
+            const float2 a = mx_unpack(mx_decode2<FMT>(code[u])), b = mx_unpack(mx_decode2<FMT>(code[u] >> (FMT == SAT_MX8 ? 16 : 8)));
+            float *o = x + row[u] * ld + col[u];
+            if (col[u] + 4 <= d) {
+                *reinterpret_cast<float4 *>(o) = make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
+            } else {
+                o[0] = a.x * s;
+                if (col[u] + 1 < d) o[1] = a.y * s;
+                if (col[u] + 2 < d) o[2] = b.x * s;
+            }
+        }
+    }
+}
+
+static sat_status mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q)
+{
+    if (q->rows == 0) return SAT_OK;
+    const int32_t groups = mx_groups(q->d);
+    const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8);
+    ProfScope prof(ctx, SATK_MX, (double)q->rows * (4.0 * q->d + mx_row_bytes(q) + groups), 0.0);
+    sat_pdl(ctx->stream, q->format == SAT_MX8 ? k_mx_quantise<SAT_MX8> : k_mx_quantise<SAT_MX4>, (unsigned)blocks, 256, 0)(x, ld, total, groups, q->d, mx_view(q));
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
+extern "C" sat_status sat_mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q)
+{
+    CHECK_CTX(ctx);
+    SAT_TRY(mx_check(ctx, q, "sat_mx_quantise"));
+    if (!ok_ld(ld, q->d) || (q->rows > 0 && (!x || !aligned16(x)))) return sat_fail(ctx, SAT_EINVAL, "sat_mx_quantise: null / misaligned x or bad leading dimension");
+    return mx_quantise(ctx, x, ld, q);
+}
+
+extern "C" sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int32_t ld)
+{
+    CHECK_CTX(ctx);
+    SAT_TRY(mx_check(ctx, q, "sat_mx_dequantise"));
+    if (!ok_ld(ld, q->d) || (q->rows > 0 && (!x || !aligned16(x)))) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dequantise: null / misaligned x or bad leading dimension");
+    if (q->rows == 0) return SAT_OK;
+    const int32_t groups = mx_groups(q->d);
+    const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8);
+    ProfScope prof(ctx, SATK_MX, (double)q->rows * (4.0 * q->d + mx_row_bytes(q) + groups), 0.0);
+    sat_pdl(ctx->stream, q->format == SAT_MX8 ? k_mx_dequantise<SAT_MX8> : k_mx_dequantise<SAT_MX4>, (unsigned)blocks, 256, 0)(mx_view(q), total, groups, q->d, x, ld);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
+// =====================================================================================
+// contractions on CUDA cores: C[M x N] = sum_k a(i, k) b(k, j), tiles of 64 x 64, fp32 FMA
+// =====================================================================================
+enum { MX_NT = 0, MX_NN = 1, MX_TN = 2 };
+struct MxSimple {
+    MxView q1, q2;        // NT: A^, W^;  NN: -, W^;  TN: A^, -
+    const float *x;       // NN: A;  TN: B
+    int64_t ld_x;
+    int64_t M, K, kps;    // kps: terms per block along z (TN)
+    int32_t N;
+    const float *bias;
+    float *C, *cs;        // TN: partial sums [z][M x N] and [z][N]
+    int64_t ldc;
+};
+template <int OP, int F1, int F2>
+__global__ void __launch_bounds__(256)
+k_mx_simple(MxSimple p)
+{
+    sat_grid_wait();
+    __shared__ float As[16][68], Bs[16][68];
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int64_t i0 = (int64_t)blockIdx.x * 64;
+    const int32_t j0 = (int32_t)blockIdx.y * 64;
+    const int64_t k0 = (int64_t)blockIdx.z * p.kps, k1 = k0 + p.kps < p.K ? k0 + p.kps : p.K;
+    float acc[4][4] = {}, cs = 0.f;
+    for (int64_t kb = k0; kb < k1; kb += 16) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int t = threadIdx.x + 256 * u;
+            {
+                const int kk = OP == MX_TN ? t >> 6 : t & 15, ii = OP == MX_TN ? t & 63 : t >> 4;   // along the rows in memory
+                const int64_t k = kb + kk, i = i0 + ii;
+                float a = 0.f;
+                if (k < k1 && i < p.M) a = OP == MX_TN ? mx_element<F1>(p.q1, k, (int32_t)i) : OP == MX_NN ? __ldg(p.x + i * p.ld_x + k) : mx_element<F1>(p.q1, i, (int32_t)k);
+                As[kk][ii] = a;
+            }
+            {
+                const int kk = OP == MX_NT ? t & 15 : t >> 6, jj = OP == MX_NT ? t >> 4 : t & 63;
+                const int64_t k = kb + kk;
+                const int32_t j = j0 + jj;
+                float b = 0.f;
+                if (k < k1 && j < p.N) b = OP == MX_TN ? __ldg(p.x + k * p.ld_x + j) : OP == MX_NN ? mx_element<F2>(p.q2, k, j) : mx_element<F2>(p.q2, j, (int32_t)k);
+                Bs[kk][jj] = b;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const float4 a = *reinterpret_cast<const float4 *>(&As[k][4 * ty]), b = *reinterpret_cast<const float4 *>(&Bs[k][4 * tx]);
+            const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
+        }
+        if (OP == MX_TN && p.cs && blockIdx.x == 0 && threadIdx.x < 64)
+            for (int k = 0; k < 16; ++k) cs += Bs[k][threadIdx.x];
+        __syncthreads();
+    }
+    float *C = OP == MX_TN ? p.C + (int64_t)blockIdx.z * p.M * p.N : p.C;
+    const int64_t ldc = OP == MX_TN ? p.N : p.ldc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t r = i0 + 4 * ty + i;
+            const int32_t c = j0 + 4 * tx + j;
+            if (r < p.M && c < p.N) C[r * ldc + c] = acc[i][j] + (p.bias ? __ldg(p.bias + c) : 0.f);
+        }
+    if (OP == MX_TN && p.cs && blockIdx.x == 0 && threadIdx.x < 64 && j0 + (int32_t)threadIdx.x < p.N) p.cs[(int64_t)blockIdx.z * p.N + j0 + threadIdx.x] = cs;
+}
+
+static sat_status mx_grid(sat_ctx *ctx, int64_t M, int32_t N, int64_t splits, dim3 *grid)
+{
+    if (cdiv64(N, 64) > 65535 || splits > 65535 || cdiv64(M, 64) > INT32_MAX) return sat_fail(ctx, SAT_EINVAL, "microscaled contraction: shape is too large");
+    *grid = dim3((unsigned)cdiv64(M, 64), (unsigned)cdiv64(N, 64), (unsigned)splits);
+    return SAT_OK;
+}
+
+extern "C" sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W,
+                                      const float *bias, float *C, int32_t ldc)
+{
+    CHECK_CTX(ctx);
+    SAT_TRY(mx_check(ctx, W, "sat_mx_dense_nt"));
+    if (W->format != SAT_MX4 || (Aq && Aq->format != SAT_MX4)) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: operands are in 4 bits (SAT_MX4)");
+    if (Aq) SAT_TRY(mx_check(ctx, Aq, "sat_mx_dense_nt"));
+    if (m < 0 || m > INT32_MAX || (Aq && (Aq->rows != m || Aq->d != W->d)) || W->rows == 0)
+        return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: shapes of the operands do not fit");
+    const int32_t n = (int32_t)W->rows, k = W->d;
+    if ((m > 0 && !A && !Aq) || (A && (!ok_ld(lda, k) || !aligned16(A))) || !ok_ld(ldc, n) || (m > 0 && (!C || !aligned16(C))))
+        return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: null / misaligned tensor or bad leading dimension");
+    if (m == 0) return SAT_OK;
+    sat_mx_matrix tmp;
+    if (!Aq) {
+        const int32_t groups = mx_groups(k), lds = (groups + 3) & ~3, ldq = groups * 16;
+        SAT_TRY(sat_ensure(ctx, ctx->buf_mx, (size_t)m * (ldq + lds)));
+        tmp = sat_mx_matrix{(uint8_t *)ctx->buf_mx.p, (uint8_t *)ctx->buf_mx.p + (size_t)m * ldq, m, k, ldq, lds, SAT_MX4};
+        Aq = &tmp;
+    }
+    if (A) SAT_TRY(mx_quantise(ctx, A, lda, Aq));
+    ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
+    dim3 grid;
+    SAT_TRY(mx_grid(ctx, m, n, 1, &grid));
+    const MxSimple p{mx_view(Aq), mx_view(W), nullptr, 0, m, k, k, n, bias, C, nullptr, ldc};
+    sat_pdl(ctx->stream, k_mx_simple<MX_NT, SAT_MX4, SAT_MX4>, grid, 256, 0)(p);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
+extern "C" sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc)
+{
+    CHECK_CTX(ctx);
+    SAT_TRY(mx_check(ctx, W, "sat_mx_dense_nn"));
+    const int32_t n = W->d, k = (int32_t)W->rows;
+    if (m < 0 || m > INT32_MAX || (k > 0 && !ok_ld(lda, k)) || !ok_ld(ldc, n) || (m > 0 && ((k > 0 && (!A || !aligned16(A))) || !C || !aligned16(C))))
+        return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nn: null / misaligned tensor or bad shape");
+    if (m == 0) return SAT_OK;
+    ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
+    dim3 grid;
+    SAT_TRY(mx_grid(ctx, m, n, 1, &grid));
+    const MxSimple p{MxView{}, mx_view(W), A, lda, m, k, k, n, nullptr, C, nullptr, ldc};
+    sat_pdl(ctx->stream, W->format == SAT_MX8 ? k_mx_simple<MX_NN, SAT_MX8, SAT_MX8> : k_mx_simple<MX_NN, SAT_MX4, SAT_MX4>, grid, 256, 0)(p);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
+static sat_status mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
+{
+    const int32_t m = A->d;
+    ProfScope prof(ctx, SATK_MX, (double)A->rows * (mx_row_bytes(A) + mx_groups(m) + 4.0 * n), 2.0 * (double)A->rows * m * n);
+    const int64_t rows = A->rows > 0 ? A->rows : 1, tiles = cdiv64(m, 64) * cdiv64(n, 64);
+    int64_t splits = std::max<int64_t>(cdiv64(rows, 4096), std::min<int64_t>(cdiv64(4 * ctx->sms, tiles), cdiv64(rows, 64)));
+    if (splits > 1024) splits = 1024;
+    const int64_t kps = cdiv64(cdiv64(rows, splits), 16) * 16;
+    splits = cdiv64(rows, kps);
+    SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)splits * ((size_t)m * n + n) * sizeof(float)));
+    float *part = (float *)ctx->buf_splitk.p, *part_cs = colsum ? part + (size_t)splits * m * n : nullptr;
+    dim3 grid;
+    SAT_TRY(mx_grid(ctx, m, n, splits, &grid));
+    const MxSimple p{mx_view(A), MxView{}, B, ldb, m, A->rows, kps, n, nullptr, part, part_cs, n};
+    sat_pdl(ctx->stream, A->format == SAT_MX8 ? k_mx_simple<MX_TN, SAT_MX8, SAT_MX8> : k_mx_simple<MX_TN, SAT_MX4, SAT_MX4>, grid, 256, 0)(p);
+    SAT_LAUNCHED(ctx);
+    return sat_splitk_reduce(ctx, part, (int64_t)m * n, (int32_t)splits, accumulate, C, n, n, part_cs, n, colsum);
+}
+
+extern "C" sat_status sat_mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
+{
+    CHECK_CTX(ctx);
+    SAT_TRY(mx_check(ctx, A, "sat_mx_dense_tn"));
+    if (n <= 0 || !C || !ok_ld(ldb, n) || (A->rows > 0 && (!B || !aligned16(B))) || (accumulate != 0 && accumulate != 1))
+        return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: null / misaligned tensor or bad shape");
+    return mx_dense_tn(ctx, A, n, B, ldb, C, colsum, accumulate);
+}
