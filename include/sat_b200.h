@@ -530,7 +530,7 @@ sat_status sat_cache_requantise(sat_ctx *ctx, int32_t layer, int32_t age, int32_
 enum { SAT_MX8 = 8, SAT_MX4 = 4 };
 typedef struct sat_mx_matrix {
     uint8_t *codes, *scales;
-    int64_t rows;                /* up to 2^31 - 1 */
+    int64_t rows;                /* rows and d up to 2^31 - 256 */
     int32_t d, ld_codes, ld_scales;
     int32_t format;              /* SAT_MX8 or SAT_MX4 */
 } sat_mx_matrix;
@@ -546,7 +546,7 @@ sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int
  *   sat_mx_dense_tn  C[A.d x n] (+)= A^^T B[A.rows x n], colsum[n] (+)= 1^T B: weight and bias gradient from a stored input.  C is
  *                    dense row-major, colsum may be NULL; accumulate = 1 adds to both.
  * sat_mx_dense_nt multiplies 4-bit codes exactly and adds in fp32; the other two split fp32 operands into terms that carry all of
- * their 24 bits.  An infinity or a NaN in an fp32 operand makes NaN of every result that it reaches.  Results are bit-reproducible.
+ * their 24 bits (what lies below 2^-133 is dropped).  An infinity or a NaN in an fp32 operand makes NaN of every result that it reaches.  Results are bit-reproducible.
  * Empty sums (no rows, W without rows) are zero, or the bias.  Calls on one context share its workspaces like all calls of this
  * header: two captured graphs with calls of one context must not run at the same time, and the first call of a size may allocate (make
  * it before a capture). */

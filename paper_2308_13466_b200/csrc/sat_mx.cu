@@ -3,95 +3,19 @@
 //   sat_mx_dense_nt   C = A^ W^^T + bias    both operands 4-bit
 //   sat_mx_dense_nn   C = A W^              A fp32
 //   sat_mx_dense_tn   C (+)= A^^T B         B fp32, split over the rows
-#include "sat_internal.h"
-#include "sat_ptx.h"
+#include "sat_mx.h"
 
 #include <algorithm>
 
-#define MX_GROUP 32
-
-static inline int32_t mx_groups(int32_t d) { return (d + MX_GROUP - 1) / MX_GROUP; }
-// bytes of codes in a row, the last group filled up
-static inline int32_t mx_row_bytes(const sat_mx_matrix *q) { return mx_groups(q->d) * (q->format == SAT_MX8 ? 32 : 16); }
-
-// The matrix as kernels take it
-struct MxView {
-    uint8_t *codes, *scales;
-    int64_t ld_codes, ld_scales;
-};
-static inline MxView mx_view(const sat_mx_matrix *q) { return MxView{q->codes, q->scales, q->ld_codes, q->ld_scales}; }
-
 static sat_status mx_check(sat_ctx *ctx, const sat_mx_matrix *q, const char *who)
 {
-    if (!q || (q->format != SAT_MX8 && q->format != SAT_MX4) || q->rows < 0 || q->rows > INT32_MAX || q->d <= 0 || q->d > INT32_MAX - 63)
+    if (!q || (q->format != SAT_MX8 && q->format != SAT_MX4) || q->rows < 0 || q->rows > MX_MAX || q->d <= 0 || q->d > MX_MAX)
         return sat_fail(ctx, SAT_EINVAL, "%s: no microscaled matrix, or one of bad format or shape", who);
     if (q->rows > 0 && (!q->codes || !q->scales || !aligned16(q->codes) || ((uintptr_t)q->scales & 3)))
         return sat_fail(ctx, SAT_EINVAL, "%s: null or misaligned codes / scales", who);
     if (q->ld_codes < mx_row_bytes(q) || (q->ld_codes & 15) || q->ld_scales < mx_groups(q->d) || (q->ld_scales & 3))
         return sat_fail(ctx, SAT_EINVAL, "%s: bad row stride of codes or scales", who);
     return SAT_OK;
-}
-
-// =====================================================================================
-// the two formats
-// =====================================================================================
-// Scale byte of a group from the bits of its largest magnitude: the exponent that brings it to [largest / 2, largest], rounded up from the
-// fraction's compare with 1.75 (448 = 1.75 2^8) or 1.5 (6 = 1.5 2^2) by a carry; 255 where that magnitude is no finite number.
-template <int FMT>
-__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax)
-{
-    if (amax >= 0x7F800000u) return 255u;
-    const int32_t e = (int32_t)((amax + (FMT == SAT_MX8 ? 0x1FFFFFu : 0x3FFFFFu)) >> 23) - (FMT == SAT_MX8 ? 8 : 2);
-    return e > 0 ? (uint32_t)e : 0u;
-}
-// 2^(127 - byte), which is never subnormal: bytes go up to 253, and NaN's comes out as 0.  (x 2^-e is rounded only where it is below
-// 2^-126, far under half a step of either format.)
-__device__ __forceinline__ float mx_inverse(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }
-// 2^(byte - 127); byte 0 is a subnormal number, 255 stands for NaN
-__device__ __forceinline__ float mx_power(uint32_t byte)
-{
-    return byte == 255u ? __uint_as_float(0x7FFFFFFFu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-}
-// four elements -> four bytes (SAT_MX8) or two (SAT_MX4), the first element lowest
-template <int FMT>
-__device__ __forceinline__ uint32_t mx_encode4(float a, float b, float c, float d)
-{
-    uint32_t r;
-    if (FMT == SAT_MX8)
-        asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
-            : "=r"(r)
-            : "f"(a), "f"(b), "f"(c), "f"(d));
-    else
-        asm("{\n\t.reg .b8 l, h, z;\n\tcvt.rn.satfinite.e2m1x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h, l, h};\n\t}"
-            : "=r"(r)
-            : "f"(a), "f"(b), "f"(c), "f"(d));
-    return r;
-}
-// two elements as a pair of halves, without the scale
-template <int FMT>
-__device__ __forceinline__ uint32_t mx_decode2(uint32_t code)
-{
-    uint32_t r;
-    if (FMT == SAT_MX8)
-        asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(r) : "r"(code));
-    else
-        asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(r) : "r"(code));
-    return r;
-}
-__device__ __forceinline__ float2 mx_unpack(uint32_t halves)
-{
-    float2 f;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(halves));
-    return f;
-}
-// element (r, c)
-template <int FMT>
-__device__ __forceinline__ float mx_element(const MxView &q, int64_t r, int32_t c)
-{
-    const float s = mx_power(__ldg(q.scales + r * q.ld_scales + (c >> 5)));
-    if (FMT == SAT_MX8) return mx_unpack(mx_decode2<FMT>(__ldg(q.codes + r * q.ld_codes + c))).x * s;
-    const float2 p = mx_unpack(mx_decode2<FMT>(__ldg(q.codes + r * q.ld_codes + (c >> 1))));
-    return ((c & 1) ? p.y : p.x) * s;
 }
 
 // =====================================================================================
@@ -300,7 +224,7 @@ extern "C" sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, i
     SAT_TRY(mx_check(ctx, W, "sat_mx_dense_nt"));
     if (W->format != SAT_MX4 || (Aq && Aq->format != SAT_MX4)) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: operands are in 4 bits (SAT_MX4)");
     if (Aq) SAT_TRY(mx_check(ctx, Aq, "sat_mx_dense_nt"));
-    if (m < 0 || m > INT32_MAX || (Aq && (Aq->rows != m || Aq->d != W->d)) || W->rows == 0)
+    if (m < 0 || m > MX_MAX || (Aq && (Aq->rows != m || Aq->d != W->d)) || W->rows == 0)
         return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: shapes of the operands do not fit");
     const int32_t n = (int32_t)W->rows, k = W->d;
     if ((m > 0 && !A && !Aq) || (A && (!ok_ld(lda, k) || !aligned16(A))) || !ok_ld(ldc, n) || (m > 0 && (!C || !aligned16(C))))
@@ -328,10 +252,11 @@ extern "C" sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, i
     CHECK_CTX(ctx);
     SAT_TRY(mx_check(ctx, W, "sat_mx_dense_nn"));
     const int32_t n = W->d, k = (int32_t)W->rows;
-    if (m < 0 || m > INT32_MAX || (k > 0 && !ok_ld(lda, k)) || !ok_ld(ldc, n) || (m > 0 && ((k > 0 && (!A || !aligned16(A))) || !C || !aligned16(C))))
+    if (m < 0 || m > MX_MAX || (k > 0 && !ok_ld(lda, k)) || !ok_ld(ldc, n) || (m > 0 && ((k > 0 && (!A || !aligned16(A))) || !C || !aligned16(C))))
         return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nn: null / misaligned tensor or bad shape");
     if (m == 0) return SAT_OK;
     ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
+    if (k > 0 && sat_use_tc(n, k)) return sat_mx_tc_nn(ctx, m, A, lda, W, C, ldc);
     dim3 grid;
     SAT_TRY(mx_grid(ctx, m, n, 1, &grid));
     const MxSimple p{MxView{}, mx_view(W), A, lda, m, k, k, n, nullptr, C, nullptr, ldc};
@@ -344,6 +269,7 @@ static sat_status mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, c
 {
     const int32_t m = A->d;
     ProfScope prof(ctx, SATK_MX, (double)A->rows * (mx_row_bytes(A) + mx_groups(m) + 4.0 * n), 2.0 * (double)A->rows * m * n);
+    if (A->rows > 0 && sat_use_tc(n, m)) return sat_mx_tc_tn(ctx, A, n, B, ldb, C, colsum, accumulate);
     const int64_t rows = A->rows > 0 ? A->rows : 1, tiles = cdiv64(m, 64) * cdiv64(n, 64);
     int64_t splits = std::max<int64_t>(cdiv64(rows, 4096), std::min<int64_t>(cdiv64(4 * ctx->sms, tiles), cdiv64(rows, 64)));
     if (splits > 1024) splits = 1024;
