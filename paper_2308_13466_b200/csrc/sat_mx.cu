@@ -230,6 +230,8 @@ extern "C" sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, i
     if ((m > 0 && !A && !Aq) || (A && (!ok_ld(lda, k) || !aligned16(A))) || !ok_ld(ldc, n) || (m > 0 && (!C || !aligned16(C))))
         return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: null / misaligned tensor or bad leading dimension");
     if (m == 0) return SAT_OK;
+    ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
+    if (sat_use_tc(n, k)) return sat_mx_tc_nt(ctx, m, A, lda, Aq, W, bias, C, ldc);
     sat_mx_matrix tmp;
     if (!Aq) {
         const int32_t groups = mx_groups(k), lds = (groups + 3) & ~3, ldq = groups * 16;
@@ -238,7 +240,6 @@ extern "C" sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, i
         Aq = &tmp;
     }
     if (A) SAT_TRY(mx_quantise(ctx, A, lda, Aq));
-    ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
     dim3 grid;
     SAT_TRY(mx_grid(ctx, m, n, 1, &grid));
     const MxSimple p{mx_view(Aq), mx_view(W), nullptr, 0, m, k, k, n, bias, C, nullptr, ldc};

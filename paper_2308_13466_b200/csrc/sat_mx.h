@@ -79,6 +79,15 @@ __device__ __forceinline__ float mx_element(const MxView &q, int64_t r, int32_t 
     return ((c & 1) ? p.y : p.x) * s;
 }
 
-// Contractions on the tensor cores (sat_mx_tc.cu); shapes are checked by the callers and not empty
+// columns of a tile: as few tiles of at most 256 as possible, of equal width, whole groups
+static inline int32_t mx_tile_columns(int32_t n)
+{
+    const int32_t tiles = (n + 255) / 256;
+    return ((n + tiles - 1) / tiles + MX_GROUP - 1) / MX_GROUP * MX_GROUP;
+}
+
+// Contractions on the tensor cores (sat_mx_nt.cu, sat_mx_tc.cu); shapes are checked by the callers and not empty
 sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc);
 sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate);
+// A (quantised, and kept in Aq where given) or, without it, Aq
+sat_status sat_mx_tc_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias, float *C, int32_t ldc);

@@ -1,0 +1,356 @@
+// Product of 4-bit operands on the 5th-generation tensor cores (sat_mx_dense_nt):
+//     C[m x n] = A^[m x k] W^[n x k]^T + bias,   A fp32 and quantised on the way in, or stored
+// kind::mxf4 with a scale per 32 terms: the tensor core multiplies e2m1 by e2m1, applies both powers of two and adds in fp32; a product
+// has at most six significant bits, so sums are exact or nearly so.  What bounds it is memory: 4 bytes an element of A in, 4 bytes an element of
+// C out, each once; the contraction is under a tenth of that time at the widths of a layer.
+//
+// One CTA per SM walks tiles of 128 rows by up to 256 columns.  24 warps: 0..15 quantise (a warpgroup per 32 of a stage's 128 terms, a
+// thread per row and group, so that a group's maximum needs no exchange), 16..19 the epilogue, 20 MMAs, 21 TMA loads of A, 22 W's codes (TMA) and
+// scales.  Scales lie in shared memory as the tensor core wants them, row r and group g of a stage at (r % 32) 16 + (r / 32) 4 + g, and are
+// copied to TMEM (four columns per 128 rows) in front of the stage's two MMAs.
+#include "sat_mx.h"
+#include "sat_ptx.h"
+
+#include <algorithm>
+
+#define NT_THREADS (24 * 32)
+#define NT_KB 128                       /* terms per stage: 64 bytes of codes, 64-byte swizzle */
+#define NT_OP 3                         /* stages of operand tiles */
+#define NT_RAW 2                        /* boxes of 128 rows x 32 floats per warpgroup in flight */
+#define NT_A_TILE (128 * NT_KB / 2)
+#define NT_W_TILE (256 * NT_KB / 2)
+#define NT_SFA (NT_A_TILE + NT_W_TILE)  /* scales of A: 512 bytes, of W: 1024 */
+#define NT_SFW (NT_SFA + 512)
+#define NT_STAGE (26 * 1024)
+#define NT_BOX (128 * 32 * 4)
+#define NT_TURN (4 * 32 * 36 * 4)
+
+struct NtShared {
+    uint64_t raw_full[4][NT_RAW], raw_empty[4][NT_RAW];   // per warpgroup
+    uint64_t op_full[NT_OP], op_empty[NT_OP];             // 16 quantising warps, W's warp and W's TMA bytes; the MMAs have read them
+    uint64_t acc_full, acc_empty;
+    uint32_t tmem_base;
+    int dead;
+};
+#define NT_SMEM (1024 + NT_OP * NT_STAGE + 4 * NT_RAW * NT_BOX + NT_TURN + (int)sizeof(NtShared))
+static_assert(NT_SFW + 1024 <= NT_STAGE && NT_SMEM <= 227 * 1024, "shared memory");
+
+struct NtArgs {
+    MxView a, w;                 // a: where A comes from or is kept, or null
+    int64_t ldc;
+    int32_t m, n, k, groups, stages;
+    int32_t bn, tiles_n, tiles;
+    const float *bias;
+    float *C;
+    int *status;
+};
+
+// kind::mxf4, e2m1 by e2m1, e8m0 scales; `pair`: which two of a stage's four scales
+__device__ __forceinline__ uint32_t nt_idesc(int32_t bn, uint32_t pair)
+{
+    return (2u * pair) << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 | (2u * pair) << 29;
+}
+__device__ __forceinline__ void nt_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+        "}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void nt_copy_scales(uint32_t taddr, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+struct NtMem {
+    uint8_t *op, *raw;
+    float *turn;
+    NtShared *sh;
+    uint32_t tmem;
+};
+
+__device__ __forceinline__ void nt_issue(const NtArgs &p, const NtMem &s)
+{
+    volatile int *dead = &s.sh->dead;
+    const uint64_t a0 = make_desc(smem_u32(s.op), 16, 512, 4), w0 = make_desc(smem_u32(s.op) + NT_A_TILE, 16, 512, 4);
+    const uint64_t f0 = make_desc(smem_u32(s.op) + NT_SFA, 16, 128, 0);
+    uint32_t st = 0, ph = 0, done = 0;
+    for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x, ++done) {
+        if (!mbar_wait_all(&s.sh->acc_empty, (done & 1u) ^ 1u, dead, p.status)) return;
+        tc_fence_after();
+        for (int32_t k = 0; k < p.stages; ++k) {
+            if (!mbar_wait_all(&s.sh->op_full[st], ph, dead, p.status)) return;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t off = (uint64_t)(st * (NT_STAGE >> 4));
+                const uint32_t sfa = s.tmem + 256u + 16u * st, sfw = sfa + 4u;   // a stage has its own columns: nothing is overwritten in use
+                nt_copy_scales(sfa, f0 + off);
+                nt_copy_scales(sfw, f0 + off + (512 >> 4));
+                if (p.bn > 128) nt_copy_scales(sfw + 4u, f0 + off + (1024 >> 4));
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h)   // 64 terms, 32 bytes of a row
+                    nt_mma(s.tmem, a0 + off + 2 * h, w0 + off + 2 * h, nt_idesc(p.bn, h), sfa, sfw, k > 0 || h > 0 ? 1u : 0u);
+                tc_commit<1>(&s.sh->op_empty[st]);
+                if (k + 1 == p.stages) tc_commit<1>(&s.sh->acc_full);
+            }
+            __syncwarp();
+            if (++st == NT_OP) st = 0, ph ^= 1u;
+        }
+    }
+}
+
+__device__ __forceinline__ void nt_load_a(const NtArgs &p, const NtMem &s, const CUtensorMap *map_a)
+{
+    volatile int *dead = &s.sh->dead;
+    uint32_t slot = 0, ph = 0;
+    for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+        const int32_t m0 = t / p.tiles_n * 128;
+        for (int32_t k = 0; k < p.stages; ++k) {
+            for (int g = 0; g < 4; ++g) {
+                if (!mbar_wait(&s.sh->raw_empty[g][slot], ph ^ 1u, dead, p.status)) return;
+                mbar_expect_tx(&s.sh->raw_full[g][slot], NT_BOX);
+                tma_load_2d(s.raw + (g * NT_RAW + slot) * NT_BOX, map_a, &s.sh->raw_full[g][slot], k * NT_KB + 32 * g, m0);
+            }
+            if (++slot == NT_RAW) slot = 0, ph ^= 1u;
+        }
+    }
+}
+
+__device__ __forceinline__ void nt_load_w(const NtArgs &p, const NtMem &s, const CUtensorMap *map_w, int lane)
+{
+    volatile int *dead = &s.sh->dead;
+    uint32_t st = 0, ph = 0;
+    for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+        const int32_t n0 = t % p.tiles_n * p.bn;
+        for (int32_t k = 0; k < p.stages; ++k) {
+            // four scales of each of up to eight rows; one where there is no such row or group
+            uint32_t f[8];
+            const int32_t left = p.groups - 4 * k;
+            const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : (1u << 8 * left) - 1u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int32_t r = 32 * i + lane;
+                f[i] = 0x7F7F7F7Fu;
+                if (r < p.bn && n0 + r < p.n) f[i] = (__ldg(reinterpret_cast<const uint32_t *>(p.w.scales + (int64_t)(n0 + r) * p.w.ld_scales) + k) & keep) | (0x7F7F7F7Fu & ~keep);
+            }
+            if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, p.status)) return;
+            uint8_t *op = s.op + st * NT_STAGE;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (32 * i < p.bn) *reinterpret_cast<uint32_t *>(op + NT_SFW + (i >> 2) * 512 + lane * 16 + (i & 3) * 4) = f[i];
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_expect_tx(&s.sh->op_full[st], (uint32_t)p.bn * 64u);
+                tma_load_2d(op + NT_A_TILE, map_w, &s.sh->op_full[st], k * (NT_KB / 2), n0);
+            }
+            if (++st == NT_OP) st = 0, ph ^= 1u;
+        }
+    }
+}
+
+// 32 elements -> 16 bytes of codes and the scale byte, as k_mx_quantise does
+__device__ __forceinline__ uint4 nt_quantise(const float4 (&v)[8], uint32_t &byte)
+{
+    uint32_t top[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        top[i] = max(max(__float_as_uint(v[i].x) & 0x7FFFFFFFu, __float_as_uint(v[i].y) & 0x7FFFFFFFu), max(__float_as_uint(v[i].z) & 0x7FFFFFFFu, __float_as_uint(v[i].w) & 0x7FFFFFFFu));
+    byte = mx_scale_byte<SAT_MX4>(max(max(max(top[0], top[1]), max(top[2], top[3])), max(max(top[4], top[5]), max(top[6], top[7]))));
+    if (byte == 255u) return make_uint4(0u, 0u, 0u, 0u);
+    const float f = mx_inverse(byte);
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        c[i] = (mx_encode4<SAT_MX4>(v[2 * i].x * f, v[2 * i].y * f, v[2 * i].z * f, v[2 * i].w * f) & 0xFFFFu) |
+               mx_encode4<SAT_MX4>(v[2 * i + 1].x * f, v[2 * i + 1].y * f, v[2 * i + 1].z * f, v[2 * i + 1].w * f) << 16;
+    return make_uint4(c[0], c[1], c[2], c[3]);
+}
+
+template <bool STORED>
+__device__ __forceinline__ void nt_rows(const NtArgs &p, const NtMem &s, int warp, int lane)
+{
+    volatile int *dead = &s.sh->dead;
+    const int g = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t at = (uint32_t)row * 64u + (uint32_t)((g ^ ((row >> 1) & 3)) << 4), sf_at = NT_SFA + (row & 31) * 16 + (row >> 5) * 4 + g;
+    uint32_t slot = 0, rph = 0, st = 0, ph = 0;
+    for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+        const int64_t r = (int64_t)(t / p.tiles_n) * 128 + row;
+        const bool keep = !STORED && p.a.codes && t % p.tiles_n == 0 && r < p.m;
+        for (int32_t k = 0; k < p.stages; ++k) {
+            uint4 code = make_uint4(0u, 0u, 0u, 0u);
+            uint32_t byte = 127u;
+            const int32_t group = 4 * k + g;
+            if (STORED) {
+                if (r < p.m && group < p.groups) {
+                    code = __ldg(reinterpret_cast<const uint4 *>(p.a.codes + r * p.a.ld_codes) + group);
+                    byte = __ldg(p.a.scales + r * p.a.ld_scales + group);
+                }
+            } else {
+                if (!mbar_wait_all(&s.sh->raw_full[g][slot], rph, dead, p.status)) return;
+                const uint8_t *x = s.raw + (g * NT_RAW + slot) * NT_BOX + row * 128;
+                float4 v[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] = *reinterpret_cast<const float4 *>(x + ((c ^ (row & 7)) << 4));
+                code = nt_quantise(v, byte);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s.sh->raw_empty[g][slot]);
+                if (++slot == NT_RAW) slot = 0, rph ^= 1u;
+                if (keep && group < p.groups) {
+                    *(reinterpret_cast<uint4 *>(p.a.codes + r * p.a.ld_codes) + group) = code;
+                    p.a.scales[r * p.a.ld_scales + group] = (uint8_t)byte;
+                }
+            }
+            if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, p.status)) return;
+            uint8_t *op = s.op + st * NT_STAGE;
+            *reinterpret_cast<uint4 *>(op + at) = code;
+            op[sf_at] = (uint8_t)byte;
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->op_full[st]);
+            if (++st == NT_OP) st = 0, ph ^= 1u;
+        }
+    }
+}
+
+__device__ __forceinline__ void nt_results(const NtArgs &p, const NtMem &s, int warp, int lane)
+{
+    volatile int *dead = &s.sh->dead;
+    float *tb = s.turn + warp * (32 * 36);
+    const uint32_t lanes = s.tmem + ((uint32_t)(warp * 32) << 16);
+    uint32_t done = 0;
+    for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x, ++done) {
+        const int32_t m0 = t / p.tiles_n * 128 + warp * 32, n0 = t % p.tiles_n * p.bn;
+        if (!mbar_wait_all(&s.sh->acc_full, done & 1u, dead, p.status)) return;
+        tc_fence_after();
+        for (int32_t c = 0; c < p.bn; c += 32) {
+            uint32_t acc[32];
+            tc_ld32(lanes + (uint32_t)c, acc);
+            if (c + 32 >= p.bn) {   // the accumulator has been read
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s.sh->acc_empty);
+            }
+            // a lane has a row: blocks of 32 x 32 are turned around so that eight lanes write 128 bytes of one
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4 *>(tb + lane * 36 + e) = make_uint4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+            __syncwarp();
+            const int32_t col = n0 + c + 4 * (lane & 7);
+            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (p.bias) {
+                if (col < p.n) b.x = __ldg(p.bias + col);
+                if (col + 1 < p.n) b.y = __ldg(p.bias + col + 1);
+                if (col + 2 < p.n) b.z = __ldg(p.bias + col + 2);
+                if (col + 3 < p.n) b.w = __ldg(p.bias + col + 3);
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const int32_t row = m0 + i + (lane >> 3);
+                float4 v = *reinterpret_cast<const float4 *>(tb + (i + (lane >> 3)) * 36 + 4 * (lane & 7));
+                v.x += b.x;
+                v.y += b.y;
+                v.z += b.z;
+                v.w += b.w;
+                if (row < p.m && col < p.n) {
+                    float *o = p.C + (int64_t)row * p.ldc + col;
+                    if (col + 4 <= p.n) {
+                        *reinterpret_cast<float4 *>(o) = v;
+                    } else {
+                        o[0] = v.x;
+                        if (col + 1 < p.n) o[1] = v.y;
+                        if (col + 2 < p.n) o[2] = v.z;
+                    }
+                }
+            }
+            __syncwarp();
+        }
+    }
+}
+
+template <bool STORED>
+__global__ void __launch_bounds__(NT_THREADS, 1)
+k_mx_nt(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ NtArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    NtMem s;
+    s.op = smem;
+    s.raw = smem + NT_OP * NT_STAGE;
+    s.turn = reinterpret_cast<float *>(s.raw + 4 * NT_RAW * NT_BOX);
+    s.sh = reinterpret_cast<NtShared *>(s.raw + 4 * NT_RAW * NT_BOX + NT_TURN);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int g = 0; g < 4; ++g)
+            for (int i = 0; i < NT_RAW; ++i) {
+                mbar_init(&s.sh->raw_full[g][i], 1);
+                mbar_init(&s.sh->raw_empty[g][i], 4);
+            }
+        for (int i = 0; i < NT_OP; ++i) {
+            mbar_init(&s.sh->op_full[i], 16 + 1);
+            mbar_init(&s.sh->op_empty[i], 1);
+        }
+        mbar_init(&s.sh->acc_full, 1);
+        mbar_init(&s.sh->acc_empty, 4);
+        s.sh->dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 20) tc_alloc<1>(&s.sh->tmem_base, 512u);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    s.tmem = s.sh->tmem_base;
+    sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
+    if (warp < 16) nt_rows<STORED>(p, s, warp, lane);
+    else if (warp < 20) nt_results(p, s, warp - 16, lane);
+    else if (warp == 20) nt_issue(p, s);
+    else if (warp == 21 && lane == 0 && !STORED) nt_load_a(p, s, &map_a);
+    else if (warp == 22) nt_load_w(p, s, &map_w, lane);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 20) {
+        tc_fence_after();
+        tc_dealloc<1>(s.tmem, 512u);
+    }
+}
+
+template <bool STORED>
+static sat_status nt_launch(sat_ctx *ctx, const CUtensorMap &map_a, const CUtensorMap &map_w, const NtArgs &p)
+{
+    static PerDeviceOnce attr;
+    if (attr.need(ctx->device)) {
+        SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_nt<STORED>, cudaFuncAttributeMaxDynamicSharedMemorySize, NT_SMEM));
+        attr.mark(ctx->device);
+    }
+    sat_pdl(ctx->stream, k_mx_nt<STORED>, (unsigned)std::min(p.tiles, ctx->sms), NT_THREADS, NT_SMEM)(map_a, map_w, p);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
+sat_status sat_mx_tc_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias, float *C, int32_t ldc)
+{
+    NtArgs p{};
+    if (Aq) p.a = mx_view(Aq);
+    p.w = mx_view(W);
+    p.m = (int32_t)m;
+    p.n = (int32_t)W->rows;
+    p.k = W->d;
+    p.groups = mx_groups(p.k);
+    p.stages = (p.groups + 3) / 4;
+    p.bn = mx_tile_columns(p.n);
+    p.tiles_n = (int32_t)cdiv64(p.n, p.bn);
+    if (cdiv64(m, 128) * p.tiles_n > INT32_MAX / 2) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: shape is too large");
+    p.tiles = (int32_t)cdiv64(m, 128) * p.tiles_n;
+    p.bias = bias;
+    p.C = C;
+    p.ldc = ldc;
+    p.status = ctx->d_flag + 1;
+    CUtensorMap map_a{}, map_w;
+    if (A) SAT_TRY(sat_tensor_map(ctx, &map_a, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, p.k, m, (int64_t)lda * 4, 32, 128, CU_TENSOR_MAP_SWIZZLE_128B));
+    SAT_TRY(sat_tensor_map(ctx, &map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, W->codes, mx_row_bytes(W), W->rows, W->ld_codes, NT_KB / 2, p.bn, CU_TENSOR_MAP_SWIZZLE_64B));
+    return A ? nt_launch<false>(ctx, map_a, map_w, p) : nt_launch<true>(ctx, map_a, map_w, p);
+}

@@ -10,7 +10,7 @@
 // have an accumulator of their own.  The hi accumulator is taken out after MX_FLUSH stages (24 instructions) and added up in registers,
 // rounded to nearest; relative error 3e-7 to 1e-6, about that of an fp32 FMA loop.
 //
-// One CTA per SM, 18 warps.  Warps 0..15 convert a stage of 32 terms (raw fp32 and codes in shared memory, brought by TMA, to
+// One CTA per SM, 20 warps, two of them idle.  Warps 0..15 convert a stage of 32 terms (raw fp32 and codes in shared memory, brought by TMA, to
 // swizzled bf16 tiles) and hold the sums; warp 16 issues the MMAs; warp 17 issues the TMA loads and adds up the columns of X where
 // the bias gradient is asked for.  The fp32 operand is the M side (128 lanes of TMEM), the codes are the N side (up to 256 columns).
 #include "sat_mx.h"
@@ -19,7 +19,7 @@
 #include <algorithm>
 
 #define MXT_WORKERS 16
-#define MXT_THREADS ((MXT_WORKERS + 2) * 32)
+#define MXT_THREADS ((MXT_WORKERS + 4) * 32)   /* five whole warpgroups, see k_mx_gemm */
 #define MXT_KB 32                    /* terms per stage */
 #define MXT_OP 3                     /* stages of converted tiles */
 #define MXT_RAW 4                    /* stages of raw tiles */
@@ -83,6 +83,8 @@ __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
 }
 // A code's bits moved to bf16's exponent and fraction are the number times 2^-120 (e4m3) or 2^-126 (e2m1), subnormal codes included; one
 // exact product with a power of two puts that and the group's scale right.  Scales above 2^7 (2^1) need a second one.
+// Integer logic runs at half the rate of multiply-adds, so the bits are moved by the latter: with a code in the low byte of a half-word,
+// code 2^s has its exponent and fraction in place, and (sign bit) (2^t - 2^s) more moves the sign up to bit 15.
 template <int FMT>
 struct MxtScale {
     uint32_t first, second;   // pairs of bf16
@@ -91,35 +93,40 @@ struct MxtScale {
     {
         constexpr uint32_t bias = FMT == SAT_MX8 ? 120u : 126u;
         const uint32_t e = byte + bias;                       // exponent of the whole factor + 127
-        two = e > 254u && byte != 255u;
+        two = e > 254u;
         const uint32_t f = byte == 255u ? 0x7FFFu : two ? 254u << 7 : e << 7;
-        first = f | f << 16;
-        const uint32_t g = two ? (e - 127u) << 7 : 0x3F80u;   // what is left of it: e - 127 - 127, plus 127
-        second = g | g << 16;
-    }
-    __device__ __forceinline__ uint32_t operator()(uint32_t v) const
-    {
-        v = bf16x2_mul(v, first);
-        return two ? bf16x2_mul(v, second) : v;
+        first = f * 0x10001u;
+        second = byte == 255u ? 0x3F803F80u : ((e - 127u) << 7) * 0x10001u;   // what is left of it: e - 127 - 127, plus 127
     }
 };
-// eight elements: two words of e4m3 or one of e2m1 -> four pairs, in order
-__device__ __forceinline__ uint4 mxt_spread8(uint32_t lo, uint32_t hi)
+// eight elements (two words of e4m3 or one of e2m1) as four pairs of bf16, in order
+template <int FMT>
+__device__ __forceinline__ uint4 mxt_decode8(uint32_t lo, uint32_t hi, const MxtScale<FMT> &sc)
 {
-    const uint32_t x[4] = {__byte_perm(lo, 0, 0x1404), __byte_perm(lo, 0, 0x3424), __byte_perm(hi, 0, 0x1404), __byte_perm(hi, 0, 0x3424)};
-    uint32_t v[4];
+    uint32_t x[4];
+    if (FMT == SAT_MX8) {
+        x[0] = __byte_perm(lo, 0, 0x4140);
+        x[1] = __byte_perm(lo, 0, 0x4342);
+        x[2] = __byte_perm(hi, 0, 0x4140);
+        x[3] = __byte_perm(hi, 0, 0x4342);
+    } else {
+        const uint32_t even = lo & 0x0F0F0F0Fu, odd = (lo >> 4) & 0x0F0F0F0Fu;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = ((x[i] >> 4) & 0x07F007F0u) | (x[i] & 0x80008000u);
-    return make_uint4(v[0], v[1], v[2], v[3]);
+        for (uint32_t i = 0; i < 4; ++i) {
+            // byte i of either, and their sign bits, which are zero, above them
+            asm("prmt.b32 %0, %1, %2, %3;" : "=r"(x[i]) : "r"(even), "r"(odd), "r"(0xC480u + 0x1111u * i));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t sign = x[i] & (FMT == SAT_MX8 ? 0x00800080u : 0x00080008u);
+        x[i] = bf16x2_mul(x[i] * (FMT == SAT_MX8 ? 16u : 64u) + sign * (FMT == SAT_MX8 ? 256u - 16u : 4096u - 64u), sc.first);
+    }
+    return make_uint4(x[0], x[1], x[2], x[3]);
 }
-__device__ __forceinline__ uint4 mxt_spread4(uint32_t w)
+__device__ __forceinline__ uint4 bf16x8_mul(const uint4 &v, uint32_t s)
 {
-    const uint32_t e = w << 4;   // byte j: the even element of pair j in its upper half
-    const uint32_t x[4] = {__byte_perm(e, w, 0x4000), __byte_perm(e, w, 0x5010), __byte_perm(e, w, 0x6020), __byte_perm(e, w, 0x7030)};
-    uint32_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = ((x[i] >> 6) & 0x01C001C0u) | (x[i] & 0x80008000u);
-    return make_uint4(v[0], v[1], v[2], v[3]);
+    return make_uint4(bf16x2_mul(v.x, s), bf16x2_mul(v.y, s), bf16x2_mul(v.z, s), bf16x2_mul(v.w, s));
 }
 // eight fp32 values -> eight bf16 each of hi, mid, lo (upper halves; what is left after two of them fits a third)
 __device__ __forceinline__ void mxt_split8(const float4 &a, const float4 &b, uint4 &hi, uint4 &mid, uint4 &lo)
@@ -128,12 +135,10 @@ __device__ __forceinline__ void mxt_split8(const float4 &a, const float4 &b, uin
     uint32_t h[4], m[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t u0 = __float_as_uint(x[2 * i]), u1 = __float_as_uint(x[2 * i + 1]);
-        const float r0 = x[2 * i] - __uint_as_float(u0 & 0xFFFF0000u), r1 = x[2 * i + 1] - __uint_as_float(u1 & 0xFFFF0000u);
-        const uint32_t v0 = __float_as_uint(r0), v1 = __float_as_uint(r1);
-        const float s0 = r0 - __uint_as_float(v0 & 0xFFFF0000u), s1 = r1 - __uint_as_float(v1 & 0xFFFF0000u);
-        h[i] = __byte_perm(u0, u1, 0x7632);
-        m[i] = __byte_perm(v0, v1, 0x7632);
+        h[i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
+        const float r0 = x[2 * i] - __uint_as_float(h[i] * 0x10000u), r1 = x[2 * i + 1] - __uint_as_float(h[i] & 0xFFFF0000u);
+        m[i] = __byte_perm(__float_as_uint(r0), __float_as_uint(r1), 0x7632);
+        const float s0 = r0 - __uint_as_float(m[i] * 0x10000u), s1 = r1 - __uint_as_float(m[i] & 0xFFFF0000u);
         l[i] = __byte_perm(__float_as_uint(s0), __float_as_uint(s1), 0x7632);
     }
     hi = make_uint4(h[0], h[1], h[2], h[3]);
@@ -307,23 +312,25 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int3
     const bool has_q = 16 * place < a.bn;
     const int chunks = a.bn / 32;
 
-    // scale bytes come two stages ahead
-    int32_t ahead = first;
-    int32_t ahead_k = 0;
-    MxtItem at{};
-    if (ahead < a.items) at = mxt_item(a, ahead);
+    // scale bytes come two stages ahead: `left` more terms of the item ahead, the byte of its next stage at `next`
+    int32_t ahead = first, left = 0;
+    const uint8_t *next = a.scales;
+    bool in_range = false;
+    const int64_t stage_scales = a.ld_scales * MXT_KB;
     auto scale = [&]() -> uint32_t {
-        uint32_t byte = 127u;
-        if (ahead < a.items) {
-            const int32_t k = at.k0 + ahead_k * MXT_KB + term;
-            const int32_t g = (at.n0 + 16 * place) / MX_GROUP;
-            if (has_q && k < at.k1 && g < a.groups) byte = __ldg(a.scales + (int64_t)k * a.ld_scales + g);
-            if (++ahead_k == at.stages) {
-                ahead_k = 0;
-                ahead += step;
-                if (ahead < a.items) at = mxt_item(a, ahead);
-            }
+        if (left <= 0) {
+            if (ahead >= a.items) return 127u;
+            const MxtItem t = mxt_item(a, ahead);
+            const int32_t g = (t.n0 + 16 * place) / MX_GROUP;
+            in_range = has_q && g < a.groups;
+            next = a.scales + (int64_t)(t.k0 + term) * a.ld_scales + g;
+            left = t.k1 - t.k0;
+            ahead += step;
         }
+        uint32_t byte = 127u;
+        if (in_range && term < left) byte = __ldg(next);
+        next += stage_scales;
+        left -= MXT_KB;
         return byte;
     };
     uint32_t b0 = scale(), b1 = scale();
@@ -355,6 +362,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int3
             ++taken;
         };
         int32_t in_run = 0;
+#pragma unroll 1
         for (int32_t k = 0; k < it.stages; ++k) {
             const uint32_t byte = b0;
             b0 = b1;
@@ -379,9 +387,8 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int3
             uint4 h, m, l;
             mxt_split8(xa, xb, h, m, l);
             const MxtScale<FMT> sc(byte);
-            uint4 v0 = FMT == SAT_MX8 ? mxt_spread8(c[0], c[1]) : mxt_spread4(c[0]), v1 = FMT == SAT_MX8 ? mxt_spread8(c[2], c[3]) : mxt_spread4(c[1]);
-            v0 = make_uint4(sc(v0.x), sc(v0.y), sc(v0.z), sc(v0.w));
-            v1 = make_uint4(sc(v1.x), sc(v1.y), sc(v1.z), sc(v1.w));
+            uint4 v0 = mxt_decode8<FMT>(c[0], c[1], sc), v1 = FMT == SAT_MX8 ? mxt_decode8<FMT>(c[2], c[3], sc) : mxt_decode8<FMT>(c[1], 0u, sc);
+            if (sc.two) v0 = bf16x8_mul(v0, sc.second), v1 = bf16x8_mul(v1, sc.second);
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->raw_empty[rst]);
             if (++rst == MXT_RAW) rst = 0, rph ^= 1u;
@@ -501,22 +508,22 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
     sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
-    if (warp == MXT_WORKERS) mxt_mma<TN>(a, s, blockIdx.x, gridDim.x);
-    else if (warp > MXT_WORKERS) mxt_load<TN, FMT>(a, s, &map_x, &map_q, blockIdx.x, gridDim.x, lane);
-    else mxt_work<TN, FMT>(a, s, blockIdx.x, gridDim.x, warp, lane);
+    // 640 threads start with 96 registers each; the four warpgroups of workers, which hold 64 sums a thread, go to 104 and the fifth one
+    // to 64: 4 x 104 + 64 = 5 x 96
+    if (warp < MXT_WORKERS) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        mxt_work<TN, FMT>(a, s, blockIdx.x, gridDim.x, warp, lane);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == MXT_WORKERS) mxt_mma<TN>(a, s, blockIdx.x, gridDim.x);
+        else if (warp == MXT_WORKERS + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, blockIdx.x, gridDim.x, lane);
+    }
     tc_fence_before();
     __syncthreads();
     if (warp == MXT_WORKERS) {
         tc_fence_after();
         tc_dealloc<1>(s.tmem, 512u);
     }
-}
-
-// columns of a tile: as few tiles of at most 256 as possible, of equal width, whole groups
-static int32_t mxt_columns(int32_t n)
-{
-    const int32_t tiles = (n + 255) / 256;
-    return ((n + tiles - 1) / tiles + MX_GROUP - 1) / MX_GROUP * MX_GROUP;
 }
 
 static sat_status mxt_map_q(sat_ctx *ctx, CUtensorMap *map, const sat_mx_matrix *q, int32_t bn)
@@ -546,7 +553,7 @@ sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, co
     a.M = (int32_t)m;
     a.N = W->d;
     a.K = a.kps = (int32_t)W->rows;
-    a.bn = mxt_columns(a.N);
+    a.bn = mx_tile_columns(a.N);
     a.tiles_m = (int32_t)cdiv64(m, 128);
     a.tiles_n = (int32_t)cdiv64(a.N, a.bn);
     if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX / 2) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nn: shape is too large");
@@ -569,7 +576,7 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
     a.M = n;
     a.N = A->d;
     a.K = (int32_t)A->rows;
-    a.bn = mxt_columns(a.N);
+    a.bn = mx_tile_columns(a.N);
     a.tiles_m = (int32_t)cdiv64(n, 128);
     a.tiles_n = (int32_t)cdiv64(a.N, a.bn);
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, stages = cdiv64(a.K, MXT_KB);
