@@ -15,7 +15,7 @@
 
 #define NT_THREADS (24 * 32)
 #define NT_KB 128                       /* terms per stage: 64 bytes of codes, 64-byte swizzle */
-#define NT_OP 3                         /* stages of operand tiles */
+#define NT_OP 2                         /* stages of operand tiles */
 #define NT_RAW 2                        /* boxes of 128 rows x 32 floats per warpgroup in flight */
 #define NT_A_TILE (128 * NT_KB / 2)
 #define NT_W_TILE (256 * NT_KB / 2)
@@ -23,7 +23,8 @@
 #define NT_SFW (NT_SFA + 512)
 #define NT_STAGE (26 * 1024)
 #define NT_BOX (128 * 32 * 4)
-#define NT_TURN (4 * 32 * 36 * 4)
+#define NT_OUT (4 * 2 * 4096)            /* results on their way out: two blocks of 32 x 32 per warp */
+#define NT_BIAS (4 * 256 * 4)
 
 struct NtShared {
     uint64_t raw_full[4][NT_RAW], raw_empty[4][NT_RAW];   // per warpgroup
@@ -32,7 +33,7 @@ struct NtShared {
     uint32_t tmem_base;
     int dead;
 };
-#define NT_SMEM (1024 + NT_OP * NT_STAGE + 4 * NT_RAW * NT_BOX + NT_TURN + (int)sizeof(NtShared))
+#define NT_SMEM (1024 + NT_OP * NT_STAGE + 4 * NT_RAW * NT_BOX + NT_OUT + NT_BIAS + (int)sizeof(NtShared))
 static_assert(NT_SFW + 1024 <= NT_STAGE && NT_SMEM <= 227 * 1024, "shared memory");
 
 struct NtArgs {
@@ -67,8 +68,7 @@ __device__ __forceinline__ void nt_copy_scales(uint32_t taddr, uint64_t desc)
 }
 
 struct NtMem {
-    uint8_t *op, *raw;
-    float *turn;
+    uint8_t *op, *raw, *out;
     NtShared *sh;
     uint32_t tmem;
 };
@@ -217,71 +217,75 @@ __device__ __forceinline__ void nt_rows(const NtArgs &p, const NtMem &s, int war
     }
 }
 
-__device__ __forceinline__ void nt_results(const NtArgs &p, const NtMem &s, int warp, int lane)
+// A lane has a row of a block of 32 x 32; it goes to shared memory (128 bytes a row, swizzled) and from there out by TMA, which leaves out
+// what lies behind the edges
+__device__ __forceinline__ void nt_results(const NtArgs &p, const NtMem &s, const CUtensorMap *map_c, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    float *tb = s.turn + warp * (32 * 36);
+    float *bias = reinterpret_cast<float *>(s.out + NT_OUT) + warp * 256;
     const uint32_t lanes = s.tmem + ((uint32_t)(warp * 32) << 16);
-    uint32_t done = 0;
+    uint32_t done = 0, buf = 0;
+    int32_t bias_of = -1;
     for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x, ++done) {
         const int32_t m0 = t / p.tiles_n * 128 + warp * 32, n0 = t % p.tiles_n * p.bn;
-        if (!mbar_wait_all(&s.sh->acc_full, done & 1u, dead, p.status)) return;
+        if (p.bias && n0 != bias_of) {
+            for (int32_t c = lane; c < p.bn; c += 32) bias[c] = n0 + c < p.n ? __ldg(p.bias + n0 + c) : 0.f;
+            __syncwarp();
+            bias_of = n0;
+        }
+        if (!mbar_wait_all(&s.sh->acc_full, done & 1u, dead, p.status)) break;
         tc_fence_after();
         for (int32_t c = 0; c < p.bn; c += 32) {
-            uint32_t acc[32];
-            tc_ld32(lanes + (uint32_t)c, acc);
+            uint32_t r[32];
+            tc_ld32(lanes + (uint32_t)c, r);
             if (c + 32 >= p.bn) {   // the accumulator has been read
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s.sh->acc_empty);
             }
-            // a lane has a row: blocks of 32 x 32 are turned around so that eight lanes write 128 bytes of one
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4 *>(tb + lane * 36 + e) = make_uint4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+            if (m0 >= p.m || n0 + c >= p.n) continue;
+            uint8_t *o = s.out + (2 * warp + buf) * 4096;
+            if (lane == 0) tma_store_wait_read<1>();
             __syncwarp();
-            const int32_t col = n0 + c + 4 * (lane & 7);
-            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (p.bias) {
-                if (col < p.n) b.x = __ldg(p.bias + col);
-                if (col + 1 < p.n) b.y = __ldg(p.bias + col + 1);
-                if (col + 2 < p.n) b.z = __ldg(p.bias + col + 2);
-                if (col + 3 < p.n) b.w = __ldg(p.bias + col + 3);
-            }
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const int32_t row = m0 + i + (lane >> 3);
-                float4 v = *reinterpret_cast<const float4 *>(tb + (i + (lane >> 3)) * 36 + 4 * (lane & 7));
-                v.x += b.x;
-                v.y += b.y;
-                v.z += b.z;
-                v.w += b.w;
-                if (row < p.m && col < p.n) {
-                    float *o = p.C + (int64_t)row * p.ldc + col;
-                    if (col + 4 <= p.n) {
-                        *reinterpret_cast<float4 *>(o) = v;
-                    } else {
-                        o[0] = v.x;
-                        if (col + 1 < p.n) o[1] = v.y;
-                        if (col + 2 < p.n) o[2] = v.z;
-                    }
+            for (int e = 0; e < 8; ++e) {
+                float4 v = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]), __uint_as_float(r[4 * e + 2]), __uint_as_float(r[4 * e + 3]));
+                if (p.bias) {
+                    const float4 b = *reinterpret_cast<const float4 *>(bias + c + 4 * e);
+                    v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
                 }
+                *reinterpret_cast<float4 *>(o + lane * 128 + ((e ^ (lane & 7)) << 4)) = v;
             }
+            if (n0 + c + 32 > p.n && (p.n & 3)) {   // a bulk store writes the last 16 bytes of a row whole
+                __syncwarp();
+                for (int i = 0; i < 32; ++i)
+                    if (m0 + i < p.m && n0 + c + lane < p.n)
+                        p.C[(int64_t)(m0 + i) * p.ldc + n0 + c + lane] = *reinterpret_cast<const float *>(o + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
+                __syncwarp();
+                continue;
+            }
+            fence_async_smem();
             __syncwarp();
+            if (lane == 0) tma_store_2d(map_c, o, n0 + c, m0);
+            buf ^= 1u;
         }
+        __syncwarp();   // (the bias of another tile is not written while a lane still reads this one's)
     }
+    if (lane == 0) tma_store_wait_all();
 }
 
 template <bool STORED>
 __global__ void __launch_bounds__(NT_THREADS, 1)
-k_mx_nt(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ NtArgs p)
+k_mx_nt(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_c,
+        const __grid_constant__ NtArgs p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     NtMem s;
     s.op = smem;
     s.raw = smem + NT_OP * NT_STAGE;
-    s.turn = reinterpret_cast<float *>(s.raw + 4 * NT_RAW * NT_BOX);
-    s.sh = reinterpret_cast<NtShared *>(s.raw + 4 * NT_RAW * NT_BOX + NT_TURN);
+    s.out = s.raw + 4 * NT_RAW * NT_BOX;
+    s.sh = reinterpret_cast<NtShared *>(s.out + NT_OUT + NT_BIAS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int g = 0; g < 4; ++g)
@@ -305,7 +309,7 @@ k_mx_nt(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
     s.tmem = s.sh->tmem_base;
     sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
     if (warp < 16) nt_rows<STORED>(p, s, warp, lane);
-    else if (warp < 20) nt_results(p, s, warp - 16, lane);
+    else if (warp < 20) nt_results(p, s, &map_c, warp - 16, lane);
     else if (warp == 20) nt_issue(p, s);
     else if (warp == 21 && lane == 0 && !STORED) nt_load_a(p, s, &map_a);
     else if (warp == 22) nt_load_w(p, s, &map_w, lane);
@@ -319,14 +323,14 @@ k_mx_nt(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
 }
 
 template <bool STORED>
-static sat_status nt_launch(sat_ctx *ctx, const CUtensorMap &map_a, const CUtensorMap &map_w, const NtArgs &p)
+static sat_status nt_launch(sat_ctx *ctx, const CUtensorMap &map_a, const CUtensorMap &map_w, const CUtensorMap &map_c, const NtArgs &p)
 {
     static PerDeviceOnce attr;
     if (attr.need(ctx->device)) {
         SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_nt<STORED>, cudaFuncAttributeMaxDynamicSharedMemorySize, NT_SMEM));
         attr.mark(ctx->device);
     }
-    sat_pdl(ctx->stream, k_mx_nt<STORED>, (unsigned)std::min(p.tiles, ctx->sms), NT_THREADS, NT_SMEM)(map_a, map_w, p);
+    sat_pdl(ctx->stream, k_mx_nt<STORED>, (unsigned)std::min(p.tiles, ctx->sms), NT_THREADS, NT_SMEM)(map_a, map_w, map_c, p);
     SAT_LAUNCHED(ctx);
     return SAT_OK;
 }
@@ -349,8 +353,9 @@ sat_status sat_mx_tc_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, co
     p.C = C;
     p.ldc = ldc;
     p.status = ctx->d_flag + 1;
-    CUtensorMap map_a{}, map_w;
+    CUtensorMap map_a{}, map_w, map_c;
     if (A) SAT_TRY(sat_tensor_map(ctx, &map_a, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, p.k, m, (int64_t)lda * 4, 32, 128, CU_TENSOR_MAP_SWIZZLE_128B));
     SAT_TRY(sat_tensor_map(ctx, &map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, W->codes, mx_row_bytes(W), W->rows, W->ld_codes, NT_KB / 2, p.bn, CU_TENSOR_MAP_SWIZZLE_64B));
-    return A ? nt_launch<false>(ctx, map_a, map_w, p) : nt_launch<true>(ctx, map_a, map_w, p);
+    SAT_TRY(sat_tensor_map(ctx, &map_c, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, C, p.n, m, (int64_t)ldc * 4, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B));
+    return A ? nt_launch<false>(ctx, map_a, map_w, map_c, p) : nt_launch<true>(ctx, map_a, map_w, map_c, p);
 }
