@@ -119,38 +119,6 @@ __device__ __forceinline__ void split_tile_residual(const uint8_t *hi_tile, uint
         if (two) *reinterpret_cast<float4 *>(lo_tile + off2) = residual4(x2);
     }
 }
-// A warp's arrival on a barrier that the MMA issuer waits for.  CTAS = 1: every lane arrives.  2: lane 0 does, on the barrier at the same
-// place in CTA 0 of the pair, without a scope, that is at CTA scope.  An assumption rests on that: that shared-memory writes in front of
-// the proxy fence and TMEM reads in front of their wait are done for the pair's MMAs when the arrival is seen.  The memory model does not
-// say so across two CTAs; it is the form in which CUTLASS's cluster barriers arrive at the other CTA of a pair, and
-// tests/test_gpu_edges.py compares pair launches with single CTAs bit by bit.  (With .release.cluster the arrival also waits for
-// everything else the SM has in flight, 1.4 us: a 179250 x 512 x 512 contraction took 490 us instead of 370; waits that acquire at
-// cluster scope, which would be half of it, cost 0.3-0.5 % of an epoch.)
-template <int CTAS>
-__device__ __forceinline__ void mbar_arrive_warp(uint64_t *bar, int lane)
-{
-    if (CTAS == 1) {
-        mbar_arrive(bar);
-        return;
-    }
-    __syncwarp();
-    if (lane == 0)
-        asm volatile(
-            "{\n\t"
-            ".reg .b32 a;\n\t"
-            "mapa.shared::cluster.u32 a, %0, 0;\n\t"
-            "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t"
-            "}" ::"r"(smem_u32(bar))
-            : "memory");
-}
-// lane 0's arrival on the same barriers with single CTAs too
-template <int CTAS>
-__device__ __forceinline__ void mbar_arrive_lane0(uint64_t *bar, int lane)
-{
-    __syncwarp();
-    if (CTAS == 2) mbar_arrive_warp<CTAS>(bar, lane);
-    else if (lane == 0) mbar_arrive(bar);
-}
 // =====================================================================================
 // K-major kernel
 // =====================================================================================

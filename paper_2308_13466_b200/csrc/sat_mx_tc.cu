@@ -1,18 +1,23 @@
 // Contractions of fp32 rows with microscaled matrices on the 5th-generation tensor cores.
-//     k_mx_gemm<true>    C[q.d x n] = Q^^T X     sat_mx_dense_tn: the terms run over the rows of both, split over CTAs
+//     k_mx_gemm<true>    C[q.d x n] = Q^^T X     sat_mx_dense_tn: the terms run over the rows of both, split over CTA pairs
 //     k_mx_gemm<false>   C[m x q.d] = X Q^       sat_mx_dense_nn: the terms run over the columns of X and the rows of Q
 // What a code stands for has four significant bits and a power of two, so it is a bf16 number.  An fp32 operand is cut into three bf16
 // terms by taking the upper half of its bits off twice, which is exact: x = hi + mid + lo, eight bits each.  Three MMAs of
 // kind::f16 with bf16 operands then give exact products, and all that is rounded is the sum.
 //
-// The tensor core chops its running sum at every instruction (16 products), always towards zero, so a sum in one accumulator drifts:
+// The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts:
 // about a third of a unit of 2^-23 per instruction.  Only the products with hi matter for that; those with mid and lo are 2^-8 of them and
-// have an accumulator of their own.  The hi accumulator is taken out after MX_FLUSH stages (24 instructions) and added up in registers,
+// have an accumulator of their own.  The hi accumulator is taken out after MXT_FLUSH stages (24 instructions) and added up in registers,
 // rounded to nearest; relative error 3e-7 to 1e-6, about that of an fp32 FMA loop.
 //
-// One CTA per SM, 20 warps, two of them idle.  Warps 0..15 convert a stage of 32 terms (raw fp32 and codes in shared memory, brought by TMA, to
-// swizzled bf16 tiles) and hold the sums; warp 16 issues the MMAs; warp 17 issues the TMA loads and adds up the columns of X where
-// the bias gradient is asked for.  The fp32 operand is the M side (128 lanes of TMEM), the codes are the N side (up to 256 columns).
+// A pair of CTAs shares a tile of 256 columns of Q (the M side, 128 lanes of TMEM in either CTA) by up to 256 columns (TN) or rows (NN) of
+// X.  What bounds it besides memory is shared memory, at 128 bytes a clock: per stage of 32 terms a CTA takes in 16 KB of X and 4 KB of codes
+// (written by TMA, read once), writes 24 KB and 8 KB of bf16, and the tensor core reads 32 KB (each CTA holds one half of X, and a tile of Q
+// stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  With single CTAs and X as the M side it
+// was 183 KB for as many products.
+//
+// 20 warps.  Warps 0..15 convert, in two groups on alternate stages, and hold the sums; warp 16 of the first CTA issues the MMAs; warp 17 the
+// loads; warp 18 adds up the columns of X where the bias gradient is asked for.
 #include "sat_mx.h"
 #include "sat_ptx.h"
 
@@ -21,53 +26,52 @@
 #define MXT_WORKERS 16
 #define MXT_THREADS ((MXT_WORKERS + 4) * 32)   /* five whole warpgroups, see k_mx_gemm */
 #define MXT_KB 32                    /* terms per stage */
-#define MXT_OP 3                     /* stages of converted tiles */
-#define MXT_RAW 4                    /* stages of raw tiles */
+#define MXT_RING 4                   /* stages of raw and of converted tiles; a power of two */
 #define MXT_FLUSH 12                 /* stages between two reads of the hi accumulator */
+#define MXT_Q_TILE (128 * MXT_KB * 2)
 #define MXT_X_PLANE (128 * MXT_KB * 2)
-#define MXT_Q_TILE (256 * MXT_KB * 2)
-#define MXT_STAGE (3 * MXT_X_PLANE + MXT_Q_TILE)
+#define MXT_STAGE (MXT_Q_TILE + 3 * MXT_X_PLANE)
 #define MXT_X_RAW (128 * MXT_KB * 4)
-#define MXT_Q_RAW (256 * MXT_KB)
+#define MXT_Q_RAW (128 * MXT_KB)
 #define MXT_RAW_STAGE (MXT_X_RAW + MXT_Q_RAW)
+#define MXT_SCALES (MXT_KB * 4)       /* of a stage: four groups a term */
 
 struct MxtShared {
-    uint64_t raw_full[MXT_RAW], raw_empty[MXT_RAW];   // TMA bytes have landed; the workers (and the column sums) have read them
-    uint64_t op_full[MXT_OP], op_empty[MXT_OP];       // the workers have written the tiles; the MMAs have read them
-    uint64_t acc_full, acc_empty;                     // the hi accumulator is to be taken out; has been
-    uint64_t turned;                                  // (NN) the results have left the operand stages
+    uint8_t scales[MXT_RING][MXT_SCALES];
+    uint64_t raw_full[MXT_RING], raw_empty[MXT_RING];   // TMA bytes and scales have landed; a group of workers (and the column sums) has read them
+    uint64_t op_full[MXT_RING], op_empty[MXT_RING];     // (first CTA) both CTAs' workers have written the tiles; the MMAs have read them
+    uint64_t acc_full, acc_empty;                       // the hi accumulator is to be taken out; (first CTA) both CTAs have
     uint32_t tmem_base;
     int dead;
 };
-#define MXT_SMEM (1024 + MXT_OP * MXT_STAGE + MXT_RAW * MXT_RAW_STAGE + (int)sizeof(MxtShared))
+#define MXT_SMEM (1024 + MXT_RING * (MXT_STAGE + MXT_RAW_STAGE) + (int)sizeof(MxtShared))
 static_assert(MXT_SMEM <= 227 * 1024, "shared memory");
-static_assert(MXT_OP * MXT_STAGE >= MXT_WORKERS * 32 * 36 * 4, "the results are turned around in the operand stages");
 
 struct MxtArgs {
     const uint8_t *scales;
     int64_t ld_scales;
     int32_t groups;            // of a row of Q
-    int32_t M, N;              // rows of the tile grid: columns of X (TN) or rows of X (NN); columns of Q
+    int32_t D, N;              // columns of Q; columns (TN) or rows (NN) of X
     int32_t K, kps;            // terms, and terms of a split (a multiple of MXT_KB)
-    int32_t bn, tiles_m, tiles_n;
+    int32_t bn, tiles_d, tiles_n;
     int32_t items;             // tiles times splits, the tiles of a split next to each other
-    float *C;                  // TN: [splits][N][M] partial sums, or with one split the result; NN: [M x ldc]
-    int64_t ldc;
-    float *colsum;             // TN: [splits][M] column sums of X, or none
-    int direct, accumulate;    // TN with one split: C and colsum are the results, and are added to
+    float *C;                  // element (column j of Q, column or row i of X) of split z at C + z split + i by_x + j by_q
+    int64_t split, by_x, by_q;
+    float *colsum;             // TN: [splits][N] column sums of X, or none
+    int add;                   // to what is there
     int *status;
 };
 // A tile and its terms [k0, k1)
 struct MxtItem {
-    int32_t m0, n0, split, k0, k1, stages;
+    int32_t d0, n0, split, k0, k1, stages;
 };
 __device__ __forceinline__ MxtItem mxt_item(const MxtArgs &a, int32_t i)
 {
     MxtItem t;
-    const int32_t tiles = a.tiles_m * a.tiles_n, tile = i % tiles;
+    const int32_t tiles = a.tiles_d * a.tiles_n, tile = i % tiles;
     t.split = i / tiles;
-    t.m0 = tile / a.tiles_n * 128;
-    t.n0 = tile % a.tiles_n * a.bn;
+    t.d0 = tile % a.tiles_d * 256;
+    t.n0 = tile / a.tiles_d * a.bn;
     t.k0 = t.split * a.kps;
     t.k1 = a.K - t.k0 < a.kps ? a.K : t.k0 + a.kps;
     t.stages = (t.k1 - t.k0 + MXT_KB - 1) / MXT_KB;
@@ -160,7 +164,7 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t *r)
 template <bool TN>
 __device__ __forceinline__ uint32_t mxt_idesc(int32_t bn)
 {
-    return 1u << 4 | 1u << 7 | 1u << 10 | (TN ? 1u << 15 : 0u) | 1u << 16 | (uint32_t)(bn >> 3) << 17 | (128u >> 4) << 24;
+    return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | (TN ? 1u << 16 : 0u) | (uint32_t)(bn >> 3) << 17 | (256u >> 4) << 24;
 }
 
 // ---- the roles --------------------------------------------------------------------------------------------------------------
@@ -168,103 +172,123 @@ struct MxtMem {
     uint8_t *op, *raw;
     MxtShared *sh;
     uint32_t tmem;
+    int32_t rank;              // CTA of the pair
+    int32_t unit, units;       // pair, and pairs
 };
 
 template <bool TN>
-__device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s, int32_t first, int32_t step)
+__device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
 {
     volatile int *dead = &s.sh->dead;
-    const uint32_t idesc = mxt_idesc<TN>(a.bn);
+    const uint32_t idesc = mxt_idesc<TN>(a.bn), hi = s.tmem, rest = s.tmem + 256u;
     // MN-major tiles: blocks of 64 columns (128 bytes a term, 128-byte swizzle) MXT_KB x 128 bytes apart, groups of eight terms 1024 bytes
     // apart; an instruction takes 16 terms.  K-major (X without TN): a row's 32 terms are 64 bytes, 64-byte swizzle, eight rows 512 apart.
-    const uint64_t q0 = make_desc(smem_u32(s.op) + 3 * MXT_X_PLANE, MXT_KB * 128, 1024, 2);
-    const uint64_t x0 = TN ? make_desc(smem_u32(s.op), MXT_KB * 128, 1024, 2) : make_desc(smem_u32(s.op), 16, 512, 4);
+    const uint64_t q0 = make_desc(smem_u32(s.op), MXT_KB * 128, 1024, 2);
+    const uint64_t x0 = TN ? make_desc(smem_u32(s.op) + MXT_Q_TILE, MXT_KB * 128, 1024, 2) : make_desc(smem_u32(s.op) + MXT_Q_TILE, 16, 512, 4);
     constexpr uint32_t x_step = (TN ? 2048 : 32) >> 4, q_step = 2048 >> 4, plane = MXT_X_PLANE >> 4;
-    uint32_t st = 0, ph = 0, taken = 0;   // taken: times the accumulators were handed over so far
-    for (int32_t i = first; i < a.items; i += step) {
+    uint32_t g = 0, taken = 0;   // stages so far; times the accumulators were handed over
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
         int32_t in_run = 0;               // stages since the hi accumulator was last handed over
-        for (int32_t k = 0; k < stages; ++k) {
-            if (!mbar_wait_all(&s.sh->op_full[st], ph, dead, a.status)) return;
-            tc_fence_after();
-            const uint64_t x = x0 + (uint64_t)(st * (MXT_STAGE >> 4)), q = q0 + (uint64_t)(st * (MXT_STAGE >> 4));
+        for (int32_t k = 0; k < stages; ++k, ++g) {
+            const uint32_t st = g % MXT_RING;
+            if (!mbar_wait_all(&s.sh->op_full[st], (g / MXT_RING) & 1u, dead, a.status)) return;
             // (acc_empty's phase `taken - 1` completes when the workers have read what was handed over last)
-            if (k == 0 && taken > 0) {
+            if (k == 0 && taken > 0 && !mbar_wait_all(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
+            tc_fence_after();
+            const uint64_t q = q0 + (uint64_t)(st * (MXT_STAGE >> 4)), x = x0 + (uint64_t)(st * (MXT_STAGE >> 4));
+            const bool run_starts = in_run == 0 && k > 0, hand_over = ++in_run == MXT_FLUSH || k + 1 == stages;
+            if (!run_starts) {
+                if (elect_one()) {
+#pragma unroll
+                    for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {   // the tile of Q stays in the collector for its three products
+                        tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, k > 0 || ks > 0 ? 1u : 0u);
+                        tc_mma_f16<3, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, 1u);
+                        tc_mma_f16<2, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, k > 0 || ks > 0 ? 1u : 0u);
+                    }
+                }
+            } else {   // mid and lo go ahead while the hi accumulator is still being read
+                if (elect_one()) {
+#pragma unroll
+                    for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {
+                        tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
+                        tc_mma_f16<2, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, 1u);
+                    }
+                }
+                __syncwarp();
                 if (!mbar_wait_all(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
                 tc_fence_after();
-            }
-            if (elect_one()) {
+                if (elect_one()) {
 #pragma unroll
-                for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks)
-#pragma unroll
-                    for (uint32_t t = 1; t < 3; ++t)
-                        tc_mma_f16<0, 1>(s.tmem + 256u, x + ks * x_step + t * plane, q + ks * q_step, idesc, k > 0 || ks > 0 || t > 1 ? 1u : 0u);
+                    for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) tc_mma_f16<0, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, ks > 0 ? 1u : 0u);
+                }
             }
             __syncwarp();
-            if (in_run == 0 && k > 0) {
-                if (!mbar_wait_all(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
-                tc_fence_after();
-            }
-            const bool hand_over = ++in_run == MXT_FLUSH || k + 1 == stages;
             if (elect_one()) {
-#pragma unroll
-                for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks)
-                    tc_mma_f16<0, 1>(s.tmem, x + ks * x_step, q + ks * q_step, idesc, in_run > 1 || ks > 0 ? 1u : 0u);
-                tc_commit<1>(&s.sh->op_empty[st]);
-                if (hand_over) tc_commit<1>(&s.sh->acc_full);
+                tc_commit<2>(&s.sh->op_empty[st]);
+                if (hand_over) tc_commit<2>(&s.sh->acc_full);
             }
             __syncwarp();
             if (hand_over) ++taken, in_run = 0;
-            if (++st == MXT_OP) st = 0, ph ^= 1u;
         }
     }
 }
 
-// TMA loads, up to MXT_RAW stages ahead of the workers; the column sums of X in doubles, four columns a lane
+// TMA loads and, a term per lane, asynchronous copies of the scales, up to MXT_RING stages ahead of the workers
 template <bool TN, int FMT>
-__device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, const CUtensorMap *map_x, const CUtensorMap *map_q, int32_t first, int32_t step, int lane)
+__device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, const CUtensorMap *map_x, const CUtensorMap *map_q, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    int32_t ahead = first;              // what is loaded next
-    int32_t ahead_k = 0;
-    MxtItem at{};
-    if (ahead < a.items) at = mxt_item(a, ahead);
-    uint32_t lst = 0, lph = 0;
-    auto load = [&]() -> bool {
-        if (ahead >= a.items) return true;
-        if (!mbar_wait_all(&s.sh->raw_empty[lst], lph ^ 1u, dead, a.status)) return false;
-        if (lane == 0) {
-            uint8_t *x = s.raw + (size_t)lst * MXT_RAW_STAGE, *q = x + MXT_X_RAW;
-            uint64_t *bar = &s.sh->raw_full[lst];
-            const int32_t k = at.k0 + ahead_k * MXT_KB;
-            const int32_t boxes = TN ? (a.M - at.m0 + 31) / 32 < 4 ? (a.M - at.m0 + 31) / 32 : 4 : 1;
-            mbar_expect_tx(bar, (TN ? (uint32_t)boxes * 4096u : (uint32_t)MXT_X_RAW) + (uint32_t)(a.bn * MXT_KB * FMT / 8));
-            if (TN)
-                for (int b = 0; b < boxes; ++b) tma_load_2d(x + b * 4096, map_x, bar, at.m0 + 32 * b, k);
-            else tma_load_2d(x, map_x, bar, k, at.m0);
-            tma_load_2d(q, map_q, bar, at.n0 * FMT / 8, k);
-        }
-        __syncwarp();
-        if (++lst == MXT_RAW) lst = 0, lph ^= 1u;
-        if (++ahead_k == at.stages) {
-            ahead_k = 0;
-            ahead += step;
-            if (ahead < a.items) at = mxt_item(a, ahead);
-        }
-        return true;
-    };
-    for (int i = 0; i < MXT_RAW - 1; ++i)
-        if (!load()) return;
-    uint32_t st = 0, ph = 0;
-    for (int32_t i = first; i < a.items; i += step) {
+    const int32_t half = a.bn / 2;
+    uint32_t g = 0;
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
-        const bool sums = TN && a.colsum && it.n0 == 0;
+        const int32_t x0 = it.n0 + s.rank * half, q0 = it.d0 + s.rank * 128;
+        const int32_t boxes = x0 >= a.N ? 0 : !TN ? 1 : min((a.N - x0 + 31) / 32, half / 32);
+        const bool has_q = q0 < a.D;
+        const uint32_t bytes = (uint32_t)boxes * (TN ? 4096u : (uint32_t)half * 128u) + (has_q ? 128u * MXT_KB * FMT / 8 : 0u);
+        const uint8_t *scales = a.scales + (int64_t)(it.k0 + lane) * a.ld_scales + q0 / MX_GROUP;   // four bytes, of which some may lie behind the row's last
+        for (int32_t k = it.k0; k < it.k1; k += MXT_KB, ++g, scales += MXT_KB * a.ld_scales) {
+            const uint32_t st = g % MXT_RING;
+            if (!mbar_wait_all(&s.sh->raw_empty[st], ((g / MXT_RING) & 1u) ^ 1u, dead, a.status)) return;
+            uint64_t *bar = &s.sh->raw_full[st];
+            if (lane == 0) {
+                uint8_t *x = s.raw + (size_t)st * MXT_RAW_STAGE;
+                mbar_expect_tx(bar, bytes);
+                if (TN)
+                    for (int b = 0; b < boxes; ++b) tma_load_2d(x + b * 4096, map_x, bar, x0 + 32 * b, k);
+                else if (boxes) tma_load_2d(x, map_x, bar, k, x0);
+                if (has_q) tma_load_2d(x + MXT_X_RAW, map_q, bar, q0 / 8 * FMT, k);
+            }
+            __syncwarp();
+            const bool there = has_q && k + lane < it.k1;   // (else four zero bytes and nothing read)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(s.sh->scales[st] + 4 * lane)), "l"(there ? scales : a.scales), "r"(there ? 4u : 0u) : "memory");
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    // the pair's MMAs have signalled every stage: nothing arrives here any more once both CTAs may exit
+    for (uint32_t st = 0; st < MXT_RING; ++st) {
+        const uint32_t uses = (g + MXT_RING - 1 - st) / MXT_RING;
+        if (uses > 0 && !mbar_wait_all(&s.sh->op_empty[st], (uses - 1) & 1u, dead, a.status)) return;
+    }
+}
+
+// The column sums of X (TN), four columns a lane: a stage in fp32, the stages in doubles
+__device__ __forceinline__ void mxt_sums(const MxtArgs &a, const MxtMem &s, int lane)
+{
+    volatile int *dead = &s.sh->dead;
+    const int32_t half = a.bn / 2, mine = (lane >> 3) * 32;
+    uint32_t g = 0;
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
+        const MxtItem it = mxt_item(a, i);
+        const int32_t x0 = it.n0 + s.rank * half;
+        const bool sums = it.d0 == 0, here = sums && mine < half && x0 + mine < a.N;
         double c[4] = {0., 0., 0., 0.};
-        for (int32_t k = 0; k < it.stages; ++k) {
-            if (!load()) return;
-            if (!TN) continue;
-            if (!mbar_wait_all(&s.sh->raw_full[st], ph, dead, a.status)) return;
-            if (sums && it.m0 + (lane >> 3) * 32 < a.M) {
+        for (int32_t k = 0; k < it.stages; ++k, ++g) {
+            const uint32_t st = g % MXT_RING;
+            if (!mbar_wait_all(&s.sh->raw_full[st], (g / MXT_RING) & 1u, dead, a.status)) return;
+            if (here) {
                 const uint8_t *x = s.raw + (size_t)st * MXT_RAW_STAGE + (lane >> 3) * 4096;
                 float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
@@ -282,197 +306,144 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
-            if (++st == MXT_RAW) st = 0, ph ^= 1u;
         }
-        if (sums)
+        if (here)
             for (int j = 0; j < 4; ++j) {
-                const int32_t col = it.m0 + 4 * lane + j;
-                if (col >= a.M) continue;
-                float *out = a.colsum + (int64_t)it.split * a.M + col;
-                *out = a.direct && a.accumulate ? (float)((double)*out + c[j]) : (float)c[j];
+                const int32_t col = x0 + 4 * lane + j;
+                if (4 * lane + j >= half || col >= a.N) continue;
+                float *out = a.colsum + (int64_t)it.split * a.N + col;
+                *out = a.add ? (float)((double)*out + c[j]) : (float)c[j];
             }
     }
 }
 
 template <bool TN, int FMT>
-__device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int32_t first, int32_t step, int warp, int lane)
+__device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    // Eight values of X and 16 elements of Q per thread and stage.  Terms of Q (and of X with TN): `term`; the places along a row go over the
-    // lanes so that eight lanes in turn touch all banks, in the raw rows as in the swizzled ones.
-    const int j = (lane >> 2) & 1, term = 2 * warp + (j ^ ((lane >> 3) & 1)), place = (lane & 3) | j << 2 | (lane >> 4) << 3;
-    const int row = TN ? 0 : 8 * warp + (lane >> 2), quad = lane & 3;     // (NN) row of X and which eight of its 32 terms
-    const uint32_t x_raw = TN ? (uint32_t)(place >> 2) * 4096u + (uint32_t)term * 128u : (uint32_t)row * 128u;
-    const uint32_t x_at = (uint32_t)((2 * (TN ? place & 3 : quad)) ^ ((TN ? term : row) & 7)) << 4;
-    const uint32_t x_op = TN ? (uint32_t)(place >> 3) * (MXT_KB * 128) + (uint32_t)term * 128u + (uint32_t)(((place & 7) ^ (term & 7)) << 4)
-                             : (uint32_t)row * 64u + (uint32_t)((quad ^ ((row >> 1) & 3)) << 4);
-    const uint32_t q_raw = MXT_X_RAW + (uint32_t)(term * a.bn + 16 * place) * FMT / 8;
-    const uint32_t q_op = 3 * MXT_X_PLANE + (uint32_t)(place >> 2) * (MXT_KB * 128) + (uint32_t)term * 128u;
-    const uint32_t q_at = (uint32_t)((2 * (place & 3)) ^ (term & 7)) << 4;
-    const bool has_q = 16 * place < a.bn;
-    const int chunks = a.bn / 32;
-
-    // scale bytes come two stages ahead: `left` more terms of the item ahead, the byte of its next stage at `next`
-    int32_t ahead = first, left = 0;
-    const uint8_t *next = a.scales;
-    bool in_range = false;
-    const int64_t stage_scales = a.ld_scales * MXT_KB;
-    auto scale = [&]() -> uint32_t {
-        if (left <= 0) {
-            if (ahead >= a.items) return 127u;
-            const MxtItem t = mxt_item(a, ahead);
-            const int32_t g = (t.n0 + 16 * place) / MX_GROUP;
-            in_range = has_q && g < a.groups;
-            next = a.scales + (int64_t)(t.k0 + term) * a.ld_scales + g;
-            left = t.k1 - t.k0;
-            ahead += step;
-        }
-        uint32_t byte = 127u;
-        if (in_range && term < left) byte = __ldg(next);
-        next += stage_scales;
-        left -= MXT_KB;
-        return byte;
-    };
-    uint32_t b0 = scale(), b1 = scale();
-    uint32_t rst = 0, rph = 0, ost = 0, oph = 0, taken = 0, turned = 0;
+    const uint32_t group = (uint32_t)warp >> 3;
+    const int w = warp & 7;
+    const int32_t half = a.bn / 2;
+    // 16 elements of Q and twice eight values of X per thread and stage.  Terms and places along a row go over the lanes so that eight
+    // lanes in turn touch all banks, in the raw rows as in the swizzled ones.
+    const int j = (lane >> 2) & 1, term = 4 * w + 2 * (lane >> 4) + (j ^ ((lane >> 3) & 1)), place = (lane & 3) | j << 2;
+    const uint32_t q_raw = MXT_X_RAW + (uint32_t)(term * 128 + 16 * place) * FMT / 8;
+    const uint32_t q_op = (uint32_t)(place >> 2) * (MXT_KB * 128) + (uint32_t)term * 128u + ((uint32_t)((2 * (place & 3)) ^ (term & 7)) << 4);
+    // TN: columns 8 place .. of the term, and 64 columns on.  NN: terms 8 (lane % 4) .. of a row, and of the row 64 on.
+    const int row = 8 * w + (lane >> 2), quad = lane & 3;
+    const uint32_t x_raw = TN ? (uint32_t)(place >> 2) * 4096u + (uint32_t)term * 128u + ((uint32_t)((2 * (place & 3)) ^ (term & 7)) << 4)
+                              : (uint32_t)row * 128u + ((uint32_t)((2 * quad) ^ (row & 7)) << 4);
+    const uint32_t x_op = MXT_Q_TILE + (TN ? (uint32_t)term * 128u + ((uint32_t)(place ^ (term & 7)) << 4) : (uint32_t)row * 64u + ((uint32_t)(quad ^ ((row >> 1) & 3)) << 4));
+    constexpr uint32_t x_raw2 = 8192u, x_op2 = 4096u;    // the second eight: two boxes, or 64 rows, further on
+    const int32_t x_first = TN ? 8 * place : row;        // its index within the CTA's half; the second is 64 further on
+    const int32_t chunks = a.bn / 32, slice = warp >> 2; // 32 columns of the accumulators each: chunks slice and slice + 4 are this warp's
     const uint32_t lanes = s.tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    for (int32_t i = first; i < a.items; i += step) {
-        const MxtItem it = mxt_item(a, i);
-        const bool has_x = !TN || it.m0 + 8 * place < a.M;
-        float acc[2][32];
+
+    float acc[2][32];
 #pragma unroll
-        for (int c = 0; c < 64; ++c) acc[c >> 5][c & 31] = 0.f;
-        auto take = [&](uint32_t base) {
+    for (int c = 0; c < 64; ++c) acc[c >> 5][c & 31] = 0.f;
+    uint32_t taken = 0;
+    auto take = [&](bool last) -> bool {
+        if (!mbar_wait_all(&s.sh->acc_full, taken & 1u, dead, a.status)) return false;
+        tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-                if ((warp >> 2) + 4 * c < chunks) {
+        for (int c = 0; c < 2; ++c)
+            if (slice + 4 * c < chunks) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t r[16];
-                        tc_ld16(lanes + base + (uint32_t)((warp >> 2) + 4 * c) * 32u + 16u * h, r);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t r[16];
+                    tc_ld16(lanes + (uint32_t)(slice + 4 * c) * 32u + 16u * h, r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[c][16 * h + e] += __uint_as_float(r[e]);
+                    if (last) {
+                        tc_ld16(lanes + 256u + (uint32_t)(slice + 4 * c) * 32u + 16u * h, r);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[c][16 * h + e] += __uint_as_float(r[e]);
                     }
                 }
-        };
-        auto hand_back = [&]() {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->acc_empty);
-            ++taken;
-        };
-        int32_t in_run = 0;
+            }
+        tc_fence_before();
+        mbar_arrive_warp<2>(&s.sh->acc_empty, lane);
+        ++taken;
+        return true;
+    };
+    // A lane has a column of Q, a register a column or row of X: consecutive lanes write consecutive floats
+    auto finish = [&](int32_t item) -> bool {
+        if (!take(true)) return false;
+        const MxtItem it = mxt_item(a, item);
+        const int32_t col = it.d0 + s.rank * 128 + (warp & 3) * 32 + lane;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int32_t first = it.n0 + (slice + 4 * c) * 32;
+            float *o = a.C + it.split * a.split + first * a.by_x + col * a.by_q;
+            if (slice + 4 * c < chunks && col < a.D)
+#pragma unroll
+                for (int e = 0; e < 32; ++e, o += a.by_x)
+                    if (first + e < a.N) *o = a.add ? *o + acc[c][e] : acc[c][e];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) acc[c][e] = 0.f;
+        }
+        return true;
+    };
+
+    uint32_t base = 0;      // stages before this item
+    int32_t pending = -1;   // the item that is to be finished
+    for (int32_t i = s.unit;; i += s.units) {
+        MxtItem it{};       // (no stages behind the last one)
+        if (i < a.items) it = mxt_item(a, i);
+        const bool has_q = it.d0 + s.rank * 128 + 16 * place < a.D;
+        const int32_t x0 = it.n0 + s.rank * half + x_first;
+        const bool has_x = x_first < half && x0 < a.N, has_x2 = x_first + 64 < half && x0 + 64 < a.N;
+        int32_t run_end = MXT_FLUSH;
 #pragma unroll 1
-        for (int32_t k = 0; k < it.stages; ++k) {
-            const uint32_t byte = b0;
-            b0 = b1;
-            b1 = scale();
-            if (!mbar_wait_all(&s.sh->raw_full[rst], rph, dead, a.status)) return;
-            const uint8_t *raw = s.raw + (size_t)rst * MXT_RAW_STAGE;
-            float4 xa = make_float4(0.f, 0.f, 0.f, 0.f), xb = xa;
-            if (has_x) {
-                xa = *reinterpret_cast<const float4 *>(raw + x_raw + x_at);
-                xb = *reinterpret_cast<const float4 *>(raw + x_raw + (x_at ^ 16u));
-            }
-            uint32_t c[4] = {0u, 0u, 0u, 0u};
-            if (has_q) {
-                if (FMT == SAT_MX8) {
-                    const uint4 t = *reinterpret_cast<const uint4 *>(raw + q_raw);
-                    c[0] = t.x, c[1] = t.y, c[2] = t.z, c[3] = t.w;
-                } else {
-                    const uint2 t = *reinterpret_cast<const uint2 *>(raw + q_raw);
-                    c[0] = t.x, c[1] = t.y;
-                }
-            }
-            uint4 h, m, l;
-            mxt_split8(xa, xb, h, m, l);
-            const MxtScale<FMT> sc(byte);
-            uint4 v0 = mxt_decode8<FMT>(c[0], c[1], sc), v1 = FMT == SAT_MX8 ? mxt_decode8<FMT>(c[2], c[3], sc) : mxt_decode8<FMT>(c[1], 0u, sc);
-            if (sc.two) v0 = bf16x8_mul(v0, sc.second), v1 = bf16x8_mul(v1, sc.second);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->raw_empty[rst]);
-            if (++rst == MXT_RAW) rst = 0, rph ^= 1u;
-            if (!mbar_wait_all(&s.sh->op_empty[ost], oph ^ 1u, dead, a.status)) return;
-            uint8_t *op = s.op + (size_t)ost * MXT_STAGE;
-            if (has_x) {
-                *reinterpret_cast<uint4 *>(op + x_op) = h;
-                *reinterpret_cast<uint4 *>(op + x_op + MXT_X_PLANE) = m;
-                *reinterpret_cast<uint4 *>(op + x_op + 2 * MXT_X_PLANE) = l;
-            }
-            if (has_q) {
-                *reinterpret_cast<uint4 *>(op + q_op + q_at) = v0;
-                *reinterpret_cast<uint4 *>(op + q_op + (q_at ^ 16u)) = v1;
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->op_full[ost]);
-            if (++ost == MXT_OP) ost = 0, oph ^= 1u;
-            // taken out one stage late, so that the MMAs have something to do meanwhile
-            if (in_run == MXT_FLUSH) {
-                if (!mbar_wait_all(&s.sh->acc_full, taken & 1u, dead, a.status)) return;
-                tc_fence_after();
-                take(0u);
-                hand_back();
-                in_run = 0;
-            }
-            ++in_run;
-        }
-        if (!mbar_wait_all(&s.sh->acc_full, taken & 1u, dead, a.status)) return;
-        tc_fence_after();
-        take(0u);
-        take(256u);
-        hand_back();
-        const int32_t q32 = (warp & 3) * 32;
-        if (TN) {
-            // a lane has a column of X, a register a column of Q: consecutive lanes write consecutive floats
-            const int32_t col = it.m0 + q32 + lane;
-            float *C = a.C + (int64_t)it.split * a.M * a.N;
-            if (col < a.M)
+        for (int32_t k = (int32_t)((group ^ base) & 1u);; k += 2) {
+            if (k < it.stages) {
+                const uint32_t g = base + (uint32_t)k, st = g % MXT_RING, ph = (g / MXT_RING) & 1u;
+                if (!mbar_wait_all(&s.sh->raw_full[st], ph, dead, a.status)) return;
+                if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
+                const uint8_t *raw = s.raw + (size_t)st * MXT_RAW_STAGE;
+                uint8_t *op = s.op + (size_t)st * MXT_STAGE;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int32_t r0 = it.n0 + ((warp >> 2) + 4 * c) * 32;
-                    if ((warp >> 2) + 4 * c < chunks)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (r0 + e < a.N) {
-                                float *o = C + (int64_t)(r0 + e) * a.M + col;
-                                *o = a.direct && a.accumulate ? *o + acc[c][e] : acc[c][e];
-                            }
-                }
-        } else {
-            // a lane has a row: blocks of 32 x 32 are turned around in the operand stages, which every MMA has left
-            float *tb = reinterpret_cast<float *>(s.op) + warp * (32 * 36);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int32_t col = it.n0 + ((warp >> 2) + 4 * c) * 32 + 4 * (lane & 7);
-                if ((warp >> 2) + 4 * c < chunks) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4 *>(tb + lane * 36 + e) = make_float4(acc[c][e], acc[c][e + 1], acc[c][e + 2], acc[c][e + 3]);
-                    __syncwarp();
-#pragma unroll
-                    for (int r = 0; r < 32; r += 4) {
-                        const int32_t row_out = it.m0 + q32 + r + (lane >> 3);
-                        const float4 v = *reinterpret_cast<const float4 *>(tb + (r + (lane >> 3)) * 36 + 4 * (lane & 7));
-                        if (row_out < a.M && col < a.N) {
-                            float *o = a.C + (int64_t)row_out * a.ldc + col;
-                            if (col + 4 <= a.N) {
-                                *reinterpret_cast<float4 *>(o) = v;
-                            } else {
-                                o[0] = v.x;
-                                if (col + 1 < a.N) o[1] = v.y;
-                                if (col + 2 < a.N) o[2] = v.z;
-                            }
-                        }
+                for (int h = 0; h < 2; ++h)
+                    if (h ? has_x2 : has_x) {
+                        uint4 hi, mid, lo;
+                        mxt_split8(*reinterpret_cast<const float4 *>(raw + x_raw + h * x_raw2), *reinterpret_cast<const float4 *>(raw + (x_raw ^ 16u) + h * x_raw2), hi, mid, lo);
+                        uint8_t *o = op + x_op + h * x_op2;
+                        *reinterpret_cast<uint4 *>(o) = hi;
+                        *reinterpret_cast<uint4 *>(o + MXT_X_PLANE) = mid;
+                        *reinterpret_cast<uint4 *>(o + 2 * MXT_X_PLANE) = lo;
                     }
-                    __syncwarp();
+                if (has_q) {
+                    const MxtScale<FMT> sc(s.sh->scales[st][4 * term + (place >> 1)]);
+                    uint4 v0, v1;
+                    if (FMT == SAT_MX8) {
+                        const uint4 c = *reinterpret_cast<const uint4 *>(raw + q_raw);
+                        v0 = mxt_decode8<FMT>(c.x, c.y, sc), v1 = mxt_decode8<FMT>(c.z, c.w, sc);
+                    } else {
+                        const uint2 c = *reinterpret_cast<const uint2 *>(raw + q_raw);
+                        v0 = mxt_decode8<FMT>(c.x, 0u, sc), v1 = mxt_decode8<FMT>(c.y, 0u, sc);
+                    }
+                    if (sc.two) v0 = bf16x8_mul(v0, sc.second), v1 = bf16x8_mul(v1, sc.second);
+                    *reinterpret_cast<uint4 *>(op + q_op) = v0;
+                    *reinterpret_cast<uint4 *>(op + (q_op ^ 16u)) = v1;
                 }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
+                mbar_arrive_warp<2>(&s.sh->op_full[st], lane);
             }
-            // every warp has before the first of them converts into the stages again
-            if (lane == 0) mbar_arrive(&s.sh->turned);
-            if (!mbar_wait_all(&s.sh->turned, turned & 1u, dead, a.status)) return;
-            ++turned;
+            // Accumulators are taken out a stage late, so that the MMAs have something to do meanwhile
+            if (pending >= 0) {
+                if (!finish(pending)) return;
+                pending = -1;
+            }
+            for (; run_end < it.stages && run_end <= k; run_end += MXT_FLUSH)
+                if (!take(false)) return;
+            if (k >= it.stages) break;
         }
+        if (i >= a.items) return;
+        base += (uint32_t)it.stages;
+        pending = i;
     }
 }
 
@@ -484,27 +455,28 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     MxtMem s;
     s.op = smem;
-    s.raw = smem + MXT_OP * MXT_STAGE;
-    s.sh = (MxtShared *)(s.raw + MXT_RAW * MXT_RAW_STAGE);
+    s.raw = smem + MXT_RING * MXT_STAGE;
+    s.sh = (MxtShared *)(s.raw + MXT_RING * MXT_RAW_STAGE);
+    s.rank = (int32_t)(blockIdx.x & 1u);
+    s.unit = (int32_t)(blockIdx.x >> 1);
+    s.units = (int32_t)(gridDim.x >> 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < MXT_RAW; ++i) {
-            mbar_init(&s.sh->raw_full[i], 1);
-            mbar_init(&s.sh->raw_empty[i], MXT_WORKERS + (TN ? 1 : 0));
-        }
-        for (int i = 0; i < MXT_OP; ++i) {
-            mbar_init(&s.sh->op_full[i], MXT_WORKERS);
+        for (int i = 0; i < MXT_RING; ++i) {
+            mbar_init(&s.sh->raw_full[i], 1 + 32);
+            mbar_init(&s.sh->raw_empty[i], MXT_WORKERS / 2 + (TN && a.colsum ? 1 : 0));
+            mbar_init(&s.sh->op_full[i], MXT_WORKERS);        // a group of either CTA
             mbar_init(&s.sh->op_empty[i], 1);
         }
         mbar_init(&s.sh->acc_full, 1);
-        mbar_init(&s.sh->acc_empty, MXT_WORKERS);
-        mbar_init(&s.sh->turned, MXT_WORKERS);
+        mbar_init(&s.sh->acc_empty, 2 * MXT_WORKERS);
         s.sh->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == MXT_WORKERS) tc_alloc<1>(&s.sh->tmem_base, 512u);
+    if (warp == MXT_WORKERS) tc_alloc<2>(&s.sh->tmem_base, 512u);
     tc_fence_before();
     __syncthreads();
+    cluster_sync();   // the other CTA's barriers are initialised and its TMEM is allocated
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
     sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
@@ -512,23 +484,57 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     // to 64: 4 x 104 + 64 = 5 x 96
     if (warp < MXT_WORKERS) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-        mxt_work<TN, FMT>(a, s, blockIdx.x, gridDim.x, warp, lane);
+        mxt_work<TN, FMT>(a, s, warp, lane);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == MXT_WORKERS) mxt_mma<TN>(a, s, blockIdx.x, gridDim.x);
-        else if (warp == MXT_WORKERS + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, blockIdx.x, gridDim.x, lane);
+        if (warp == MXT_WORKERS && s.rank == 0) mxt_mma<TN>(a, s);
+        else if (warp == MXT_WORKERS + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
+        else if (TN && warp == MXT_WORKERS + 2 && a.colsum) mxt_sums(a, s, lane);
     }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
+    cluster_sync();   // neither CTA's shared memory or TMEM is in use by the other any more
     if (warp == MXT_WORKERS) {
         tc_fence_after();
-        tc_dealloc<1>(s.tmem, 512u);
+        tc_dealloc<2>(s.tmem, 512u);
     }
 }
 
-static sat_status mxt_map_q(sat_ctx *ctx, CUtensorMap *map, const sat_mx_matrix *q, int32_t bn)
+// C[j][i] (+)= sum over the splits of part[z][i][j], cs[i] (+)= that of part_cs[z][i], in a fixed order: 32 columns of Q by eight of X per block,
+// four threads to an element
+__global__ void __launch_bounds__(1024)
+k_mx_reduce(const float *__restrict__ part, const float *__restrict__ part_cs, int32_t splits, int32_t D, int32_t N, int add, float *__restrict__ C, float *__restrict__ colsum)
 {
-    return sat_tensor_map(ctx, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q->codes, mx_row_bytes(q), q->rows, q->ld_codes, bn * q->format / 8, MXT_KB, CU_TENSOR_MAP_SWIZZLE_NONE);
+    sat_grid_wait();
+    __shared__ float red[4][8][33];
+    const int lane = threadIdx.x & 31, i = (threadIdx.x >> 5) & 7, z4 = threadIdx.x >> 8;
+    const int32_t col = (int32_t)blockIdx.x * 32 + lane, row = (int32_t)blockIdx.y * 8 + i;
+    const int64_t plane = (int64_t)D * N;
+    float t = 0.f;
+    if (col < D && row < N) {
+        const float *p = part + (int64_t)row * D + col;
+#pragma unroll 8
+        for (int32_t z = z4; z < splits; z += 4) t += __ldg(p + z * plane);
+    }
+    red[z4][i][lane] = t;
+    __syncthreads();
+    if (threadIdx.x < 256) {
+        const int jj = threadIdx.x >> 3, ii = threadIdx.x & 7;   // eight lanes write eight consecutive floats of a row of C
+        const int32_t c = (int32_t)blockIdx.x * 32 + jj, r = (int32_t)blockIdx.y * 8 + ii;
+        if (c < D && r < N) {
+            const float sum = (red[0][ii][jj] + red[1][ii][jj]) + (red[2][ii][jj] + red[3][ii][jj]);
+            float *o = C + (int64_t)c * N + r;
+            *o = add ? *o + sum : sum;
+        }
+    } else if (threadIdx.x < 264 && blockIdx.x == 0 && colsum) {
+        const int32_t r = (int32_t)blockIdx.y * 8 + (int32_t)threadIdx.x - 256;
+        if (r < N) {
+            double sum = 0.;
+            for (int32_t z = 0; z < splits; ++z) sum += (double)__ldg(part_cs + (int64_t)z * N + r);
+            colsum[r] = add ? (float)((double)colsum[r] + sum) : (float)sum;
+        }
+    }
 }
 
 template <bool TN, int FMT>
@@ -539,67 +545,79 @@ static sat_status mxt_launch(sat_ctx *ctx, const CUtensorMap &map_x, const CUten
         SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_gemm<TN, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MXT_SMEM));
         attr.mark(ctx->device);
     }
-    sat_pdl(ctx->stream, k_mx_gemm<TN, FMT>, (unsigned)std::min<int64_t>(a.items, ctx->sms), MXT_THREADS, MXT_SMEM)(map_x, map_q, a);
+    sat_pdl(ctx->stream, k_mx_gemm<TN, FMT>, 2u * (unsigned)std::min(a.items, ctx->sms / 2), MXT_THREADS, MXT_SMEM, 2)(map_x, map_q, a);
     SAT_LAUNCHED(ctx);
     return SAT_OK;
 }
 
+// what both have in common
+static sat_status mxt_args(sat_ctx *ctx, const sat_mx_matrix *q, int64_t n, int32_t bn, MxtArgs *a, CUtensorMap *map_q)
+{
+    a->scales = q->scales;
+    a->ld_scales = q->ld_scales;
+    a->groups = mx_groups(q->d);
+    a->D = q->d;
+    a->N = (int32_t)n;
+    a->K = a->kps = (int32_t)q->rows;
+    a->bn = bn;
+    a->tiles_d = (int32_t)cdiv64(q->d, 256);
+    a->tiles_n = (int32_t)cdiv64(n, bn);
+    if ((int64_t)a->tiles_d * a->tiles_n > INT32_MAX / 2) return sat_fail(ctx, SAT_EINVAL, "microscaled contraction: shape is too large");
+    a->items = a->tiles_d * a->tiles_n;
+    a->status = ctx->d_flag + 1;
+    return sat_tensor_map(ctx, map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, q->codes, mx_row_bytes(q), q->rows, q->ld_codes, 128 * q->format / 8, MXT_KB, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
 sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc)
 {
+    // 256 rows a tile, or fewer where that leaves pairs of SMs without one
+    int32_t bn = 256;
+    while (bn > 64 && cdiv64(W->d, 256) * cdiv64(m, bn) < ctx->sms / 2) bn /= 2;
     MxtArgs a{};
-    a.scales = W->scales;
-    a.ld_scales = W->ld_scales;
-    a.groups = mx_groups(W->d);
-    a.M = (int32_t)m;
-    a.N = W->d;
-    a.K = a.kps = (int32_t)W->rows;
-    a.bn = mx_tile_columns(a.N);
-    a.tiles_m = (int32_t)cdiv64(m, 128);
-    a.tiles_n = (int32_t)cdiv64(a.N, a.bn);
-    if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX / 2) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nn: shape is too large");
-    a.items = a.tiles_m * a.tiles_n;
-    a.C = C;
-    a.ldc = ldc;
-    a.status = ctx->d_flag + 1;
     CUtensorMap map_x, map_q;
-    SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, W->rows, m, (int64_t)lda * 4, MXT_KB, 128, CU_TENSOR_MAP_SWIZZLE_128B));
-    SAT_TRY(mxt_map_q(ctx, &map_q, W, a.bn));
+    SAT_TRY(mxt_args(ctx, W, m, bn, &a, &map_q));
+    a.C = C;
+    a.by_x = ldc;
+    a.by_q = 1;
+    SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, W->rows, m, (int64_t)lda * 4, MXT_KB, bn / 2, CU_TENSOR_MAP_SWIZZLE_128B));
     return W->format == SAT_MX8 ? mxt_launch<false, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<false, SAT_MX4>(ctx, map_x, map_q, a);
 }
 
 sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
 {
+    const int32_t tiles_n = (int32_t)cdiv64(n, 256), bn = (int32_t)cdiv64(cdiv64(n, tiles_n), 64) * 64;
     MxtArgs a{};
-    a.scales = A->scales;
-    a.ld_scales = A->ld_scales;
-    a.groups = mx_groups(A->d);
-    a.M = n;
-    a.N = A->d;
-    a.K = (int32_t)A->rows;
-    a.bn = mx_tile_columns(a.N);
-    a.tiles_m = (int32_t)cdiv64(n, 128);
-    a.tiles_n = (int32_t)cdiv64(a.N, a.bn);
-    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, stages = cdiv64(a.K, MXT_KB);
-    if (tiles > INT32_MAX / 2) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: shape is too large");
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(ctx->sms / tiles, cdiv64(stages, 4)));
-    a.kps = (int32_t)std::min<int64_t>(cdiv64(stages, splits) * MXT_KB, INT32_MAX & ~(MXT_KB - 1));
-    const int64_t n_splits = cdiv64(a.K, a.kps);
-    a.items = (int32_t)(tiles * n_splits);
-    a.direct = n_splits == 1;
-    a.accumulate = accumulate;
-    a.status = ctx->d_flag + 1;
-    if (a.direct) {
+    CUtensorMap map_x, map_q;
+    SAT_TRY(mxt_args(ctx, A, n, bn, &a, &map_q));
+    // Row splits: what takes the fewest stages in a row on the busiest pair, a split costing about six stages to set up and to add up
+    const int64_t units = ctx->sms / 2, tiles = a.items, stages = cdiv64(A->rows, MXT_KB);
+    int64_t best = 1, best_cost = INT64_MAX;
+    for (int64_t s = 1; s <= std::min<int64_t>(2 * units / tiles + 1, cdiv64(stages, 4)); ++s) {
+        const int64_t cost = cdiv64(tiles * s, units) * (cdiv64(stages, s) + 6);
+        if (cost < best_cost) best = s, best_cost = cost;
+    }
+    a.kps = (int32_t)std::min<int64_t>(cdiv64(stages, best) * MXT_KB, INT32_MAX & ~(MXT_KB - 1));
+    const int32_t splits = (int32_t)cdiv64(A->rows, a.kps);
+    a.items *= splits;
+    if (splits == 1) {
         a.C = C;
+        a.by_x = 1;
+        a.by_q = n;
+        a.add = accumulate;
         a.colsum = colsum;
     } else {
-        SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)n_splits * ((size_t)a.N * n + n) * sizeof(float)));
+        a.split = (int64_t)a.D * n;
+        SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)splits * (size_t)(a.split + n) * sizeof(float)));
         a.C = (float *)ctx->buf_splitk.p;
-        a.colsum = colsum ? a.C + (size_t)n_splits * a.N * n : nullptr;
+        a.by_x = a.D;
+        a.by_q = 1;
+        a.colsum = colsum ? a.C + splits * a.split : nullptr;
     }
-    CUtensorMap map_x, map_q;
     SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, B, n, A->rows, (int64_t)ldb * 4, 32, MXT_KB, CU_TENSOR_MAP_SWIZZLE_128B));
-    SAT_TRY(mxt_map_q(ctx, &map_q, A, a.bn));
     SAT_TRY((A->format == SAT_MX8 ? mxt_launch<true, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<true, SAT_MX4>(ctx, map_x, map_q, a)));
-    if (a.direct) return SAT_OK;
-    return sat_splitk_reduce(ctx, a.C, (int64_t)a.N * n, (int32_t)n_splits, accumulate, C, n, n, a.colsum, n, colsum);
+    if (splits == 1) return SAT_OK;
+    if (cdiv64(n, 8) > 65535) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: shape is too large");
+    sat_pdl(ctx->stream, k_mx_reduce, dim3((unsigned)cdiv64(a.D, 32), (unsigned)cdiv64(n, 8)), 1024, 0)(a.C, a.colsum, splits, a.D, n, accumulate, C, colsum);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
 }

@@ -145,17 +145,19 @@ __device__ __forceinline__ void tc_mma(uint32_t tmem_d, uint64_t adesc, uint64_t
         else TC_MMA_ASM("1", "tf32", "");
     }
 }
-// the same with half-precision operands
+// the same with 16-bit operands; USE_A = 3: it is taken from there and stays
 template <int USE_A, int GROUP>
 __device__ __forceinline__ void tc_mma_f16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
     if (GROUP == 2) {
         if (USE_A == 1) TC_MMA_ASM("2", "f16", ".collector::a::fill");
         else if (USE_A == 2) TC_MMA_ASM("2", "f16", ".collector::a::lastuse");
+        else if (USE_A == 3) TC_MMA_ASM("2", "f16", ".collector::a::use");
         else TC_MMA_ASM("2", "f16", "");
     } else {
         if (USE_A == 1) TC_MMA_ASM("1", "f16", ".collector::a::fill");
         else if (USE_A == 2) TC_MMA_ASM("1", "f16", ".collector::a::lastuse");
+        else if (USE_A == 3) TC_MMA_ASM("1", "f16", ".collector::a::use");
         else TC_MMA_ASM("1", "f16", "");
     }
 }
@@ -187,6 +189,38 @@ __device__ __forceinline__ uint64_t make_desc(uint32_t saddr, uint32_t lbo_bytes
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// A warp's arrival on a barrier that the MMA issuer waits for.  CTAS = 1: every lane arrives.  2: lane 0 does, on the barrier at the same
+// place in CTA 0 of the pair, without a scope, that is at CTA scope.  An assumption rests on that: that shared-memory writes in front of
+// the proxy fence and TMEM reads in front of their wait are done for the pair's MMAs when the arrival is seen.  The memory model does not
+// say so across two CTAs; it is the form in which CUTLASS's cluster barriers arrive at the other CTA of a pair, and
+// tests/test_gpu_edges.py compares pair launches with single CTAs bit by bit.  (With .release.cluster the arrival also waits for
+// everything else the SM has in flight, 1.4 us: a 179250 x 512 x 512 contraction took 490 us instead of 370; waits that acquire at
+// cluster scope, which would be half of it, cost 0.3-0.5 % of an epoch.)
+template <int CTAS>
+__device__ __forceinline__ void mbar_arrive_warp(uint64_t *bar, int lane)
+{
+    if (CTAS == 1) {
+        mbar_arrive(bar);
+        return;
+    }
+    __syncwarp();
+    if (lane == 0)
+        asm volatile(
+            "{\n\t"
+            ".reg .b32 a;\n\t"
+            "mapa.shared::cluster.u32 a, %0, 0;\n\t"
+            "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t"
+            "}" ::"r"(smem_u32(bar))
+            : "memory");
+}
+// lane 0's arrival on the same barriers with single CTAs too
+template <int CTAS>
+__device__ __forceinline__ void mbar_arrive_lane0(uint64_t *bar, int lane)
+{
+    __syncwarp();
+    if (CTAS == 2) mbar_arrive_warp<CTAS>(bar, lane);
+    else if (lane == 0) mbar_arrive(bar);
 }
 // make generic-proxy shared-memory writes visible to the tensor-core (async) proxy
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
