@@ -17,7 +17,7 @@
 // was 183 KB for as many products.
 //
 // 20 warps.  Warps 0..15 convert, in two groups on alternate stages, and hold the sums; warp 16 of the first CTA issues the MMAs; warp 17 the
-// loads; warp 18 adds up the columns of X where the bias gradient is asked for.
+// loads; warps 18 and 19 add up the columns of X where the bias gradient is asked for.
 #include "sat_mx.h"
 #include "sat_ptx.h"
 
@@ -26,7 +26,8 @@
 #define MXT_WORKERS 16
 #define MXT_THREADS ((MXT_WORKERS + 4) * 32)   /* five whole warpgroups, see k_mx_gemm */
 #define MXT_KB 32                    /* terms per stage */
-#define MXT_RING 4                   /* stages of raw and of converted tiles; a power of two */
+#define MXT_RAW 6                    /* stages of raw tiles; an even number, so that either group keeps to its own */
+#define MXT_OP 3                     /* stages of converted tiles */
 #define MXT_FLUSH 12                 /* stages between two reads of the hi accumulator */
 #define MXT_Q_TILE (128 * MXT_KB * 2)
 #define MXT_X_PLANE (128 * MXT_KB * 2)
@@ -37,14 +38,16 @@
 #define MXT_SCALES (MXT_KB * 4)       /* of a stage: four groups a term */
 
 struct MxtShared {
-    uint8_t scales[MXT_RING][MXT_SCALES];
-    uint64_t raw_full[MXT_RING], raw_empty[MXT_RING];   // TMA bytes and scales have landed; a group of workers (and the column sums) has read them
-    uint64_t op_full[MXT_RING], op_empty[MXT_RING];     // (first CTA) both CTAs' workers have written the tiles; the MMAs have read them
+    double sums[128];
+    uint64_t sums_full, sums_empty;
+    uint8_t scales[MXT_RAW][MXT_SCALES];
+    uint64_t raw_full[MXT_RAW], raw_empty[MXT_RAW];   // TMA bytes and scales have landed; a group of workers (and the column sums) has read them
+    uint64_t op_full[MXT_OP], op_empty[MXT_OP];     // (first CTA) both CTAs' workers have written the tiles; the MMAs have read them
     uint64_t acc_full, acc_empty;                       // the hi accumulator is to be taken out; (first CTA) both CTAs have
     uint32_t tmem_base;
     int dead;
 };
-#define MXT_SMEM (1024 + MXT_RING * (MXT_STAGE + MXT_RAW_STAGE) + (int)sizeof(MxtShared))
+#define MXT_SMEM (1024 + MXT_OP * MXT_STAGE + MXT_RAW * MXT_RAW_STAGE + (int)sizeof(MxtShared))
 static_assert(MXT_SMEM <= 227 * 1024, "shared memory");
 
 struct MxtArgs {
@@ -167,6 +170,30 @@ __device__ __forceinline__ uint32_t mxt_idesc(int32_t bn)
     return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | (TN ? 1u << 16 : 0u) | (uint32_t)(bn >> 3) << 17 | (256u >> 4) << 24;
 }
 
+// Waits like mbar_wait_all, but the hardware may put the warp aside for up to a microsecond a time: what waits here would take issue slots
+// from the warps that convert, which are bound by them
+__device__ __forceinline__ bool mxt_wait(uint64_t *bar, uint32_t parity, volatile int *dead, int *status)
+{
+    const uint32_t addr = smem_u32(bar);
+    for (uint32_t it = 0; it < TC_WAIT_LIMIT; ++it) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t"
+            ".reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t"
+            "}"
+            : "=r"(ok)
+            : "r"(addr), "r"(parity), "r"(1000u)
+            : "memory");
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if (__any_sync(0xffffffffu, *dead)) return false;
+    }
+    *dead = 1;
+    atomicOr(status, 1);
+    return false;
+}
+
 // ---- the roles --------------------------------------------------------------------------------------------------------------
 struct MxtMem {
     uint8_t *op, *raw;
@@ -186,15 +213,14 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
     const uint64_t q0 = make_desc(smem_u32(s.op), MXT_KB * 128, 1024, 2);
     const uint64_t x0 = TN ? make_desc(smem_u32(s.op) + MXT_Q_TILE, MXT_KB * 128, 1024, 2) : make_desc(smem_u32(s.op) + MXT_Q_TILE, 16, 512, 4);
     constexpr uint32_t x_step = (TN ? 2048 : 32) >> 4, q_step = 2048 >> 4, plane = MXT_X_PLANE >> 4;
-    uint32_t g = 0, taken = 0;   // stages so far; times the accumulators were handed over
+    uint32_t st = 0, ph = 0, taken = 0;   // taken: times the accumulators were handed over
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
         int32_t in_run = 0;               // stages since the hi accumulator was last handed over
-        for (int32_t k = 0; k < stages; ++k, ++g) {
-            const uint32_t st = g % MXT_RING;
-            if (!mbar_wait_all(&s.sh->op_full[st], (g / MXT_RING) & 1u, dead, a.status)) return;
+        for (int32_t k = 0; k < stages; ++k) {
+            if (!mxt_wait(&s.sh->op_full[st], ph, dead, a.status)) return;
             // (acc_empty's phase `taken - 1` completes when the workers have read what was handed over last)
-            if (k == 0 && taken > 0 && !mbar_wait_all(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
+            if (k == 0 && taken > 0 && !mxt_wait(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
             tc_fence_after();
             const uint64_t q = q0 + (uint64_t)(st * (MXT_STAGE >> 4)), x = x0 + (uint64_t)(st * (MXT_STAGE >> 4));
             const bool run_starts = in_run == 0 && k > 0, hand_over = ++in_run == MXT_FLUSH || k + 1 == stages;
@@ -216,7 +242,7 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
                     }
                 }
                 __syncwarp();
-                if (!mbar_wait_all(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
+                if (!mxt_wait(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
@@ -230,6 +256,7 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
             }
             __syncwarp();
             if (hand_over) ++taken, in_run = 0;
+            if (++st == MXT_OP) st = 0, ph ^= 1u;
         }
     }
 }
@@ -240,7 +267,7 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
 {
     volatile int *dead = &s.sh->dead;
     const int32_t half = a.bn / 2;
-    uint32_t g = 0;
+    uint32_t st = 0, ph = 0, total = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         const int32_t x0 = it.n0 + s.rank * half, q0 = it.d0 + s.rank * 128;
@@ -248,9 +275,8 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
         const bool has_q = q0 < a.D;
         const uint32_t bytes = (uint32_t)boxes * (TN ? 4096u : (uint32_t)half * 128u) + (has_q ? 128u * MXT_KB * FMT / 8 : 0u);
         const uint8_t *scales = a.scales + (int64_t)(it.k0 + lane) * a.ld_scales + q0 / MX_GROUP;   // four bytes, of which some may lie behind the row's last
-        for (int32_t k = it.k0; k < it.k1; k += MXT_KB, ++g, scales += MXT_KB * a.ld_scales) {
-            const uint32_t st = g % MXT_RING;
-            if (!mbar_wait_all(&s.sh->raw_empty[st], ((g / MXT_RING) & 1u) ^ 1u, dead, a.status)) return;
+        for (int32_t k = it.k0; k < it.k1; k += MXT_KB, ++total, scales += MXT_KB * a.ld_scales) {
+            if (!mxt_wait(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
             uint64_t *bar = &s.sh->raw_full[st];
             if (lane == 0) {
                 uint8_t *x = s.raw + (size_t)st * MXT_RAW_STAGE;
@@ -264,56 +290,69 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
             const bool there = has_q && k + lane < it.k1;   // (else four zero bytes and nothing read)
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(s.sh->scales[st] + 4 * lane)), "l"(there ? scales : a.scales), "r"(there ? 4u : 0u) : "memory");
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+            if (++st == MXT_RAW) st = 0, ph ^= 1u;
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     // the pair's MMAs have signalled every stage: nothing arrives here any more once both CTAs may exit
-    for (uint32_t st = 0; st < MXT_RING; ++st) {
-        const uint32_t uses = (g + MXT_RING - 1 - st) / MXT_RING;
-        if (uses > 0 && !mbar_wait_all(&s.sh->op_empty[st], (uses - 1) & 1u, dead, a.status)) return;
+    for (uint32_t i = 0; i < MXT_OP; ++i) {
+        const uint32_t uses = (total + MXT_OP - 1 - i) / MXT_OP;
+        if (uses > 0 && !mxt_wait(&s.sh->op_empty[i], (uses - 1) & 1u, dead, a.status)) return;
     }
 }
 
-// The column sums of X (TN), four columns a lane: a stage in fp32, the stages in doubles
-__device__ __forceinline__ void mxt_sums(const MxtArgs &a, const MxtMem &s, int lane)
+// The column sums of X (TN), four columns a lane: half a stage in fp32, the stages in doubles.  Two warps, with one half of every stage's terms each
+// (one alone took longer over a stage than everything else); the second one leaves its sums to the first.
+__device__ __forceinline__ void mxt_sums(const MxtArgs &a, const MxtMem &s, int part, int lane)
 {
     volatile int *dead = &s.sh->dead;
     const int32_t half = a.bn / 2, mine = (lane >> 3) * 32;
-    uint32_t g = 0;
+    uint32_t st = 0, ph = 0, turn = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         const int32_t x0 = it.n0 + s.rank * half;
         const bool sums = it.d0 == 0, here = sums && mine < half && x0 + mine < a.N;
         double c[4] = {0., 0., 0., 0.};
-        for (int32_t k = 0; k < it.stages; ++k, ++g) {
-            const uint32_t st = g % MXT_RING;
-            if (!mbar_wait_all(&s.sh->raw_full[st], (g / MXT_RING) & 1u, dead, a.status)) return;
+        for (int32_t k = 0; k < it.stages; ++k) {
+            if (!mxt_wait(&s.sh->raw_full[st], ph, dead, a.status)) return;
             if (here) {
-                const uint8_t *x = s.raw + (size_t)st * MXT_RAW_STAGE + (lane >> 3) * 4096;
-                float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-                for (int r = 0; r < MXT_KB; ++r) {
+                const uint8_t *x = s.raw + st * MXT_RAW_STAGE + (lane >> 3) * 4096 + part * (MXT_KB / 2 * 128);
+                float2 t = make_float2(0.f, 0.f), u = t;
+#pragma unroll
+                for (int r = 0; r < MXT_KB / 2; ++r) {
                     const float4 v = *reinterpret_cast<const float4 *>(x + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-                    t.x += v.x;
-                    t.y += v.y;
-                    t.z += v.z;
-                    t.w += v.w;
+                    t = __fadd2_rn(t, make_float2(v.x, v.y));
+                    u = __fadd2_rn(u, make_float2(v.z, v.w));
                 }
                 c[0] += t.x;
                 c[1] += t.y;
-                c[2] += t.z;
-                c[3] += t.w;
+                c[2] += u.x;
+                c[3] += u.y;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
+            if (++st == MXT_RAW) st = 0, ph ^= 1u;
         }
-        if (here)
+        if (!sums) continue;
+        double *slot = s.sh->sums + 4 * lane;
+        if (part == 1) {
+            if (!mxt_wait(&s.sh->sums_empty, (turn & 1u) ^ 1u, dead, a.status)) return;
+            for (int j = 0; j < 4; ++j) slot[j] = c[j];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->sums_full);
+        } else {
+            if (!mxt_wait(&s.sh->sums_full, turn & 1u, dead, a.status)) return;
             for (int j = 0; j < 4; ++j) {
                 const int32_t col = x0 + 4 * lane + j;
-                if (4 * lane + j >= half || col >= a.N) continue;
+                const double both = c[j] + slot[j];
+                if (!here || 4 * lane + j >= half || col >= a.N) continue;
                 float *out = a.colsum + (int64_t)it.split * a.N + col;
-                *out = a.add ? (float)((double)*out + c[j]) : (float)c[j];
+                *out = a.add ? (float)((double)*out + both) : (float)both;
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->sums_empty);
+        }
+        ++turn;
     }
 }
 
@@ -344,7 +383,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
     for (int c = 0; c < 64; ++c) acc[c >> 5][c & 31] = 0.f;
     uint32_t taken = 0;
     auto take = [&](bool last) -> bool {
-        if (!mbar_wait_all(&s.sh->acc_full, taken & 1u, dead, a.status)) return false;
+        if (!mxt_wait(&s.sh->acc_full, taken & 1u, dead, a.status)) return false;
         tc_fence_after();
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -376,17 +415,24 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         for (int c = 0; c < 2; ++c) {
             const int32_t first = it.n0 + (slice + 4 * c) * 32;
             float *o = a.C + it.split * a.split + first * a.by_x + col * a.by_q;
-            if (slice + 4 * c < chunks && col < a.D)
+            if (slice + 4 * c < chunks && col < a.D) {
+                if (first + 32 <= a.N && !(TN && a.add)) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e, o += a.by_x)
-                    if (first + e < a.N) *o = a.add ? *o + acc[c][e] : acc[c][e];
+                    for (int e = 0; e < 32; ++e, o += a.by_x) *o = acc[c][e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e, o += a.by_x)
+                        if (first + e < a.N) *o = TN && a.add ? *o + acc[c][e] : acc[c][e];
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 32; ++e) acc[c][e] = 0.f;
         }
         return true;
     };
 
-    uint32_t base = 0;      // stages before this item
+    uint32_t base = 0;      // parity of the stages before this item
+    uint32_t rs = group, rph = 0, os = group, oph = 0;
     int32_t pending = -1;   // the item that is to be finished
     for (int32_t i = s.unit;; i += s.units) {
         MxtItem it{};       // (no stages behind the last one)
@@ -396,13 +442,12 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         const bool has_x = x_first < half && x0 < a.N, has_x2 = x_first + 64 < half && x0 + 64 < a.N;
         int32_t run_end = MXT_FLUSH;
 #pragma unroll 1
-        for (int32_t k = (int32_t)((group ^ base) & 1u);; k += 2) {
+        for (int32_t k = (int32_t)(group ^ base);; k += 2) {
             if (k < it.stages) {
-                const uint32_t g = base + (uint32_t)k, st = g % MXT_RING, ph = (g / MXT_RING) & 1u;
-                if (!mbar_wait_all(&s.sh->raw_full[st], ph, dead, a.status)) return;
-                if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
-                const uint8_t *raw = s.raw + (size_t)st * MXT_RAW_STAGE;
-                uint8_t *op = s.op + (size_t)st * MXT_STAGE;
+                if (!mxt_wait(&s.sh->raw_full[rs], rph, dead, a.status)) return;
+                if (!mxt_wait(&s.sh->op_empty[os], oph ^ 1u, dead, a.status)) return;
+                const uint8_t *raw = s.raw + rs * MXT_RAW_STAGE;
+                uint8_t *op = s.op + os * MXT_STAGE;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     if (h ? has_x2 : has_x) {
@@ -414,7 +459,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
                         *reinterpret_cast<uint4 *>(o + 2 * MXT_X_PLANE) = lo;
                     }
                 if (has_q) {
-                    const MxtScale<FMT> sc(s.sh->scales[st][4 * term + (place >> 1)]);
+                    const MxtScale<FMT> sc(s.sh->scales[rs][4 * term + (place >> 1)]);
                     uint4 v0, v1;
                     if (FMT == SAT_MX8) {
                         const uint4 c = *reinterpret_cast<const uint4 *>(raw + q_raw);
@@ -429,8 +474,10 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
-                mbar_arrive_warp<2>(&s.sh->op_full[st], lane);
+                if (lane == 0) mbar_arrive(&s.sh->raw_empty[rs]);
+                mbar_arrive_warp<2>(&s.sh->op_full[os], lane);
+                if ((rs += 2) >= MXT_RAW) rs -= MXT_RAW, rph ^= 1u;
+                if ((os += 2) >= MXT_OP) os -= MXT_OP, oph ^= 1u;
             }
             // Accumulators are taken out a stage late, so that the MMAs have something to do meanwhile
             if (pending >= 0) {
@@ -442,7 +489,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
             if (k >= it.stages) break;
         }
         if (i >= a.items) return;
-        base += (uint32_t)it.stages;
+        base ^= (uint32_t)it.stages & 1u;
         pending = i;
     }
 }
@@ -455,20 +502,24 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     MxtMem s;
     s.op = smem;
-    s.raw = smem + MXT_RING * MXT_STAGE;
-    s.sh = (MxtShared *)(s.raw + MXT_RING * MXT_RAW_STAGE);
+    s.raw = smem + MXT_OP * MXT_STAGE;
+    s.sh = (MxtShared *)(s.raw + MXT_RAW * MXT_RAW_STAGE);
     s.rank = (int32_t)(blockIdx.x & 1u);
     s.unit = (int32_t)(blockIdx.x >> 1);
     s.units = (int32_t)(gridDim.x >> 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < MXT_RING; ++i) {
-            mbar_init(&s.sh->raw_full[i], 1 + 32);
-            mbar_init(&s.sh->raw_empty[i], MXT_WORKERS / 2 + (TN && a.colsum ? 1 : 0));
+        for (int i = 0; i < MXT_RAW; ++i) {
+            mbar_init(&s.sh->raw_full[i], 1 + 32);            // the TMA's issuer and the scales' lanes
+            mbar_init(&s.sh->raw_empty[i], MXT_WORKERS / 2 + (TN && a.colsum ? 2 : 0));
+        }
+        for (int i = 0; i < MXT_OP; ++i) {
             mbar_init(&s.sh->op_full[i], MXT_WORKERS);        // a group of either CTA
             mbar_init(&s.sh->op_empty[i], 1);
         }
         mbar_init(&s.sh->acc_full, 1);
+        mbar_init(&s.sh->sums_full, 1);
+        mbar_init(&s.sh->sums_empty, 1);
         mbar_init(&s.sh->acc_empty, 2 * MXT_WORKERS);
         s.sh->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -489,7 +540,7 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == MXT_WORKERS && s.rank == 0) mxt_mma<TN>(a, s);
         else if (warp == MXT_WORKERS + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
-        else if (TN && warp == MXT_WORKERS + 2 && a.colsum) mxt_sums(a, s, lane);
+        else if (TN && warp >= MXT_WORKERS + 2 && a.colsum) mxt_sums(a, s, warp - (MXT_WORKERS + 2), lane);
     }
     __syncwarp();
     tc_fence_before();
