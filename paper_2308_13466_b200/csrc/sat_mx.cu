@@ -4,6 +4,7 @@
 //   sat_mx_dense_nn   C = A W^              A fp32
 //   sat_mx_dense_tn   C (+)= A^^T B         B fp32, split over the rows
 #include "sat_mx.h"
+#include "sat_ptx.h"
 
 #include <algorithm>
 
@@ -105,12 +106,162 @@ k_mx_dequantise(MxView q, int64_t total, int32_t groups, int32_t d, float *__res
     }
 }
 
+// Matrices of some size: boxes of 128 rows by one group, a warpgroup to a box and a thread to a group, so that neither its maximum nor its scale is
+// worked out more than once (the kernels above take nine times the instructions for an element).  fp32 rows go between memory and 128-byte
+// rows of shared memory by TMA, three boxes per warpgroup in flight, and cross the banks swizzled.
+#define MXB_SLOTS 3
+#define MXB_BOX (128 * 32 * 4)
+#define MXB_SMEM (1024 + 4 * MXB_SLOTS * MXB_BOX)
+struct MxbShared {
+    uint64_t full[4][MXB_SLOTS];
+    int dead;
+};
+__device__ __forceinline__ void mxb_sync(int wg) { asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory"); }
+
+template <int FMT>
+__global__ void __launch_bounds__(512, 1)
+k_mx_quantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, int32_t groups, int64_t rows, int wide, MxView q, int *status)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    __shared__ MxbShared sh;
+    const int wg = threadIdx.x >> 7, t = threadIdx.x & 127;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 4 * MXB_SLOTS; ++i) mbar_init(&sh.full[i / MXB_SLOTS][i % MXB_SLOTS], 1);
+        sh.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    sat_grid_wait();
+    const int64_t step = (int64_t)gridDim.x * 4;
+    int64_t b = (int64_t)blockIdx.x * 4 + wg;
+    uint8_t *mine = smem + wg * MXB_SLOTS * MXB_BOX;
+    auto load = [&](int slot, int64_t box) {
+        if (t != 0 || box >= boxes) return;
+        const int64_t tile = sat_div(box, groups);
+        mbar_expect_tx(&sh.full[wg][slot], MXB_BOX);
+        tma_load_2d(mine + slot * MXB_BOX, &map_x, &sh.full[wg][slot], (int32_t)(box - tile * groups) * MX_GROUP, (int32_t)tile * 128);
+    };
+    for (int i = 0; i < MXB_SLOTS; ++i) load(i, b + i * step);
+    uint32_t slot = 0, ph = 0;
+    for (; b < boxes; b += step) {
+        (void)mbar_wait(&sh.full[wg][slot], ph, &sh.dead, status);   // (having given up, all finish on what is there)
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float4 *>(mine + slot * MXB_BOX + t * 128 + ((i ^ (t & 7)) << 4));
+        mxb_sync(wg);
+        load((int)slot, b + MXB_SLOTS * step);
+        if (++slot == MXB_SLOTS) slot = 0, ph ^= 1u;
+        uint32_t c[FMT];
+        const uint32_t byte = mx_quantise32<FMT>(v, c);
+        const int64_t tile = sat_div(b, groups), r = tile * 128 + t;
+        const int32_t g = (int32_t)(b - tile * groups);
+        if (r < rows) {
+            uint8_t *o = q.codes + r * q.ld_codes + g * (4 * FMT);
+            if (FMT == SAT_MX8 && wide) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(o), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(c[FMT - 4]), "r"(c[FMT - 3]),
+                             "r"(c[FMT - 2]), "r"(c[FMT - 1])
+                             : "memory");
+            } else {
+#pragma unroll
+                for (int i = 0; i < FMT; i += 4) *reinterpret_cast<uint4 *>(o + 4 * i) = make_uint4(c[i], c[i + 1], c[i + 2], c[i + 3]);
+            }
+            q.scales[r * q.ld_scales + g] = (uint8_t)byte;
+        }
+    }
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(512, 1)
+k_mx_dequantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, int32_t groups, int64_t rows, int32_t d, MxView q, float *__restrict__ x, int64_t ld)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const int wg = threadIdx.x >> 7, t = threadIdx.x & 127;
+    sat_grid_wait();
+    const int64_t step = (int64_t)gridDim.x * 4;
+    int64_t b = (int64_t)blockIdx.x * 4 + wg;
+    uint8_t *mine = smem + wg * MXB_SLOTS * MXB_BOX;
+    uint32_t next[FMT], next_byte = 0u;
+    auto fetch = [&](int64_t box) {
+        if (box >= boxes) return;
+        const int64_t tile = sat_div(box, groups), r = tile * 128 + t;
+        const int32_t g = (int32_t)(box - tile * groups);
+        if (r >= rows) return;
+        const uint8_t *o = q.codes + r * q.ld_codes + g * (4 * FMT);
+#pragma unroll
+        for (int i = 0; i < FMT; i += 4) {
+            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(o + 4 * i));
+            next[i] = w.x, next[i + 1] = w.y, next[i + 2] = w.z, next[i + 3] = w.w;
+        }
+        next_byte = __ldg(q.scales + r * q.ld_scales + g);
+    };
+#pragma unroll
+    for (int i = 0; i < FMT; ++i) next[i] = 0u;
+    fetch(b);
+    uint32_t slot = 0;
+    for (; b < boxes; b += step) {
+        uint32_t c[FMT];
+#pragma unroll
+        for (int i = 0; i < FMT; ++i) c[i] = next[i];
+        const float s = mx_power(next_byte);
+        fetch(b + step);
+        uint8_t *box = mine + slot * MXB_BOX;
+        if (t == 0) tma_store_wait_read<MXB_SLOTS - 1>();   // the box that was here has left
+        mxb_sync(wg);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t w = FMT == SAT_MX8 ? c[i % FMT] : c[(i / 2) % FMT] >> (16 * (i & 1));
+            const float2 lo = mx_unpack(mx_decode2<FMT>(w)), hi = mx_unpack(mx_decode2<FMT>(w >> (FMT == SAT_MX8 ? 16 : 8)));
+            *reinterpret_cast<float4 *>(box + t * 128 + ((i ^ (t & 7)) << 4)) = make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
+        }
+        const int64_t tile = sat_div(b, groups);
+        const int32_t col = (int32_t)(b - tile * groups) * MX_GROUP;
+        if (col + MX_GROUP > d && (d & 3)) {   // a bulk store writes the last 16 bytes of a row whole
+            mxb_sync(wg);
+            for (int i = t >> 5; i < 128; i += 4)
+                if (tile * 128 + i < rows && col + (t & 31) < d)
+                    x[(tile * 128 + i) * ld + col + (t & 31)] = *reinterpret_cast<const float *>(box + i * 128 + ((((t & 31) >> 2) ^ (i & 7)) << 4) + (t & 3) * 4);
+            mxb_sync(wg);
+            continue;
+        }
+        fence_async_smem();
+        mxb_sync(wg);
+        if (t == 0) tma_store_2d(&map_x, box, col, (int32_t)tile * 128);
+        if (++slot == MXB_SLOTS) slot = 0;
+    }
+    if (t == 0) tma_store_wait_all();
+}
+
+// From which size on boxes are used
+#define MXB_LEAST(ctx) (4 * (int64_t)(ctx)->sms)
+
+template <typename K, typename... A>
+static sat_status mx_launch_boxes(sat_ctx *ctx, PerDeviceOnce &attr, K kernel, int64_t boxes, const A &...args)
+{
+    if (attr.need(ctx->device)) {
+        SAT_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MXB_SMEM));
+        attr.mark(ctx->device);
+    }
+    sat_pdl(ctx->stream, kernel, (unsigned)std::min<int64_t>(cdiv64(boxes, 4), ctx->sms), 512, MXB_SMEM)(args...);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
 static sat_status mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q)
 {
     if (q->rows == 0) return SAT_OK;
     const int32_t groups = mx_groups(q->d);
-    const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8);
+    const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8), boxes = cdiv64(q->rows, 128) * groups;
     ProfScope prof(ctx, SATK_MX, (double)q->rows * (4.0 * q->d + mx_row_bytes(q) + groups), 0.0);
+    if (boxes >= MXB_LEAST(ctx)) {
+        static PerDeviceOnce attr8, attr4;
+        CUtensorMap map;
+        SAT_TRY(sat_tensor_map(ctx, &map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, x, q->d, q->rows, (int64_t)ld * 4, MX_GROUP, 128, CU_TENSOR_MAP_SWIZZLE_128B));
+        const int wide = !(((uintptr_t)q->codes | (uintptr_t)q->ld_codes) & 31);
+        if (q->format == SAT_MX8) return mx_launch_boxes(ctx, attr8, k_mx_quantise_boxes<SAT_MX8>, boxes, map, boxes, groups, q->rows, wide, mx_view(q), ctx->d_flag + 1);
+        return mx_launch_boxes(ctx, attr4, k_mx_quantise_boxes<SAT_MX4>, boxes, map, boxes, groups, q->rows, wide, mx_view(q), ctx->d_flag + 1);
+    }
     sat_pdl(ctx->stream, q->format == SAT_MX8 ? k_mx_quantise<SAT_MX8> : k_mx_quantise<SAT_MX4>, (unsigned)blocks, 256, 0)(x, ld, total, groups, q->d, mx_view(q));
     SAT_LAUNCHED(ctx);
     return SAT_OK;
@@ -131,8 +282,15 @@ extern "C" sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, fl
     if (!ok_ld(ld, q->d) || (q->rows > 0 && (!x || !aligned16(x)))) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dequantise: null / misaligned x or bad leading dimension");
     if (q->rows == 0) return SAT_OK;
     const int32_t groups = mx_groups(q->d);
-    const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8);
+    const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8), boxes = cdiv64(q->rows, 128) * groups;
     ProfScope prof(ctx, SATK_MX, (double)q->rows * (4.0 * q->d + mx_row_bytes(q) + groups), 0.0);
+    if (boxes >= MXB_LEAST(ctx)) {
+        static PerDeviceOnce attr8, attr4;
+        CUtensorMap map;
+        SAT_TRY(sat_tensor_map(ctx, &map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, x, q->d, q->rows, (int64_t)ld * 4, MX_GROUP, 128, CU_TENSOR_MAP_SWIZZLE_128B));
+        if (q->format == SAT_MX8) return mx_launch_boxes(ctx, attr8, k_mx_dequantise_boxes<SAT_MX8>, boxes, map, boxes, groups, q->rows, q->d, mx_view(q), x, (int64_t)ld);
+        return mx_launch_boxes(ctx, attr4, k_mx_dequantise_boxes<SAT_MX4>, boxes, map, boxes, groups, q->rows, q->d, mx_view(q), x, (int64_t)ld);
+    }
     sat_pdl(ctx->stream, q->format == SAT_MX8 ? k_mx_dequantise<SAT_MX8> : k_mx_dequantise<SAT_MX4>, (unsigned)blocks, 256, 0)(mx_view(q), total, groups, q->d, x, ld);
     SAT_LAUNCHED(ctx);
     return SAT_OK;

@@ -52,6 +52,23 @@ __device__ __forceinline__ uint32_t mx_encode4(float a, float b, float c, float 
             : "f"(a), "f"(b), "f"(c), "f"(d));
     return r;
 }
+// a group of 32 elements -> 32 or 16 bytes of codes; the scale byte
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_quantise32(const float4 (&v)[8], uint32_t (&code)[FMT])
+{
+    uint32_t top[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        top[i] = max(max(__float_as_uint(v[i].x) & 0x7FFFFFFFu, __float_as_uint(v[i].y) & 0x7FFFFFFFu), max(__float_as_uint(v[i].z) & 0x7FFFFFFFu, __float_as_uint(v[i].w) & 0x7FFFFFFFu));
+    const uint32_t byte = mx_scale_byte<FMT>(max(max(max(top[0], top[1]), max(top[2], top[3])), max(max(top[4], top[5]), max(top[6], top[7]))));
+    const float f = mx_inverse(byte);
+    uint32_t c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = byte == 255u ? 0u : mx_encode4<FMT>(v[i].x * f, v[i].y * f, v[i].z * f, v[i].w * f);
+#pragma unroll
+    for (int i = 0; i < FMT; ++i) code[i] = FMT == SAT_MX8 ? c[i] : (c[(2 * i) & 7] & 0xFFFFu) | c[(2 * i + 1) & 7] << 16;
+    return byte;
+}
 // two elements as a pair of halves, without the scale
 template <int FMT>
 __device__ __forceinline__ uint32_t mx_decode2(uint32_t code)

@@ -153,24 +153,6 @@ __device__ __forceinline__ void nt_load_w(const NtArgs &p, const NtMem &s, const
     }
 }
 
-// 32 elements -> 16 bytes of codes and the scale byte, as k_mx_quantise does
-__device__ __forceinline__ uint4 nt_quantise(const float4 (&v)[8], uint32_t &byte)
-{
-    uint32_t top[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        top[i] = max(max(__float_as_uint(v[i].x) & 0x7FFFFFFFu, __float_as_uint(v[i].y) & 0x7FFFFFFFu), max(__float_as_uint(v[i].z) & 0x7FFFFFFFu, __float_as_uint(v[i].w) & 0x7FFFFFFFu));
-    byte = mx_scale_byte<SAT_MX4>(max(max(max(top[0], top[1]), max(top[2], top[3])), max(max(top[4], top[5]), max(top[6], top[7]))));
-    if (byte == 255u) return make_uint4(0u, 0u, 0u, 0u);
-    const float f = mx_inverse(byte);
-    uint32_t c[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        c[i] = (mx_encode4<SAT_MX4>(v[2 * i].x * f, v[2 * i].y * f, v[2 * i].z * f, v[2 * i].w * f) & 0xFFFFu) |
-               mx_encode4<SAT_MX4>(v[2 * i + 1].x * f, v[2 * i + 1].y * f, v[2 * i + 1].z * f, v[2 * i + 1].w * f) << 16;
-    return make_uint4(c[0], c[1], c[2], c[3]);
-}
-
 template <bool STORED>
 __device__ __forceinline__ void nt_rows(const NtArgs &p, const NtMem &s, int warp, int lane)
 {
@@ -182,12 +164,13 @@ __device__ __forceinline__ void nt_rows(const NtArgs &p, const NtMem &s, int war
         const int64_t r = (int64_t)(t / p.tiles_n) * 128 + row;
         const bool keep = !STORED && p.a.codes && t % p.tiles_n == 0 && r < p.m;
         for (int32_t k = 0; k < p.stages; ++k) {
-            uint4 code = make_uint4(0u, 0u, 0u, 0u);
+            uint32_t c[4] = {0u, 0u, 0u, 0u};
             uint32_t byte = 127u;
             const int32_t group = 4 * k + g;
             if (STORED) {
                 if (r < p.m && group < p.groups) {
-                    code = __ldg(reinterpret_cast<const uint4 *>(p.a.codes + r * p.a.ld_codes) + group);
+                    const uint4 t = __ldg(reinterpret_cast<const uint4 *>(p.a.codes + r * p.a.ld_codes) + group);
+                    c[0] = t.x, c[1] = t.y, c[2] = t.z, c[3] = t.w;
                     byte = __ldg(p.a.scales + r * p.a.ld_scales + group);
                 }
             } else {
@@ -195,19 +178,19 @@ __device__ __forceinline__ void nt_rows(const NtArgs &p, const NtMem &s, int war
                 const uint8_t *x = s.raw + (g * NT_RAW + slot) * NT_BOX + row * 128;
                 float4 v[8];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] = *reinterpret_cast<const float4 *>(x + ((c ^ (row & 7)) << 4));
-                code = nt_quantise(v, byte);
+                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float4 *>(x + ((i ^ (row & 7)) << 4));
+                byte = mx_quantise32<SAT_MX4>(v, c);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s.sh->raw_empty[g][slot]);
                 if (++slot == NT_RAW) slot = 0, rph ^= 1u;
                 if (keep && group < p.groups) {
-                    *(reinterpret_cast<uint4 *>(p.a.codes + r * p.a.ld_codes) + group) = code;
+                    *(reinterpret_cast<uint4 *>(p.a.codes + r * p.a.ld_codes) + group) = make_uint4(c[0], c[1], c[2], c[3]);
                     p.a.scales[r * p.a.ld_scales + group] = (uint8_t)byte;
                 }
             }
             if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, p.status)) return;
             uint8_t *op = s.op + st * NT_STAGE;
-            *reinterpret_cast<uint4 *>(op + at) = code;
+            *reinterpret_cast<uint4 *>(op + at) = make_uint4(c[0], c[1], c[2], c[3]);
             op[sf_at] = (uint8_t)byte;
             fence_async_smem();
             __syncwarp();

@@ -92,7 +92,7 @@ def _untouched(view, d):
 
 # ---- quantisation ---------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("rows,d,extra", [(1, 1, 0), (3, 31, 4), (7, 32, 0), (5, 33, 8), (129, 100, 0), (1000, 256, 4), (64, 602, 0), (2049, 7, 0), (2, 4099, 0)])
+@pytest.mark.parametrize("rows,d,extra", [(1, 1, 0), (3, 31, 4), (7, 32, 0), (5, 33, 8), (129, 100, 0), (1000, 256, 4), (64, 602, 0), (2049, 7, 0), (2, 4099, 0), (9001, 257, 0), (8191, 290, 4), (76801, 30, 0), (9100, 256, 0)])
 def test_codes_and_scales_bit_by_bit(B, ctx, bits, rows, d, extra):
     import torch
     rng = np.random.default_rng(rows * 7 + d)
