@@ -466,6 +466,21 @@ def make_mx(codes, scales, d: int, fmt: int) -> sat_mx_matrix:
     return q
 
 
+# Plain values and pointers as ctypes converts them by itself: these calls serve single rows too, where marshalling is a good part of the time
+_lib.sat_mx_quantise.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+_lib.sat_mx_dequantise.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]
+_lib.sat_mx_dense_nt.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]
+_lib.sat_mx_dense_nn.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32]
+_lib.sat_mx_dense_tn.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int]
+
+
+def _rows(t):
+    """Pointer and row stride of a CUDA fp32 matrix with contiguous rows."""
+    (r, c), (s0, s1) = t.shape, t.stride()
+    assert t.is_cuda and (s1 == 1 or c <= 1)
+    return t.data_ptr(), s0 if r > 1 else max(s0, c)
+
+
 def new_mx(rows: int, d: int, fmt: int, device=None) -> sat_mx_matrix:
     """An uninitialised microscaled matrix on `device` (default: the current CUDA device)."""
     import torch
@@ -477,41 +492,43 @@ def new_mx(rows: int, d: int, fmt: int, device=None) -> sat_mx_matrix:
 
 def sat_mx_quantise(ctx, x, q: sat_mx_matrix):
     """q <- x (CUDA fp32 [rows, d])"""
-    assert tuple(x.shape) == (q.rows, q.d)
-    _check(ctx, _lib.sat_mx_quantise(ctx, _dev(x), C.c_int32(_ld(x)), C.byref(q)))
+    assert x.shape == (q.rows, q.d)
+    _check(ctx, _lib.sat_mx_quantise(ctx, *_rows(x), C.byref(q)))
 
 
 def sat_mx_dequantise(ctx, q: sat_mx_matrix, x):
     """x (CUDA fp32 [rows, d]) <- what q stands for"""
-    assert tuple(x.shape) == (q.rows, q.d)
-    _check(ctx, _lib.sat_mx_dequantise(ctx, C.byref(q), _dev(x), C.c_int32(_ld(x))))
+    assert x.shape == (q.rows, q.d)
+    _check(ctx, _lib.sat_mx_dequantise(ctx, C.byref(q), *_rows(x)))
 
 
 def sat_mx_dense_nt(ctx, A, W: sat_mx_matrix, bias, out, kept: sat_mx_matrix | None = None):
     """out[m, n] = A^[m, k] W^[n, k]^T + bias, both operands in 4 bits.  A: CUDA fp32, quantised on the way in (and kept in `kept`, if given), or a
     sat_mx_matrix."""
-    stored = isinstance(A, sat_mx_matrix)
-    assert not (stored and kept is not None)
-    m, k = (int(A.rows), int(A.d)) if stored else map(int, A.shape)
-    q = A if stored else kept
-    assert k == W.d and tuple(out.shape) == (m, W.rows) and (q is None or (q.rows, q.d) == (m, k))
-    assert bias is None or (bias.is_contiguous() and bias.numel() == W.rows)
-    _check(ctx, _lib.sat_mx_dense_nt(ctx, C.c_int64(m), None if stored else _dev(A), C.c_int32(0 if stored else _ld(A)), None if q is None else C.byref(q),
-                                     C.byref(W), _dev(bias), _dev(out), C.c_int32(_ld(out))))
+    if isinstance(A, sat_mx_matrix):
+        assert kept is None
+        m, k, a, lda, kept = A.rows, A.d, None, 0, A
+    else:
+        (m, k), (a, lda) = A.shape, _rows(A)
+        assert kept is None or (kept.rows, kept.d) == (m, k)
+    assert k == W.d and out.shape == (m, W.rows)
+    assert bias is None or (bias.is_cuda and bias.is_contiguous() and bias.numel() == W.rows)
+    _check(ctx, _lib.sat_mx_dense_nt(ctx, m, a, lda, None if kept is None else C.byref(kept), C.byref(W), None if bias is None else bias.data_ptr(), *_rows(out)))
 
 
 def sat_mx_dense_nn(ctx, A, W: sat_mx_matrix, out):
     """out[m, W.d] = A[m, W.rows] W^"""
-    assert A.shape[1] == W.rows and tuple(out.shape) == (A.shape[0], W.d)
-    _check(ctx, _lib.sat_mx_dense_nn(ctx, C.c_int64(A.shape[0]), _dev(A), C.c_int32(_ld(A)), C.byref(W), _dev(out), C.c_int32(_ld(out))))
+    m = A.shape[0]
+    assert A.shape[1] == W.rows and out.shape == (m, W.d)
+    _check(ctx, _lib.sat_mx_dense_nn(ctx, m, *_rows(A), C.byref(W), *_rows(out)))
 
 
 def sat_mx_dense_tn(ctx, A: sat_mx_matrix, Bm, out, colsum=None, accumulate: bool = False):
     """out[A.d, n] (+)= A^^T Bm[A.rows, n], colsum[n] (+)= column sums of Bm (out dense)"""
-    assert out.is_contiguous() and Bm.shape[0] == A.rows and tuple(out.shape) == (A.d, Bm.shape[1])
-    assert colsum is None or (colsum.is_contiguous() and colsum.numel() == Bm.shape[1])
-    _check(ctx, _lib.sat_mx_dense_tn(ctx, C.byref(A), C.c_int32(Bm.shape[1]), _dev(Bm), C.c_int32(_ld(Bm)), _dev(out), _dev(colsum),
-                                     C.c_int(1 if accumulate else 0)))
+    n = Bm.shape[1]
+    assert out.is_cuda and out.is_contiguous() and Bm.shape[0] == A.rows and out.shape == (A.d, n)
+    assert colsum is None or (colsum.is_cuda and colsum.is_contiguous() and colsum.numel() == n)
+    _check(ctx, _lib.sat_mx_dense_tn(ctx, C.byref(A), n, *_rows(Bm), out.data_ptr(), None if colsum is None else colsum.data_ptr(), 1 if accumulate else 0))
 
 
 def sat_dense_tn_static(stream: int, A, Bm, out):

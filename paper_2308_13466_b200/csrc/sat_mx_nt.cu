@@ -305,6 +305,121 @@ k_mx_nt(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUten
     }
 }
 
+// ---- a few rows ---------------------------------------------------------------------------------------------------------------
+// Up to NT_FEW rows of A: bound by the time to read W, if not by the launch.  Twice an element is a small integer, so a group's sum of products is
+// exact in integers (four bytes a dp4a).  Every block has all rows of A as bytes in shared memory; `lpr` lanes share a row of W, a group each in
+// turn.  One row, 512 x 512: 10.3 us with the tiles above.
+#define NT_FEW 16
+#define NT_FEW_WARPS 4
+#define NT_FEW_SMEM (96 * 1024)
+// Four codes (the low half of w) as bytes of twice their values
+__device__ __forceinline__ uint32_t nt_bytes(uint32_t w, uint32_t &negative)
+{
+    const uint32_t size = __byte_perm(0x03020100u, 0x0C080604u, w & 0x7777u);
+    uint32_t m;
+    asm("prmt.b32 %0, %1, %1, %2;" : "=r"(m) : "r"(0x80808080u), "r"(w));   // a selector's top bit spreads the byte's sign: FF or 80
+    negative = m & 0x01010101u;
+    return size ^ (negative * 255u);   // (one less than it should be where negative)
+}
+
+template <int MT>
+__global__ void __launch_bounds__(32 * NT_FEW_WARPS)
+k_mx_nt_few(const float *__restrict__ A, int64_t lda, int32_t m, int32_t n, int32_t k, int32_t groups, int32_t lpr, MxView a, MxView w, const float *__restrict__ bias,
+            float *__restrict__ C, int64_t ldc)
+{
+    extern __shared__ __align__(16) uint8_t few_smem[];
+    uint8_t *vals = few_smem;                                    // [m][groups][32] bytes
+    int16_t *exps = reinterpret_cast<int16_t *>(vals + m * groups * 32);   // [m][groups], 1000 for NaN
+    sat_grid_wait();
+    for (int32_t i = threadIdx.x >> 3; i < m * groups; i += 4 * NT_FEW_WARPS) {   // eight lanes to a group, four elements each
+        const int32_t r = i / groups, g = i - r * groups, sub = threadIdx.x & 7, c = g * MX_GROUP + 4 * sub;
+        const unsigned lanes = 0xFFu << (threadIdx.x & 24);
+        uint32_t code, byte;
+        if (A) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c < k) v = __ldg(reinterpret_cast<const float4 *>(A + r * lda + c));
+            if (c + 1 >= k) v.y = 0.f;
+            if (c + 2 >= k) v.z = 0.f;
+            if (c + 3 >= k) v.w = 0.f;
+            uint32_t top = max(max(__float_as_uint(v.x) & 0x7FFFFFFFu, __float_as_uint(v.y) & 0x7FFFFFFFu), max(__float_as_uint(v.z) & 0x7FFFFFFFu, __float_as_uint(v.w) & 0x7FFFFFFFu));
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
+            byte = mx_scale_byte<SAT_MX4>(top);
+            const float f = mx_inverse(byte);
+            code = byte == 255u ? 0u : mx_encode4<SAT_MX4>(v.x * f, v.y * f, v.z * f, v.w * f) & 0xFFFFu;
+            if (a.codes && blockIdx.x == 0) {
+                *reinterpret_cast<uint16_t *>(a.codes + r * a.ld_codes + c / 2) = (uint16_t)code;
+                if (sub == 0) a.scales[r * a.ld_scales + g] = (uint8_t)byte;
+            }
+        } else {
+            code = __ldg(reinterpret_cast<const uint16_t *>(a.codes + r * a.ld_codes + c / 2));
+            byte = __ldg(a.scales + r * a.ld_scales + g);
+        }
+        uint32_t neg;
+        const uint32_t b = nt_bytes(code, neg);
+        *reinterpret_cast<uint32_t *>(vals + i * 32 + 4 * sub) = __vadd4(b, neg);
+        if (sub == 0) exps[i] = byte == 255u ? 1000 : (int16_t)((int32_t)byte - 127);
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 31, sub = lane & (lpr - 1);
+    const int32_t rows = 32 / lpr, row = ((int32_t)blockIdx.x * NT_FEW_WARPS + (threadIdx.x >> 5)) * rows + lane / lpr;
+    const bool there = row < n;
+    float acc[MT];
+#pragma unroll
+    for (int r = 0; r < MT; ++r) acc[r] = 0.f;
+    if (there) {
+        for (int32_t g = sub; g < groups; g += lpr) {
+            const uint4 c = __ldg(reinterpret_cast<const uint4 *>(w.codes + row * w.ld_codes) + g);
+            const uint32_t byte = __ldg(w.scales + row * w.ld_scales + g), words[4] = {c.x, c.y, c.z, c.w};
+            uint32_t b[8], neg[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = nt_bytes(words[i / 2] >> (16 * (i & 1)), neg[i]);
+            const int32_t we = byte == 255u ? 2000 : (int32_t)byte - 129;   // -127, and a quarter for the doubled values
+#pragma unroll
+            for (int r = 0; r < MT; ++r) {
+                if (r >= m) break;
+                const uint4 x0 = *reinterpret_cast<const uint4 *>(vals + (r * groups + g) * 32), x1 = *reinterpret_cast<const uint4 *>(vals + (r * groups + g) * 32 + 16);
+                const uint32_t x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+                int32_t sum = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = __dp4a((int32_t)x[i], (int32_t)b[i], __dp4a((int32_t)x[i], (int32_t)neg[i], sum));
+                const int32_t e = we + exps[r * groups + g], half = e >> 1;   // in two steps: neither leaves the range before the product does
+                const float p = __int_as_float((half + 127) << 23), q = __int_as_float((e - half + 127) << 23);
+                acc[r] += e > 500 ? __int_as_float(0x7FFFFFFF) : (float)sum * p * q;
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+        if (r >= m) break;
+        for (int o = lpr >> 1; o > 0; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+        if (there && sub == 0) C[r * ldc + row] = acc[r] + (bias ? __ldg(bias + row) : 0.f);
+    }
+}
+
+// whether the bytes of A and their exponents fit
+static bool nt_few(int64_t m, int32_t groups) { return m <= NT_FEW && m * groups * 34 <= NT_FEW_SMEM; }
+
+static sat_status nt_launch_few(sat_ctx *ctx, int32_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias, float *C, int32_t ldc)
+{
+    const int32_t n = (int32_t)W->rows, k = W->d, groups = mx_groups(k);
+    int32_t lpr = 1;
+    while (lpr < groups && lpr < 32) lpr <<= 1;
+    const unsigned blocks = (unsigned)cdiv64(n, NT_FEW_WARPS * (32 / lpr));
+    const size_t smem = (size_t)m * groups * 34;
+    static PerDeviceOnce attr;
+    if (attr.need(ctx->device)) {
+        SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_nt_few<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NT_FEW_SMEM));
+        SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_nt_few<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, NT_FEW_SMEM));
+        SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_nt_few<NT_FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, NT_FEW_SMEM));
+        attr.mark(ctx->device);
+    }
+    sat_pdl(ctx->stream, m == 1 ? k_mx_nt_few<1> : m <= 4 ? k_mx_nt_few<4> : k_mx_nt_few<NT_FEW>, blocks, 32 * NT_FEW_WARPS, smem)(
+        A, (int64_t)lda, m, n, k, groups, lpr, Aq ? mx_view(Aq) : MxView{}, mx_view(W), bias, C, (int64_t)ldc);
+    SAT_LAUNCHED(ctx);
+    return SAT_OK;
+}
+
 template <bool STORED>
 static sat_status nt_launch(sat_ctx *ctx, const CUtensorMap &map_a, const CUtensorMap &map_w, const CUtensorMap &map_c, const NtArgs &p)
 {
@@ -320,6 +435,7 @@ static sat_status nt_launch(sat_ctx *ctx, const CUtensorMap &map_a, const CUtens
 
 sat_status sat_mx_tc_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias, float *C, int32_t ldc)
 {
+    if (nt_few(m, mx_groups(W->d))) return nt_launch_few(ctx, (int32_t)m, A, lda, Aq, W, bias, C, ldc);
     NtArgs p{};
     if (Aq) p.a = mx_view(Aq);
     p.w = mx_view(W);
