@@ -81,6 +81,12 @@ enum { SAT_ACT_NONE = 0, SAT_ACT_RELU = 1 };
  * there is no snapshot: then only the in-subgraph terms are summed).  With a snapshot the result is, bit for bit, that of
  * sat_predict without parameters followed by the plain call, without the [sum_m b_m x d_in] copy.  Not together with the two flags above (SAT_EINVAL). */
 #define SAT_FWD_HALO_CACHED 0x800
+/* ... and SAT_FWD_KEEP8: what is kept of AGG for the backward call is its image in 8 bits (sat_mx_quantise, SAT_MX8), a quarter of the
+ * memory.  h_out is the same; sat_layer_bwd then takes the weight gradient from the image (g_W = AGG^^T D, an unbiased few percent off
+ * per element of AGG), everything else of it is the same.  The kept form of a layer is that of its last forward call; a change of the
+ * flag drops what was kept for the other partitions.  Kept memory per layer: 33 to 36 bytes instead of 128 per 32 columns; one
+ * scratch of the largest call's AGG is shared by all layers. */
+#define SAT_FWD_KEEP8 0x1000
 enum { SAT_LOSS_SOFTMAX_CE = 0, SAT_LOSS_SIGMOID_BCE = 1 };
 enum { SAT_ROWS_INNER = 0, SAT_ROWS_HALO = 1 };          /* sat_gather_rows                      */
 enum { SAT_CACHE_ZERO = 0, SAT_CACHE_COPY = 1 };         /* sat_cache_init                       */
@@ -399,7 +405,7 @@ sat_status sat_sgd_steps(sat_ctx *ctx, int32_t n_arrays, const int64_t *counts, 
  *   flags     SAT_EPOCH_GRAD_HISTORY: SAT_BWD_GRAD_HISTORY on layers >= 2;  SAT_EPOCH_COMMIT: sat_cache_commit afterwards;
  *             SAT_EPOCH_STEP: w <- w - lr gw, b <- b - lr gb afterwards;  SAT_EPOCH_CONTINUE: this call goes on with an epoch that an
  *             earlier one began (partitions of `order` that are yet to run): its first partition too reuses the state table and adds to
- *             the gradients and to the loss
+ *             the gradients and to the loss;  SAT_EPOCH_KEEP8: SAT_FWD_KEEP8 in every layer
  * All arrays of pointers / sizes are HOST, the arrays they point to DEVICE.  *loss_sum is overwritten (unless continuing).
  * ------------------------------------------------------------------------------------- */
 typedef struct sat_epoch_buffers {
@@ -424,6 +430,7 @@ typedef struct sat_epoch_buffers {
 #define SAT_EPOCH_COMMIT 2
 #define SAT_EPOCH_STEP 4
 #define SAT_EPOCH_CONTINUE 8
+#define SAT_EPOCH_KEEP8 16
 sat_status sat_epoch(sat_ctx *ctx, const sat_epoch_buffers *buffers, const int32_t *order, int32_t n_order, int flags, float lr);
 
 /* ---------------------------------------------------------------------------------------
@@ -525,7 +532,7 @@ sat_status sat_cache_requantise(sat_ctx *ctx, int32_t layer, int32_t age, int32_
  *   codes    DEVICE, row r at byte r * ld_codes: one byte per element (SAT_MX8) or two elements a byte, the even one in the low half
  *            (SAT_MX4), the last group filled up with zeros.  16-byte aligned, ld_codes a multiple of 16 and >= 32 (16) bytes a group
  *   scales   DEVICE, row r at byte r * ld_scales: e + 127 per group.  4-byte aligned, ld_scales a multiple of 4 and >= the groups
- * Bytes between a row's end and the next row are neither read nor written.  The structure is HOST and not kept.
+ * Bytes between a row's end and the next row are not written and do not matter.  The structure is HOST and not kept.
  * ------------------------------------------------------------------------------------- */
 enum { SAT_MX8 = 8, SAT_MX4 = 4 };
 typedef struct sat_mx_matrix {

@@ -26,6 +26,7 @@ SAT_FWD_PUSH = 0x100
 SAT_FWD_HALO_GLOBAL = 0x200
 SAT_FWD_INPUT_GLOBAL = 0x400
 SAT_FWD_HALO_CACHED = 0x800
+SAT_FWD_KEEP8 = 0x1000
 SAT_ROWS_INNER, SAT_ROWS_HALO = 0, 1
 SAT_CACHE_ZERO, SAT_CACHE_COPY = 0, 1
 
@@ -51,7 +52,7 @@ class sat_mx_matrix(C.Structure):
 
 SAT_MX8, SAT_MX4 = 8, 4
 SAT_CELL_LSTM, SAT_CELL_GRU = 0, 1
-SAT_EPOCH_GRAD_HISTORY, SAT_EPOCH_COMMIT, SAT_EPOCH_STEP, SAT_EPOCH_CONTINUE = 1, 2, 4, 8
+SAT_EPOCH_GRAD_HISTORY, SAT_EPOCH_COMMIT, SAT_EPOCH_STEP, SAT_EPOCH_CONTINUE, SAT_EPOCH_KEEP8 = 1, 2, 4, 8, 16
 
 
 class sat_epoch_buffers(C.Structure):

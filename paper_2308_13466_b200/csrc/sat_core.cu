@@ -168,6 +168,7 @@ static void free_layers(sat_ctx *ctx)
 {
     for (int i = 0; i <= SAT_MAX_LAYERS; ++i) {
         dev_free(&ctx->layers[i].agg);
+        dev_free(&ctx->layers[i].kept.codes);
         dev_free(&ctx->layers[i].agg_max);
         dev_free(&ctx->layers[i].mask);
         sat_free_buf(ctx->layers[i].packed[0]);
@@ -209,6 +210,7 @@ extern "C" sat_status sat_destroy(sat_ctx *ctx)
     sat_free_buf(ctx->buf_pred_a);
     sat_free_buf(ctx->buf_misc);
     sat_free_buf(ctx->buf_mx);
+    sat_free_buf(ctx->buf_agg);
     sat_free_buf(ctx->buf_colsum);
     sat_free_buf(ctx->buf_dmask);
     sat_free_buf(ctx->buf_wsplit);

@@ -3,7 +3,7 @@
 // (marshalling of ~10 calls per partition took longer than the kernels of a graph of a few thousand nodes).
 #include "sat_internal.h"
 
-static sat_status epoch_pass(sat_ctx *ctx, const sat_epoch_buffers *e, int32_t part, bool first, int grad_history)
+static sat_status epoch_pass(sat_ctx *ctx, const sat_epoch_buffers *e, int32_t part, bool first, int grad_history, bool keep8)
 {
     const int accumulate = first ? 0 : SAT_BWD_ACCUMULATE, reuse_state = first ? 0 : 1;
     PartView v;
@@ -12,7 +12,7 @@ static sat_status epoch_pass(sat_ctx *ctx, const sat_epoch_buffers *e, int32_t p
     const float *h_in = e->x;
     int32_t ld_in = e->ld_x;
     for (int32_t l = 1; l <= L; ++l) {
-        int act = l < L ? SAT_ACT_RELU | SAT_FWD_PUSH : SAT_ACT_NONE;
+        int act = (l < L ? SAT_ACT_RELU | SAT_FWD_PUSH : SAT_ACT_NONE) | (keep8 ? SAT_FWD_KEEP8 : 0);
         const float *halo = nullptr;
         const sat_pred_params *p = l > 1 && e->pred ? e->pred[l - 2] : nullptr;
         if (l == 1) {
@@ -49,7 +49,7 @@ static sat_status epoch_pass(sat_ctx *ctx, const sat_epoch_buffers *e, int32_t p
 static sat_status epoch_check(sat_ctx *ctx, const sat_epoch_buffers *e, const int32_t *order, int32_t n_order, int flags)
 {
     if (!e || e->n_layers < 1 || e->n_layers > SAT_MAX_LAYERS || !e->dims || !e->x || !e->labels || !e->h || !e->ld_h || !e->g || !e->ld_g || !e->w || !e->b ||
-        !e->gw || !e->gb || (n_order != 0 && !order) || n_order < 0 || (flags & ~(SAT_EPOCH_GRAD_HISTORY | SAT_EPOCH_COMMIT | SAT_EPOCH_STEP | SAT_EPOCH_CONTINUE)))
+        !e->gw || !e->gb || (n_order != 0 && !order) || n_order < 0 || (flags & ~(SAT_EPOCH_GRAD_HISTORY | SAT_EPOCH_COMMIT | SAT_EPOCH_STEP | SAT_EPOCH_CONTINUE | SAT_EPOCH_KEEP8)))
         return sat_fail(ctx, SAT_EINVAL, "sat_epoch: incomplete description or unknown flags");
     PartView v;
     for (int32_t i = 0; i < (n_order > 0 ? n_order : 1); ++i) SAT_TRY(sat_part_view(ctx, n_order > 0 ? order[i] : (int32_t)SAT_ALL_PARTS, &v));
@@ -85,7 +85,7 @@ extern "C" sat_status sat_epoch(sat_ctx *ctx, const sat_epoch_buffers *e, const 
     ctx->keep_packed = order && n_order > 1;   // the parameter step comes after the passes
     sat_status st = SAT_OK;
     for (int32_t i = 0; i < (order ? n_order : 1) && st == SAT_OK; ++i)
-        st = epoch_pass(ctx, e, order ? order[i] : (int32_t)SAT_ALL_PARTS, i == 0 && begin, flags & SAT_EPOCH_GRAD_HISTORY);
+        st = epoch_pass(ctx, e, order ? order[i] : (int32_t)SAT_ALL_PARTS, i == 0 && begin, flags & SAT_EPOCH_GRAD_HISTORY, (flags & SAT_EPOCH_KEEP8) != 0);
     ctx->keep_packed = false;
     SAT_TRY(st);
     if (order && n_order == 0 && begin && e->loss_sum) SAT_CUDA(ctx, cudaMemsetAsync(e->loss_sum, 0, sizeof(double), ctx->stream));   // the loss of no partition

@@ -64,7 +64,8 @@ struct DevBuf {
 };
 
 struct LayerState {
-    float *agg = nullptr;      // [N x ld_in]  saved aggregation (rows in partition-major order)
+    float *agg = nullptr;      // [N x ld_in]  saved aggregation (rows in partition-major order), or with SAT_FWD_KEEP8 in its place
+    sat_mx_matrix kept = {};   // the same in 8 bits (scales in the allocation of the codes)
     uint32_t *agg_max = nullptr;   // [sat_spmm_parts(d_in) x N] largest magnitude of its rows, where the transform takes half-precision pairs
     uint32_t *mask = nullptr;  // [N x mask_words] bit j of word w: Z[row][32w + j] > 0
     int32_t d_in = 0, d_out = 0, ld_in = 0, mask_words = 0;
@@ -224,7 +225,7 @@ struct sat_ctx {
     // ---- scratch ----
     DevBuf buf_codec_sizes, buf_codec_off, buf_codec_bytes;  // embedding codec scratch
     DevBuf buf_ticket, buf_partial, buf_gagg, buf_splitk, buf_lstm_c, buf_lstm_s, buf_lstm_w, buf_pred_a, buf_misc, buf_colsum, buf_dmask,
-        buf_wsplit, buf_wsplit2, buf_wsplit3, buf_bias, buf_pred_train, buf_ghist_halo, buf_ghist_rows, buf_ghist_out, buf_gat, buf_gat_items, buf_q_max, buf_mx;
+        buf_wsplit, buf_wsplit2, buf_wsplit3, buf_bias, buf_pred_train, buf_ghist_halo, buf_ghist_rows, buf_ghist_out, buf_gat, buf_gat_items, buf_q_max, buf_mx, buf_agg;
 };
 
 sat_status sat_fail(sat_ctx *ctx, sat_status code, const char *fmt, ...);
@@ -345,6 +346,15 @@ struct RowMaxOut {
     uint32_t *p = nullptr;
     int64_t stride = 0;
 };
+// microscaled matrices (sat_mx.cu): as the entry points of these names, arguments checked
+sat_status sat_mx_quantise_rows(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q);
+sat_status sat_mx_gradient(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate);
+// rows [row0, row0 + rows) of a matrix
+inline sat_mx_matrix sat_mx_rows(const sat_mx_matrix &q, int64_t row0, int64_t rows)
+{
+    return sat_mx_matrix{q.codes + row0 * q.ld_codes, q.scales + row0 * q.ld_scales, rows, q.d, q.ld_codes, q.ld_scales, q.format};
+}
+
 // SpMM family (sat_spmm.cu)
 inline int32_t sat_spmm_parts(int32_t d) { return (d + 255) / 256; }
 enum class SpmmHalo { by_position, by_gid, by_slot };

@@ -21,6 +21,16 @@ static sat_status dev_realloc(sat_ctx *ctx, T **p, int64_t count)
     return SAT_OK;
 }
 
+template <typename T>
+static sat_status dev_drop(sat_ctx *ctx, T **p)
+{
+    if (!*p) return SAT_OK;
+    SAT_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
+    cudaFree(*p);
+    *p = nullptr;
+    return SAT_OK;
+}
+
 // =====================================================================================
 // sat_gather_rows
 // =====================================================================================
@@ -741,7 +751,8 @@ extern "C" sat_status sat_layer_fwd(sat_ctx *ctx, int32_t part, int32_t layer, i
     const bool in_global = (act & SAT_FWD_INPUT_GLOBAL) != 0;
     const bool halo_global = in_global || (act & SAT_FWD_HALO_GLOBAL) != 0;
     const bool halo_cached = (act & SAT_FWD_HALO_CACHED) != 0;
-    act &= ~(SAT_FWD_PUSH | SAT_FWD_HALO_GLOBAL | SAT_FWD_INPUT_GLOBAL | SAT_FWD_HALO_CACHED);
+    const bool keep8 = (act & SAT_FWD_KEEP8) != 0;
+    act &= ~(SAT_FWD_KEEP8 | SAT_FWD_PUSH | SAT_FWD_HALO_GLOBAL | SAT_FWD_INPUT_GLOBAL | SAT_FWD_HALO_CACHED);
     if (halo_cached && halo_global) return sat_fail(ctx, SAT_EINVAL, "sat_layer_fwd: SAT_FWD_HALO_CACHED excludes the global-matrix flags");
     CacheLayer *hc = nullptr;
     if (halo_cached) {
@@ -767,8 +778,17 @@ extern "C" sat_status sat_layer_fwd(sat_ctx *ctx, int32_t part, int32_t layer, i
     const bool half = layer > 1 && sat_tc_half(ctx, d_in) && sat_use_tc(d_out, d_in) && (d_in >= 384 || d_out <= 128);
     LayerState &L = ctx->layers[layer];
     const int32_t ld_agg = round_up4(d_in), words = (d_out + 31) / 32;
-    if (!L.agg || L.d_in != d_in || L.d_out != d_out) {
-        SAT_TRY(dev_realloc(ctx, &L.agg, (int64_t)ctx->n * ld_agg));
+    if (!(keep8 ? (void *)L.kept.codes : L.agg) || L.d_in != d_in || L.d_out != d_out) {
+        const int32_t groups = (d_in + 31) / 32, ld_s = round_up4(groups);
+        L.valid.assign(ctx->M, 0);
+        if (keep8) {
+            SAT_TRY(dev_drop(ctx, &L.agg));
+            SAT_TRY(dev_realloc(ctx, &L.kept.codes, (int64_t)ctx->n * (32 * groups + ld_s)));
+            L.kept = sat_mx_matrix{L.kept.codes, L.kept.codes + (int64_t)ctx->n * 32 * groups, ctx->n, d_in, 32 * groups, ld_s, SAT_MX8};
+        } else {
+            SAT_TRY(dev_drop(ctx, &L.kept.codes));
+            SAT_TRY(dev_realloc(ctx, &L.agg, (int64_t)ctx->n * ld_agg));
+        }
         SAT_TRY(dev_realloc(ctx, &L.agg_max, half ? (int64_t)ctx->n * sat_spmm_parts(d_in) : 0));
         SAT_TRY(dev_realloc(ctx, &L.mask, (int64_t)ctx->n * words));
         L.d_in = d_in;
@@ -790,10 +810,16 @@ extern "C" sat_status sat_layer_fwd(sat_ctx *ctx, int32_t part, int32_t layer, i
         ld_halo = hc->ld;
     }
     // (no snapshot yet: the halo terms are zero, the inner entries of the rows are all there is)
-    SAT_TRY(sat_spmm(ctx, v, halo_cached && !halo_base ? 1 : 0, d_in, in_base, ld_in, halo_base, ld_halo, L.agg, ld_agg, nullptr, 0, halo_kind, in_global,
+    if (keep8) SAT_TRY(sat_ensure(ctx, ctx->buf_agg, (size_t)v.n_rows * ld_agg * sizeof(float)));   // the rows themselves are needed until the transform only
+    float *agg_rows = keep8 ? (float *)ctx->buf_agg.p : L.agg + (int64_t)v.row0 * ld_agg;
+    SAT_TRY(sat_spmm(ctx, v, halo_cached && !halo_base ? 1 : 0, d_in, in_base, ld_in, halo_base, ld_halo, agg_rows - (int64_t)v.row0 * ld_agg, ld_agg, nullptr, 0, halo_kind, in_global,
                      SpmmAdd(), half ? RowMaxOut{L.agg_max, ctx->n} : RowMaxOut()));
+    if (keep8) {
+        const sat_mx_matrix q = sat_mx_rows(L.kept, v.row0, v.n_rows);
+        SAT_TRY(sat_mx_quantise_rows(ctx, agg_rows, ld_agg, &q));
+    }
     uint32_t *mask_out = act == SAT_ACT_RELU ? L.mask + (int64_t)v.row0 * words : nullptr;
-    const float *agg = L.agg + (int64_t)v.row0 * ld_agg;
+    const float *agg = agg_rows;
     if (sat_use_tc(d_out, d_in)) {
         TcWeights Wp(half);
         SAT_TRY(layer_weights(ctx, L, W, d_out, d_in, d_out, 1, bias, &Wp));
@@ -839,7 +865,8 @@ extern "C" sat_status sat_layer_bwd(sat_ctx *ctx, int32_t part, int32_t layer, c
     SAT_TRY(sat_part_view(ctx, part, &v));
     if (layer < 1 || layer > SAT_MAX_LAYERS) return sat_fail(ctx, SAT_EINVAL, "sat_layer_bwd: layer must be in [1, %d]", SAT_MAX_LAYERS);
     LayerState &L = ctx->layers[layer];
-    if (!L.agg) return sat_fail(ctx, SAT_ESTATE, "sat_layer_bwd: sat_layer_fwd has not run for layer %d", layer);
+    const bool keep8 = L.kept.codes != nullptr;
+    if (!L.agg && !keep8) return sat_fail(ctx, SAT_ESTATE, "sat_layer_bwd: sat_layer_fwd has not run for layer %d", layer);
     for (int m = (part == SAT_ALL_PARTS ? 0 : part); m < (part == SAT_ALL_PARTS ? ctx->M : part + 1); ++m)
         if (!L.valid[m]) return sat_fail(ctx, SAT_ESTATE, "sat_layer_bwd: sat_layer_fwd has not run for partition %d of layer %d", m, layer);
     const int32_t d_in = L.d_in, d_out = L.d_out;
@@ -858,14 +885,14 @@ extern "C" sat_status sat_layer_bwd(sat_ctx *ctx, int32_t part, int32_t layer, c
     int32_t mask_in_words = 0;
     if ((flags & SAT_BWD_MASK_G_IN) && layer > 1) {
         LayerState &Lp = ctx->layers[layer - 1];
-        bool ok = Lp.agg && Lp.act == SAT_ACT_RELU && Lp.mask && Lp.d_out == L.d_in;
+        bool ok = (Lp.agg || Lp.kept.codes) && Lp.act == SAT_ACT_RELU && Lp.mask && Lp.d_out == L.d_in;
         for (int m = (part == SAT_ALL_PARTS ? 0 : part); ok && m < (part == SAT_ALL_PARTS ? ctx->M : part + 1); ++m) ok = Lp.valid[m];
         if (ok) {
             mask_in = Lp.mask;
             mask_in_words = Lp.mask_words;
         }
     }
-    const float *agg = L.agg + (int64_t)v.row0 * L.ld_in;
+    const float *agg = keep8 ? nullptr : L.agg + (int64_t)v.row0 * L.ld_in;
     const bool want_dx = (g_in || g_halo) && v.n_rows > 0;
     const bool tc_w = sat_use_tc(d_out, d_in) && v.n_rows >= 256;   // weight gradient on the tensor cores
     // input gradient on the tensor cores, except when the halo gradient is wanted: that output sums thousands of signed
@@ -873,7 +900,7 @@ extern "C" sat_status sat_layer_bwd(sat_ctx *ctx, int32_t part, int32_t layer, c
     const bool tc_x = want_dx && !g_halo && sat_use_tc(d_in, d_out);
     const float *D = g_out;  // D = g_out o [Z > 0]: materialised once for the tensor-core contractions
     int32_t ld_d = ld_g;
-    if (mask && (tc_w || tc_x || hist)) {
+    if (mask && (tc_w || tc_x || hist || keep8)) {
         ld_d = round_up4(d_out);
         SAT_TRY(sat_ensure(ctx, ctx->buf_dmask, (size_t)v.n_rows * ld_d * sizeof(float)));
         D = (float *)ctx->buf_dmask.p;
@@ -882,7 +909,10 @@ extern "C" sat_status sat_layer_bwd(sat_ctx *ctx, int32_t part, int32_t layer, c
     // G_W (+)= AGG^T D, G_b (+)= 1^T D.  Down to one column, the register tiles of the narrow kernel are the faster ones where nothing has to be masked on
     // the way (epochs of 2,048 nodes with 4 classes 84.3 -> 80.1 us, of 6,000 with 7 254.8 -> 248.2)
     const bool narrow = d_out <= 64 && v.n_rows >= 256 && sat_use_tc(16, d_in) && (!mask || D != g_out) && !(ld_d & 3) && aligned16(D);
-    if (narrow) SAT_TRY(sat_gemm_tn_narrow(ctx, v.n_rows, d_in, d_out, agg, L.ld_in, D, ld_d, g_W, d_out, accumulate, g_b));
+    if (keep8) {
+        const sat_mx_matrix q = sat_mx_rows(L.kept, v.row0, v.n_rows);
+        SAT_TRY(sat_mx_gradient(ctx, &q, d_out, D, ld_d, g_W, g_b, accumulate));
+    } else if (narrow) SAT_TRY(sat_gemm_tn_narrow(ctx, v.n_rows, d_in, d_out, agg, L.ld_in, D, ld_d, g_W, d_out, accumulate, g_b));
     else if (tc_w) SAT_TRY(sat_gemm_tc_tn(ctx, v.n_rows, d_in, d_out, agg, L.ld_in, D, ld_d, g_W, d_out, accumulate, g_b));
     else SAT_TRY(sat_gemm_tn(ctx, v.n_rows, d_in, d_out, agg, L.ld_in, g_out, ld_g, mask, L.mask_words, g_W, d_out, g_b, accumulate));
     // gradient-side history, this epoch's contribution: Q_write[slot(u)] += (P_out^T D)[u] for the halo nodes u of the

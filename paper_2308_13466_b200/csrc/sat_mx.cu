@@ -248,7 +248,7 @@ static sat_status mx_launch_boxes(sat_ctx *ctx, PerDeviceOnce &attr, K kernel, i
     return SAT_OK;
 }
 
-static sat_status mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q)
+sat_status sat_mx_quantise_rows(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q)
 {
     if (q->rows == 0) return SAT_OK;
     const int32_t groups = mx_groups(q->d);
@@ -272,7 +272,7 @@ extern "C" sat_status sat_mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, 
     CHECK_CTX(ctx);
     SAT_TRY(mx_check(ctx, q, "sat_mx_quantise"));
     if (!ok_ld(ld, q->d) || (q->rows > 0 && (!x || !aligned16(x)))) return sat_fail(ctx, SAT_EINVAL, "sat_mx_quantise: null / misaligned x or bad leading dimension");
-    return mx_quantise(ctx, x, ld, q);
+    return sat_mx_quantise_rows(ctx, x, ld, q);
 }
 
 extern "C" sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int32_t ld)
@@ -397,7 +397,7 @@ extern "C" sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, i
         tmp = sat_mx_matrix{(uint8_t *)ctx->buf_mx.p, (uint8_t *)ctx->buf_mx.p + (size_t)m * ldq, m, k, ldq, lds, SAT_MX4};
         Aq = &tmp;
     }
-    if (A) SAT_TRY(mx_quantise(ctx, A, lda, Aq));
+    if (A) SAT_TRY(sat_mx_quantise_rows(ctx, A, lda, Aq));
     dim3 grid;
     SAT_TRY(mx_grid(ctx, m, n, 1, &grid));
     const MxSimple p{mx_view(Aq), mx_view(W), nullptr, 0, m, k, k, n, bias, C, nullptr, ldc};
@@ -424,7 +424,7 @@ extern "C" sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, i
     return SAT_OK;
 }
 
-static sat_status mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
+sat_status sat_mx_gradient(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
 {
     const int32_t m = A->d;
     ProfScope prof(ctx, SATK_MX, (double)A->rows * (mx_row_bytes(A) + mx_groups(m) + 4.0 * n), 2.0 * (double)A->rows * m * n);
@@ -450,5 +450,5 @@ extern "C" sat_status sat_mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int3
     SAT_TRY(mx_check(ctx, A, "sat_mx_dense_tn"));
     if (n <= 0 || !C || !ok_ld(ldb, n) || (A->rows > 0 && (!B || !aligned16(B))) || (accumulate != 0 && accumulate != 1))
         return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: null / misaligned tensor or bad shape");
-    return mx_dense_tn(ctx, A, n, B, ldb, C, colsum, accumulate);
+    return sat_mx_gradient(ctx, A, n, B, ldb, C, colsum, accumulate);
 }

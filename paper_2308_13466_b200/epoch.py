@@ -147,10 +147,10 @@ class SatEpoch:
         assert len(W) == len(b) == self.L and all(x is not None for x in b), "a parameter step takes one weight and one bias per layer"
         return B.SAT_EPOCH_STEP
 
-    def _forward_backward(self, m: int, W, b, pred, accumulate: int, reuse_state: int, grad_history: bool = False):
+    def _forward_backward(self, m: int, W, b, pred, accumulate: int, reuse_state: int, grad_history: bool = False, keep8: bool = False):
         """Forward and backward of one partition (or all) without the commit; accumulate and reuse_state: it is not the first one."""
         assert bool(accumulate) == bool(reuse_state)
-        flags = (B.SAT_EPOCH_CONTINUE if accumulate else 0) | (B.SAT_EPOCH_GRAD_HISTORY if grad_history else 0)
+        flags = (B.SAT_EPOCH_CONTINUE if accumulate else 0) | (B.SAT_EPOCH_GRAD_HISTORY if grad_history else 0) | (B.SAT_EPOCH_KEEP8 if keep8 else 0)
         self._run(W, b, pred, None if m == B.SAT_ALL_PARTS else [m], flags)
 
     def pred_update(self, pred, lr: float, max_steps: int = 1, min_gain: float | None = None, row_weight=None):
@@ -182,23 +182,24 @@ class SatEpoch:
             seen.append(losses)
         return seen
 
-    def step(self, W, b, pred, lr: float | None = None, pred_lr: float | None = None, grad_history: bool = False):
+    def step(self, W, b, pred, lr: float | None = None, pred_lr: float | None = None, grad_history: bool = False, keep8: bool = False):
         """All partitions per launch.  W, b: lists of CUDA tensors; pred: list of sat_pred_params or None.
         pred_lr: also run one predictor update (pred_update) before the ring is committed.
-        grad_history: back-propagate with the stale-gradient term (gradient-side history of the previous epoch)."""
-        flags = B.SAT_EPOCH_GRAD_HISTORY if grad_history else 0
+        grad_history: back-propagate with the stale-gradient term (gradient-side history of the previous epoch).
+        keep8: the layers keep their aggregated inputs in 8 bits, which their weight gradients are then taken from."""
+        flags = (B.SAT_EPOCH_GRAD_HISTORY if grad_history else 0) | (B.SAT_EPOCH_KEEP8 if keep8 else 0)
         if pred_lr is None or pred is None:
             self._run(W, b, pred, None, flags | B.SAT_EPOCH_COMMIT | self._step_flag(W, b, lr), lr or 0.0)
             return
-        self._forward_backward(B.SAT_ALL_PARTS, W, b, pred, 0, 0, grad_history)
+        self._forward_backward(B.SAT_ALL_PARTS, W, b, pred, 0, 0, grad_history, keep8)
         self.pred_update(pred, pred_lr)
         B.sat_cache_commit(self.ctx)
         if lr is not None:
             B.sat_sgd_steps(self.ctx, list(W) + list(b), list(self.gW) + list(self.gb), lr)
 
-    def step_per_partition(self, W, b, pred, order=None, lr: float | None = None, grad_history: bool = False):
+    def step_per_partition(self, W, b, pred, order=None, lr: float | None = None, grad_history: bool = False, keep8: bool = False):
         """Same epoch, one partition at a time (the LSTM state table is computed by the first call of every layer)."""
-        flags = B.SAT_EPOCH_COMMIT | (B.SAT_EPOCH_GRAD_HISTORY if grad_history else 0) | self._step_flag(W, b, lr)
+        flags = B.SAT_EPOCH_COMMIT | (B.SAT_EPOCH_GRAD_HISTORY if grad_history else 0) | (B.SAT_EPOCH_KEEP8 if keep8 else 0) | self._step_flag(W, b, lr)
         self._run(W, b, pred, order if order is not None else range(self.M), flags, lr or 0.0)
 
     # ---- graph-attention backbone ---------------------------------------------------
