@@ -5,30 +5,27 @@
 // terms by taking the upper half of its bits off twice, which is exact: x = hi + mid + lo, eight bits each.  Three MMAs of
 // kind::f16 with bf16 operands then give exact products, and all that is rounded is the sum.
 //
-// The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts:
-// about a third of a unit of 2^-23 per instruction.  Only the products with hi matter for that; those with mid and lo are 2^-8 of them and
-// have an accumulator of their own.  The hi accumulator is taken out after MXT_FLUSH stages (24 instructions) and added up in registers,
-// rounded to nearest; relative error 3e-7 to 1e-6, about that of an fp32 FMA loop.
+// The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts: 612257 terms in 74
+// splits were off by 1e-5 of the result.  TN therefore takes the accumulator out every MXT_RUN stages (24 instructions) and adds it, rounded to
+// nearest, to a sum that is kept in tensor memory too: 5e-7, an fp32 FMA loop's being 1e-6.  NN has a few hundred terms, which one accumulator takes.
 //
 // A pair of CTAs shares a tile of 256 columns of Q (the M side, 128 lanes of TMEM in either CTA) by up to 256 columns (TN) or rows (NN) of
 // X.  What bounds it besides memory is shared memory, at 128 bytes a clock: per stage of 32 terms a CTA takes in 16 KB of X and 4 KB of codes
 // (written by TMA, read once), writes 24 KB and 8 KB of bf16, and the tensor core reads 32 KB (each CTA holds one half of X, and a tile of Q
-// stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  With single CTAs and X as the M side it
-// was 183 KB for as many products.
+// stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  (With single CTAs and X as the M side it
+// was 183 KB for as many products.  Loading straight into registers takes 40 KB less, but what it can keep in flight does not cover the latency.)
 //
-// 20 warps.  Warps 0..15 convert, in two groups on alternate stages, and hold the sums; warp 16 of the first CTA issues the MMAs; warp 17 the
-// loads; warps 18 and 19 add up the columns of X where the bias gradient is asked for.
+// 22 warps: 0..15 convert, four groups on stages in turn; 16..19 take results out of the accumulators; 20, of the first CTA, issues the MMAs; 21 the
+// loads.
 #include "sat_mx.h"
 #include "sat_ptx.h"
 
 #include <algorithm>
 
-#define MXT_WORKERS 16
-#define MXT_THREADS ((MXT_WORKERS + 4) * 32)   /* five whole warpgroups, see k_mx_gemm */
+#define MXT_GROUPS 4                 /* groups of four converting warps; each has a raw and an operand stage of its own */
+#define MXT_EPILOGUE (4 * MXT_GROUPS)   /* first of the four warps that take results out */
+#define MXT_THREADS ((MXT_EPILOGUE + 6) * 32)
 #define MXT_KB 32                    /* terms per stage */
-#define MXT_RAW 6                    /* stages of raw tiles; an even number, so that either group keeps to its own */
-#define MXT_OP 3                     /* stages of converted tiles */
-#define MXT_FLUSH 12                 /* stages between two reads of the hi accumulator */
 #define MXT_Q_TILE (128 * MXT_KB * 2)
 #define MXT_X_PLANE (128 * MXT_KB * 2)
 #define MXT_STAGE (MXT_Q_TILE + 3 * MXT_X_PLANE)
@@ -36,18 +33,20 @@
 #define MXT_Q_RAW (128 * MXT_KB)
 #define MXT_RAW_STAGE (MXT_X_RAW + MXT_Q_RAW)
 #define MXT_SCALES (MXT_KB * 4)       /* of a stage: four groups a term */
+// stages that are added up in an accumulator
+template <bool TN> struct MxtRun { static constexpr int32_t stages = TN ? 4 : 16; };
 
 struct MxtShared {
-    double sums[128];
+    float sums[4 * MXT_GROUPS][128];
     uint64_t sums_full, sums_empty;
-    uint8_t scales[MXT_RAW][MXT_SCALES];
-    uint64_t raw_full[MXT_RAW], raw_empty[MXT_RAW];   // TMA bytes and scales have landed; a group of workers (and the column sums) has read them
-    uint64_t op_full[MXT_OP], op_empty[MXT_OP];     // (first CTA) both CTAs' workers have written the tiles; the MMAs have read them
-    uint64_t acc_full, acc_empty;                       // the hi accumulator is to be taken out; (first CTA) both CTAs have
+    uint8_t scales[MXT_GROUPS][MXT_SCALES];
+    uint64_t raw_full[MXT_GROUPS], raw_empty[MXT_GROUPS];   // TMA bytes and scales have landed; the group has read them
+    uint64_t op_full[MXT_GROUPS], op_empty[MXT_GROUPS];     // (first CTA) both CTAs' groups have written the tiles; the MMAs have read them
+    uint64_t acc_full[2], acc_empty[2];                     // an accumulator holds a run; (first CTA) both CTAs have taken it out
     uint32_t tmem_base;
     int dead;
 };
-#define MXT_SMEM (1024 + MXT_OP * MXT_STAGE + MXT_RAW * MXT_RAW_STAGE + (int)sizeof(MxtShared))
+#define MXT_SMEM (1024 + MXT_GROUPS * (MXT_STAGE + MXT_RAW_STAGE) + (int)sizeof(MxtShared))
 static_assert(MXT_SMEM <= 227 * 1024, "shared memory");
 
 struct MxtArgs {
@@ -135,22 +134,20 @@ __device__ __forceinline__ uint4 bf16x8_mul(const uint4 &v, uint32_t s)
 {
     return make_uint4(bf16x2_mul(v.x, s), bf16x2_mul(v.y, s), bf16x2_mul(v.z, s), bf16x2_mul(v.w, s));
 }
-// eight fp32 values -> eight bf16 each of hi, mid, lo (upper halves; what is left after two of them fits a third)
-__device__ __forceinline__ void mxt_split8(const float4 &a, const float4 &b, uint4 &hi, uint4 &mid, uint4 &lo)
+// four fp32 values -> four bf16 each of hi, mid, lo (upper halves; what is left after two of them fits a third)
+__device__ __forceinline__ float2 mxt_left(const float2 &x, uint32_t upper)   // x - its upper halves, by a packed multiply-add
 {
-    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t h[4], m[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        h[i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
-        const float r0 = x[2 * i] - __uint_as_float(h[i] * 0x10000u), r1 = x[2 * i + 1] - __uint_as_float(h[i] & 0xFFFF0000u);
-        m[i] = __byte_perm(__float_as_uint(r0), __float_as_uint(r1), 0x7632);
-        const float s0 = r0 - __uint_as_float(m[i] * 0x10000u), s1 = r1 - __uint_as_float(m[i] & 0xFFFF0000u);
-        l[i] = __byte_perm(__float_as_uint(s0), __float_as_uint(s1), 0x7632);
-    }
-    hi = make_uint4(h[0], h[1], h[2], h[3]);
-    mid = make_uint4(m[0], m[1], m[2], m[3]);
-    lo = make_uint4(l[0], l[1], l[2], l[3]);
+    return __ffma2_rn(make_float2(__uint_as_float(upper * 0x10000u), __uint_as_float(upper & 0xFFFF0000u)), make_float2(-1.f, -1.f), x);
+}
+__device__ __forceinline__ uint32_t mxt_upper(const float2 &x) { return __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632); }
+__device__ __forceinline__ void mxt_split4(const float4 &x, uint2 &hi, uint2 &mid, uint2 &lo)
+{
+    float2 a = make_float2(x.x, x.y), b = make_float2(x.z, x.w);
+    hi = make_uint2(mxt_upper(a), mxt_upper(b));
+    a = mxt_left(a, hi.x);
+    b = mxt_left(b, hi.y);
+    mid = make_uint2(mxt_upper(a), mxt_upper(b));
+    lo = make_uint2(mxt_upper(mxt_left(a, mid.x)), mxt_upper(mxt_left(b, mid.y)));
 }
 
 __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t *r)
@@ -160,8 +157,43 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t *r)
                    "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr)
                  : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared memory by its own addresses (through generic pointers, a conversion took a third more instructions)
+__device__ __forceinline__ float4 lds_f4(uint32_t at)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 lds_u4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds_u2(uint32_t at)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds_u1(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts_u2(uint32_t at, const uint2 &v) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(v.x), "r"(v.y) : "memory"); }
+__device__ __forceinline__ void sts_u4(uint32_t at, const uint4 &v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
 
 // bf16 operands, fp32 accumulation; Q is MN-major (its tile has a row per term), X is with TN
 template <bool TN>
@@ -170,8 +202,9 @@ __device__ __forceinline__ uint32_t mxt_idesc(int32_t bn)
     return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | (TN ? 1u << 16 : 0u) | (uint32_t)(bn >> 3) << 17 | (256u >> 4) << 24;
 }
 
-// Waits like mbar_wait_all, but the hardware may put the warp aside for up to a microsecond a time: what waits here would take issue slots
-// from the warps that convert, which are bound by them
+// Waits like mbar_wait_all in as few instructions as possible (what waits takes issue slots from the warps that convert, which are bound by them): the
+// hardware may put the warp aside for up to a microsecond a time, and whether others have given up is looked at every sixteenth time.
+template <int SLEEP_NS = 0>
 __device__ __forceinline__ bool mxt_wait(uint64_t *bar, uint32_t parity, volatile int *dead, int *status)
 {
     const uint32_t addr = smem_u32(bar);
@@ -187,7 +220,8 @@ __device__ __forceinline__ bool mxt_wait(uint64_t *bar, uint32_t parity, volatil
             : "r"(addr), "r"(parity), "r"(1000u)
             : "memory");
         if (__all_sync(0xffffffffu, ok)) return true;
-        if (__any_sync(0xffffffffu, *dead)) return false;
+        if ((it & 15u) == 15u && __any_sync(0xffffffffu, *dead)) return false;
+        if (SLEEP_NS > 0) __nanosleep(SLEEP_NS);
     }
     *dead = 1;
     atomicOr(status, 1);
@@ -202,295 +236,239 @@ struct MxtMem {
     int32_t rank;              // CTA of the pair
     int32_t unit, units;       // pair, and pairs
 };
+// Tensor memory: an accumulator and the sum of the runs (TN), or two accumulators by turns
+#define MXT_SUM 256u
+template <bool TN> __device__ __forceinline__ uint32_t mxt_buf(uint32_t run) { return TN ? 0u : run & 1u; }
+template <bool TN> __device__ __forceinline__ uint32_t mxt_phase(uint32_t run) { return TN ? run & 1u : (run >> 1) & 1u; }
 
 template <bool TN>
 __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
 {
     volatile int *dead = &s.sh->dead;
-    const uint32_t idesc = mxt_idesc<TN>(a.bn), hi = s.tmem, rest = s.tmem + 256u;
+    const uint32_t idesc = mxt_idesc<TN>(a.bn);
     // MN-major tiles: blocks of 64 columns (128 bytes a term, 128-byte swizzle) MXT_KB x 128 bytes apart, groups of eight terms 1024 bytes
     // apart; an instruction takes 16 terms.  K-major (X without TN): a row's 32 terms are 64 bytes, 64-byte swizzle, eight rows 512 apart.
     const uint64_t q0 = make_desc(smem_u32(s.op), MXT_KB * 128, 1024, 2);
     const uint64_t x0 = TN ? make_desc(smem_u32(s.op) + MXT_Q_TILE, MXT_KB * 128, 1024, 2) : make_desc(smem_u32(s.op) + MXT_Q_TILE, 16, 512, 4);
     constexpr uint32_t x_step = (TN ? 2048 : 32) >> 4, q_step = 2048 >> 4, plane = MXT_X_PLANE >> 4;
-    uint32_t st = 0, ph = 0, taken = 0;   // taken: times the accumulators were handed over
+    uint32_t st = 0, ph = 0, run = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
-        int32_t in_run = 0;               // stages since the hi accumulator was last handed over
-        for (int32_t k = 0; k < stages; ++k) {
-            if (!mxt_wait(&s.sh->op_full[st], ph, dead, a.status)) return;
-            // (acc_empty's phase `taken - 1` completes when the workers have read what was handed over last)
-            if (k == 0 && taken > 0 && !mxt_wait(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
-            tc_fence_after();
-            const uint64_t q = q0 + (uint64_t)(st * (MXT_STAGE >> 4)), x = x0 + (uint64_t)(st * (MXT_STAGE >> 4));
-            const bool run_starts = in_run == 0 && k > 0, hand_over = ++in_run == MXT_FLUSH || k + 1 == stages;
-            if (!run_starts) {
+        for (int32_t k0 = 0; k0 < stages; k0 += MxtRun<TN>::stages, ++run) {
+            const uint32_t buf = mxt_buf<TN>(run), acc = s.tmem + 256u * buf;
+            if (!mxt_wait(&s.sh->acc_empty[buf], mxt_phase<TN>(run) ^ 1u, dead, a.status)) return;
+            const int32_t n = min(stages - k0, MxtRun<TN>::stages);
+            for (int32_t k = 0; k < n; ++k) {
+                if (!mxt_wait(&s.sh->op_full[st], ph, dead, a.status)) return;
+                tc_fence_after();
+                const uint64_t q = q0 + (uint64_t)(st * (MXT_STAGE >> 4)), x = x0 + (uint64_t)(st * (MXT_STAGE >> 4));
                 if (elect_one()) {
 #pragma unroll
                     for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {   // the tile of Q stays in the collector for its three products
-                        tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, k > 0 || ks > 0 ? 1u : 0u);
-                        tc_mma_f16<3, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, 1u);
-                        tc_mma_f16<2, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, k > 0 || ks > 0 ? 1u : 0u);
+                        tc_mma_f16<1, 2>(acc, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, k > 0 || ks > 0 ? 1u : 0u);
+                        tc_mma_f16<3, 2>(acc, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
+                        tc_mma_f16<2, 2>(acc, q + ks * q_step, x + ks * x_step, idesc, 1u);
                     }
-                }
-            } else {   // mid and lo go ahead while the hi accumulator is still being read
-                if (elect_one()) {
-#pragma unroll
-                    for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {
-                        tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
-                        tc_mma_f16<2, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, 1u);
-                    }
+                    tc_commit<2>(&s.sh->op_empty[st]);
+                    if (k + 1 == n) tc_commit<2>(&s.sh->acc_full[buf]);
                 }
                 __syncwarp();
-                if (!mxt_wait(&s.sh->acc_empty, (taken - 1) & 1u, dead, a.status)) return;
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) tc_mma_f16<0, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, ks > 0 ? 1u : 0u);
-                }
+                if (++st == MXT_GROUPS) st = 0, ph ^= 1u;
             }
-            __syncwarp();
-            if (elect_one()) {
-                tc_commit<2>(&s.sh->op_empty[st]);
-                if (hand_over) tc_commit<2>(&s.sh->acc_full);
-            }
-            __syncwarp();
-            if (hand_over) ++taken, in_run = 0;
-            if (++st == MXT_OP) st = 0, ph ^= 1u;
         }
     }
 }
 
-// TMA loads and, a term per lane, asynchronous copies of the scales, up to MXT_RING stages ahead of the workers
+// TMA loads and, a term per lane, asynchronous copies of the scales, as soon as a group has read what it had
 template <bool TN, int FMT>
 __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, const CUtensorMap *map_x, const CUtensorMap *map_q, int lane)
 {
     volatile int *dead = &s.sh->dead;
     const int32_t half = a.bn / 2;
-    uint32_t st = 0, ph = 0, total = 0;
+    uint32_t st = 0, ph = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         const int32_t x0 = it.n0 + s.rank * half, q0 = it.d0 + s.rank * 128;
-        const int32_t boxes = x0 >= a.N ? 0 : !TN ? 1 : min((a.N - x0 + 31) / 32, half / 32);
-        const bool has_q = q0 < a.D;
-        const uint32_t bytes = (uint32_t)boxes * (TN ? 4096u : (uint32_t)half * 128u) + (has_q ? 128u * MXT_KB * FMT / 8 : 0u);
+        const bool has_x = x0 < a.N, has_q = q0 < a.D;
+        const uint32_t bytes = (has_x ? (uint32_t)half * 128u : 0u) + (has_q ? 128u * MXT_KB * FMT / 8 : 0u);
         const uint8_t *scales = a.scales + (int64_t)(it.k0 + lane) * a.ld_scales + q0 / MX_GROUP;   // four bytes, of which some may lie behind the row's last
-        for (int32_t k = it.k0; k < it.k1; k += MXT_KB, ++total, scales += MXT_KB * a.ld_scales) {
-            if (!mxt_wait(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
+        for (int32_t k = it.k0; k < it.k1; k += MXT_KB, scales += MXT_KB * a.ld_scales) {
+            if (!mxt_wait<40>(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
             uint64_t *bar = &s.sh->raw_full[st];
             if (lane == 0) {
-                uint8_t *x = s.raw + (size_t)st * MXT_RAW_STAGE;
+                uint8_t *x = s.raw + st * MXT_RAW_STAGE;
                 mbar_expect_tx(bar, bytes);
-                if (TN)
-                    for (int b = 0; b < boxes; ++b) tma_load_2d(x + b * 4096, map_x, bar, x0 + 32 * b, k);
-                else if (boxes) tma_load_2d(x, map_x, bar, k, x0);
+                if (has_x) tma_load_2d(x, map_x, bar, TN ? x0 : k, TN ? k : x0);
                 if (has_q) tma_load_2d(x + MXT_X_RAW, map_q, bar, q0 / 8 * FMT, k);
             }
             __syncwarp();
             const bool there = has_q && k + lane < it.k1;   // (else four zero bytes and nothing read)
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(s.sh->scales[st] + 4 * lane)), "l"(there ? scales : a.scales), "r"(there ? 4u : 0u) : "memory");
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-            if (++st == MXT_RAW) st = 0, ph ^= 1u;
+            if (++st == MXT_GROUPS) st = 0, ph ^= 1u;
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    // the pair's MMAs have signalled every stage: nothing arrives here any more once both CTAs may exit
-    for (uint32_t i = 0; i < MXT_OP; ++i) {
-        const uint32_t uses = (total + MXT_OP - 1 - i) / MXT_OP;
-        if (uses > 0 && !mxt_wait(&s.sh->op_empty[i], (uses - 1) & 1u, dead, a.status)) return;
-    }
-}
-
-// The column sums of X (TN), four columns a lane: half a stage in fp32, the stages in doubles.  Two warps, with one half of every stage's terms each
-// (one alone took longer over a stage than everything else); the second one leaves its sums to the first.
-__device__ __forceinline__ void mxt_sums(const MxtArgs &a, const MxtMem &s, int part, int lane)
-{
-    volatile int *dead = &s.sh->dead;
-    const int32_t half = a.bn / 2, mine = (lane >> 3) * 32;
-    uint32_t st = 0, ph = 0, turn = 0;
-    for (int32_t i = s.unit; i < a.items; i += s.units) {
-        const MxtItem it = mxt_item(a, i);
-        const int32_t x0 = it.n0 + s.rank * half;
-        const bool sums = it.d0 == 0, here = sums && mine < half && x0 + mine < a.N;
-        double c[4] = {0., 0., 0., 0.};
-        for (int32_t k = 0; k < it.stages; ++k) {
-            if (!mxt_wait(&s.sh->raw_full[st], ph, dead, a.status)) return;
-            if (here) {
-                const uint8_t *x = s.raw + st * MXT_RAW_STAGE + (lane >> 3) * 4096 + part * (MXT_KB / 2 * 128);
-                float2 t = make_float2(0.f, 0.f), u = t;
-#pragma unroll
-                for (int r = 0; r < MXT_KB / 2; ++r) {
-                    const float4 v = *reinterpret_cast<const float4 *>(x + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-                    t = __fadd2_rn(t, make_float2(v.x, v.y));
-                    u = __fadd2_rn(u, make_float2(v.z, v.w));
-                }
-                c[0] += t.x;
-                c[1] += t.y;
-                c[2] += u.x;
-                c[3] += u.y;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
-            if (++st == MXT_RAW) st = 0, ph ^= 1u;
-        }
-        if (!sums) continue;
-        double *slot = s.sh->sums + 4 * lane;
-        if (part == 1) {
-            if (!mxt_wait(&s.sh->sums_empty, (turn & 1u) ^ 1u, dead, a.status)) return;
-            for (int j = 0; j < 4; ++j) slot[j] = c[j];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->sums_full);
-        } else {
-            if (!mxt_wait(&s.sh->sums_full, turn & 1u, dead, a.status)) return;
-            for (int j = 0; j < 4; ++j) {
-                const int32_t col = x0 + 4 * lane + j;
-                const double both = c[j] + slot[j];
-                if (!here || 4 * lane + j >= half || col >= a.N) continue;
-                float *out = a.colsum + (int64_t)it.split * a.N + col;
-                *out = a.add ? (float)((double)*out + both) : (float)both;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->sums_empty);
-        }
-        ++turn;
-    }
 }
 
 template <bool TN, int FMT>
 __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    const uint32_t group = (uint32_t)warp >> 3;
-    const int w = warp & 7;
-    const int32_t half = a.bn / 2;
-    // 16 elements of Q and twice eight values of X per thread and stage.  Terms and places along a row go over the lanes so that eight
-    // lanes in turn touch all banks, in the raw rows as in the swizzled ones.
-    const int j = (lane >> 2) & 1, term = 4 * w + 2 * (lane >> 4) + (j ^ ((lane >> 3) & 1)), place = (lane & 3) | j << 2;
-    const uint32_t q_raw = MXT_X_RAW + (uint32_t)(term * 128 + 16 * place) * FMT / 8;
-    const uint32_t q_op = (uint32_t)(place >> 2) * (MXT_KB * 128) + (uint32_t)term * 128u + ((uint32_t)((2 * (place & 3)) ^ (term & 7)) << 4);
-    // TN: columns 8 place .. of the term, and 64 columns on.  NN: terms 8 (lane % 4) .. of a row, and of the row 64 on.
-    const int row = 8 * w + (lane >> 2), quad = lane & 3;
-    const uint32_t x_raw = TN ? (uint32_t)(place >> 2) * 4096u + (uint32_t)term * 128u + ((uint32_t)((2 * (place & 3)) ^ (term & 7)) << 4)
-                              : (uint32_t)row * 128u + ((uint32_t)((2 * quad) ^ (row & 7)) << 4);
-    const uint32_t x_op = MXT_Q_TILE + (TN ? (uint32_t)term * 128u + ((uint32_t)(place ^ (term & 7)) << 4) : (uint32_t)row * 64u + ((uint32_t)(quad ^ ((row >> 1) & 3)) << 4));
-    constexpr uint32_t x_raw2 = 8192u, x_op2 = 4096u;    // the second eight: two boxes, or 64 rows, further on
-    const int32_t x_first = TN ? 8 * place : row;        // its index within the CTA's half; the second is 64 further on
-    const int32_t chunks = a.bn / 32, slice = warp >> 2; // 32 columns of the accumulators each: chunks slice and slice + 4 are this warp's
-    const uint32_t lanes = s.tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const int32_t group = warp >> 2, w = warp & 3, half = a.bn / 2;
+    const uint32_t raw = smem_u32(s.raw) + (uint32_t)group * MXT_RAW_STAGE, op = smem_u32(s.op) + (uint32_t)group * MXT_STAGE;
+    // Per thread and stage: eight times four values of X and two times 16 elements of Q.
+    // TN: columns 4 lane .. of the terms w + 4 i; a warp reads a term's 512 bytes, half of it writes 128 of a block of 64 columns.
+    // NN: terms 4 (lane % 8) .. of the rows 4 w + lane / 8 + 16 i; eight lanes read 128 bytes of a row and write its 64.
+    const int32_t x_row = TN ? w : 4 * w + (lane >> 3), x_col = TN ? 4 * lane : 4 * (lane & 7);
+    constexpr int32_t x_apart = TN ? 4 : 16;
+    const uint32_t x_raw = raw + (uint32_t)x_row * (TN ? (uint32_t)half * 4u : 128u) + (uint32_t)x_col * 4u;
+    const uint32_t x_next = (uint32_t)x_apart * (TN ? (uint32_t)half * 4u : 128u);
+    const uint32_t x_op = op + MXT_Q_TILE + (TN ? (uint32_t)(lane >> 4) * (MXT_KB * 128) + (uint32_t)x_row * 128u + ((uint32_t)(((lane & 15) >> 1) ^ x_row) << 4)
+                                          : (uint32_t)x_row * 64u + ((uint32_t)(((lane & 7) >> 1) ^ ((x_row >> 1) & 3)) << 4)) + (uint32_t)(lane & 1) * 8u;
+    // Q: elements 16 place .. of the terms term + 16 i.  Eight lanes write a term's two halves of 128 bytes: those of the second half its 16-byte pieces in
+    // the other order, so that they meet no bank twice
+    const int32_t place = lane & 7, term = 4 * w + (lane >> 3), other = place >> 2;
+    const uint32_t q_raw = raw + MXT_X_RAW + (uint32_t)(term * 128 + 16 * place) * FMT / 8, scales = smem_u32(s.sh->scales[group]) + 4u * (uint32_t)term + ((uint32_t)place >> 1);
+    const uint32_t q_op = op + (uint32_t)other * (MXT_KB * 128) + (uint32_t)term * 128u;
+    const uint32_t q_at = (uint32_t)((2 * (place & 3) + other) ^ (term & 7)) << 4;
 
-    float acc[2][32];
+    uint32_t ph = 0, turn = 0;
+    int32_t base = 0;   // stages before this item, modulo the groups
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
+        const MxtItem it = mxt_item(a, i);
+        const int32_t x0 = it.n0 + s.rank * half;
+        const bool sums = TN && a.colsum && it.d0 == 0, has_q = it.d0 + s.rank * 128 + 16 * place < a.D;
+        // how many of this thread's rows there are (NN), or whether its columns are (TN)
+        const int32_t end = min(half, a.N - x0), has_x = TN ? (x_col < end ? 8 : 0) : (x_row < end ? (end - 1 - x_row) / x_apart + 1 : 0);
+        float4 total = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int32_t k = (group - base) & (MXT_GROUPS - 1); k < it.stages; k += MXT_GROUPS, ph ^= 1u) {
+            if (!mxt_wait(&s.sh->raw_full[group], ph, dead, a.status)) return;
+            float4 x[8];
+            uint32_t c[2][4], byte[2];
 #pragma unroll
-    for (int c = 0; c < 64; ++c) acc[c >> 5][c & 31] = 0.f;
-    uint32_t taken = 0;
-    auto take = [&](bool last) -> bool {
-        if (!mxt_wait(&s.sh->acc_full, taken & 1u, dead, a.status)) return false;
-        tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-            if (slice + 4 * c < chunks) {
+            for (int h = 0; h < 8; ++h)
+                if (h < has_x) x[h] = lds_f4(x_raw + h * x_next);
+            if (has_q)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    uint32_t r[16];
-                    tc_ld16(lanes + (uint32_t)(slice + 4 * c) * 32u + 16u * h, r);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[c][16 * h + e] += __uint_as_float(r[e]);
-                    if (last) {
-                        tc_ld16(lanes + 256u + (uint32_t)(slice + 4 * c) * 32u + 16u * h, r);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[c][16 * h + e] += __uint_as_float(r[e]);
+                    byte[h] = lds_u1(scales + 64 * h);
+                    if (FMT == SAT_MX8) {
+                        const uint4 t = lds_u4(q_raw + h * (16 * 128));
+                        c[h][0] = t.x, c[h][1] = t.y, c[h][2] = t.z, c[h][3] = t.w;
+                    } else {
+                        const uint2 t = lds_u2(q_raw + h * (16 * 64));
+                        c[h][0] = t.x, c[h][2] = t.y, c[h][1] = c[h][3] = 0u;
                     }
                 }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->raw_empty[group]);
+            if (sums && has_x) {
+                total.x += ((x[0].x + x[1].x) + (x[2].x + x[3].x)) + ((x[4].x + x[5].x) + (x[6].x + x[7].x));
+                total.y += ((x[0].y + x[1].y) + (x[2].y + x[3].y)) + ((x[4].y + x[5].y) + (x[6].y + x[7].y));
+                total.z += ((x[0].z + x[1].z) + (x[2].z + x[3].z)) + ((x[4].z + x[5].z) + (x[6].z + x[7].z));
+                total.w += ((x[0].w + x[1].w) + (x[2].w + x[3].w)) + ((x[4].w + x[5].w) + (x[6].w + x[7].w));
             }
-        tc_fence_before();
-        mbar_arrive_warp<2>(&s.sh->acc_empty, lane);
-        ++taken;
-        return true;
-    };
-    // A lane has a column of Q, a register a column or row of X: consecutive lanes write consecutive floats
-    auto finish = [&](int32_t item) -> bool {
-        if (!take(true)) return false;
-        const MxtItem it = mxt_item(a, item);
-        const int32_t col = it.d0 + s.rank * 128 + (warp & 3) * 32 + lane;
+            if (!mxt_wait(&s.sh->op_empty[group], ph ^ 1u, dead, a.status)) return;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int32_t first = it.n0 + (slice + 4 * c) * 32;
-            float *o = a.C + it.split * a.split + first * a.by_x + col * a.by_q;
-            if (slice + 4 * c < chunks && col < a.D) {
-                if (first + 32 <= a.N && !(TN && a.add)) {
+            for (int h = 0; h < 8; ++h)
+                if (h < has_x) {
+                    uint2 hi, mid, lo;
+                    mxt_split4(x[h], hi, mid, lo);
+                    // TN: the term four on has the other half of a row's swizzle
+                    const uint32_t o = TN ? (x_op ^ (uint32_t)((h & 1) << 6)) + h * 512 : x_op + h * 1024;
+                    sts_u2(o, hi);
+                    sts_u2(o + MXT_X_PLANE, mid);
+                    sts_u2(o + 2 * MXT_X_PLANE, lo);
+                }
+            if (has_q)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e, o += a.by_x) *o = acc[c][e];
+                for (int h = 0; h < 2; ++h) {
+                    const MxtScale<FMT> sc(byte[h]);
+                    // the half that is written first: the upper one for lanes of the second block
+                    const uint32_t a0 = other ? c[h][2] : c[h][0], a1 = other ? c[h][3] : c[h][1], b0 = other ? c[h][0] : c[h][2], b1 = other ? c[h][1] : c[h][3];
+                    uint4 v0 = mxt_decode8<FMT>(a0, a1, sc), v1 = mxt_decode8<FMT>(b0, b1, sc);
+                    if (sc.two) v0 = bf16x8_mul(v0, sc.second), v1 = bf16x8_mul(v1, sc.second);
+                    sts_u4(q_op + h * 2048 + q_at, v0);
+                    sts_u4(q_op + h * 2048 + (q_at ^ 16u), v1);
+                }
+            fence_async_smem();
+            mbar_arrive_warp<2>(&s.sh->op_full[group], lane);
+        }
+        base += it.stages;
+        if (sums) {   // the sixteen warps' sums of a column are added up by the warp that writes them
+            if (!mxt_wait(&s.sh->sums_empty, (turn & 1u) ^ 1u, dead, a.status)) return;
+            *reinterpret_cast<float4 *>(s.sh->sums[warp] + 4 * lane) = total;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->sums_full);
+            ++turn;
+        }
+    }
+    // the pair's MMAs have signalled this group's stages: nothing arrives here any more once both CTAs may exit
+    (void)mxt_wait(&s.sh->op_empty[group], ph ^ 1u, dead, a.status);
+}
+
+// A lane has a column of Q, a register a column or row of X: consecutive lanes write consecutive floats.  Without a sum in tensor memory (NN) runs behind
+// the first of an item are added to what that one wrote.
+template <bool TN>
+__device__ __forceinline__ void mxt_results(const MxtArgs &a, const MxtMem &s, int warp, int lane)
+{
+    volatile int *dead = &s.sh->dead;
+    const uint32_t lanes = s.tmem + ((uint32_t)(warp * 32) << 16);
+    uint32_t run = 0, turn = 0;
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
+        const MxtItem it = mxt_item(a, i);
+        const int32_t col = it.d0 + s.rank * 128 + warp * 32 + lane, n = min(a.bn, a.N - it.n0);
+        for (int32_t k0 = 0; k0 < it.stages; k0 += MxtRun<TN>::stages, ++run) {
+            const uint32_t buf = mxt_buf<TN>(run);
+            const bool write = !TN || k0 + MxtRun<TN>::stages >= it.stages, add = a.add || (!TN && k0 > 0);
+            if (!mxt_wait<100>(&s.sh->acc_full[buf], mxt_phase<TN>(run), dead, a.status)) return;
+            tc_fence_after();
+            float *o = a.C + it.split * a.split + it.n0 * a.by_x + col * a.by_q;
+            for (int32_t c = 0; c < a.bn; c += 16) {
+                uint32_t r[16], t[16];
+                tc_ld16(lanes + 256u * buf + (uint32_t)c, r);
+                if (TN && k0 > 0) tc_ld16(lanes + MXT_SUM + (uint32_t)c, t);
+                tc_wait_ld();
+                if (c + 16 >= a.bn) {   // the accumulator has been read
+                    tc_fence_before();
+                    mbar_arrive_warp<2>(&s.sh->acc_empty[buf], lane);
+                }
+                if (TN && k0 > 0) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + __uint_as_float(t[e]));
+                }
+                if (!write) {
+                    tc_st16(lanes + MXT_SUM + (uint32_t)c, r);
+                    continue;
+                }
+                if (col >= a.D) continue;
+                if (c + 16 <= n && !add) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e, o += a.by_x) *o = __uint_as_float(r[e]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e, o += a.by_x)
-                        if (first + e < a.N) *o = TN && a.add ? *o + acc[c][e] : acc[c][e];
+                    for (int e = 0; e < 16; ++e, o += a.by_x)
+                        if (c + e < n) *o = add ? *o + __uint_as_float(r[e]) : __uint_as_float(r[e]);
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 32; ++e) acc[c][e] = 0.f;
+            if (!write) tc_wait_st();
         }
-        return true;
-    };
-
-    uint32_t base = 0;      // parity of the stages before this item
-    uint32_t rs = group, rph = 0, os = group, oph = 0;
-    int32_t pending = -1;   // the item that is to be finished
-    for (int32_t i = s.unit;; i += s.units) {
-        MxtItem it{};       // (no stages behind the last one)
-        if (i < a.items) it = mxt_item(a, i);
-        const bool has_q = it.d0 + s.rank * 128 + 16 * place < a.D;
-        const int32_t x0 = it.n0 + s.rank * half + x_first;
-        const bool has_x = x_first < half && x0 < a.N, has_x2 = x_first + 64 < half && x0 + 64 < a.N;
-        int32_t run_end = MXT_FLUSH;
-#pragma unroll 1
-        for (int32_t k = (int32_t)(group ^ base);; k += 2) {
-            if (k < it.stages) {
-                if (!mxt_wait(&s.sh->raw_full[rs], rph, dead, a.status)) return;
-                if (!mxt_wait(&s.sh->op_empty[os], oph ^ 1u, dead, a.status)) return;
-                const uint8_t *raw = s.raw + rs * MXT_RAW_STAGE;
-                uint8_t *op = s.op + os * MXT_STAGE;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (h ? has_x2 : has_x) {
-                        uint4 hi, mid, lo;
-                        mxt_split8(*reinterpret_cast<const float4 *>(raw + x_raw + h * x_raw2), *reinterpret_cast<const float4 *>(raw + (x_raw ^ 16u) + h * x_raw2), hi, mid, lo);
-                        uint8_t *o = op + x_op + h * x_op2;
-                        *reinterpret_cast<uint4 *>(o) = hi;
-                        *reinterpret_cast<uint4 *>(o + MXT_X_PLANE) = mid;
-                        *reinterpret_cast<uint4 *>(o + 2 * MXT_X_PLANE) = lo;
-                    }
-                if (has_q) {
-                    const MxtScale<FMT> sc(s.sh->scales[rs][4 * term + (place >> 1)]);
-                    uint4 v0, v1;
-                    if (FMT == SAT_MX8) {
-                        const uint4 c = *reinterpret_cast<const uint4 *>(raw + q_raw);
-                        v0 = mxt_decode8<FMT>(c.x, c.y, sc), v1 = mxt_decode8<FMT>(c.z, c.w, sc);
-                    } else {
-                        const uint2 c = *reinterpret_cast<const uint2 *>(raw + q_raw);
-                        v0 = mxt_decode8<FMT>(c.x, 0u, sc), v1 = mxt_decode8<FMT>(c.y, 0u, sc);
-                    }
-                    if (sc.two) v0 = bf16x8_mul(v0, sc.second), v1 = bf16x8_mul(v1, sc.second);
-                    *reinterpret_cast<uint4 *>(op + q_op) = v0;
-                    *reinterpret_cast<uint4 *>(op + (q_op ^ 16u)) = v1;
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s.sh->raw_empty[rs]);
-                mbar_arrive_warp<2>(&s.sh->op_full[os], lane);
-                if ((rs += 2) >= MXT_RAW) rs -= MXT_RAW, rph ^= 1u;
-                if ((os += 2) >= MXT_OP) os -= MXT_OP, oph ^= 1u;
+        if (TN && a.colsum && it.d0 == 0 && warp == 0) {
+            if (!mxt_wait(&s.sh->sums_full, turn & 1u, dead, a.status)) return;
+            for (int32_t c = lane; c < a.bn / 2; c += 32) {
+                double sum = 0.;
+                for (int h = 0; h < 4 * MXT_GROUPS; ++h) sum += (double)s.sh->sums[h][c];
+                const int32_t at = it.n0 + s.rank * (a.bn / 2) + c;
+                if (at >= a.N) continue;
+                float *out = a.colsum + (int64_t)it.split * a.N + at;
+                *out = a.add ? (float)((double)*out + sum) : (float)sum;
             }
-            // Accumulators are taken out a stage late, so that the MMAs have something to do meanwhile
-            if (pending >= 0) {
-                if (!finish(pending)) return;
-                pending = -1;
-            }
-            for (; run_end < it.stages && run_end <= k; run_end += MXT_FLUSH)
-                if (!take(false)) return;
-            if (k >= it.stages) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->sums_empty);
+            ++turn;
         }
-        if (i >= a.items) return;
-        base ^= (uint32_t)it.stages & 1u;
-        pending = i;
     }
 }
 
@@ -502,51 +480,44 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     MxtMem s;
     s.op = smem;
-    s.raw = smem + MXT_OP * MXT_STAGE;
-    s.sh = (MxtShared *)(s.raw + MXT_RAW * MXT_RAW_STAGE);
+    s.raw = smem + MXT_GROUPS * MXT_STAGE;
+    s.sh = (MxtShared *)(s.raw + MXT_GROUPS * MXT_RAW_STAGE);
     s.rank = (int32_t)(blockIdx.x & 1u);
     s.unit = (int32_t)(blockIdx.x >> 1);
     s.units = (int32_t)(gridDim.x >> 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < MXT_RAW; ++i) {
-            mbar_init(&s.sh->raw_full[i], 1 + 32);            // the TMA's issuer and the scales' lanes
-            mbar_init(&s.sh->raw_empty[i], MXT_WORKERS / 2 + (TN && a.colsum ? 2 : 0));
-        }
-        for (int i = 0; i < MXT_OP; ++i) {
-            mbar_init(&s.sh->op_full[i], MXT_WORKERS);        // a group of either CTA
+        for (int i = 0; i < MXT_GROUPS; ++i) {
+            mbar_init(&s.sh->raw_full[i], 1 + 32);   // the TMA's issuer and the scales' lanes
+            mbar_init(&s.sh->raw_empty[i], 4);
+            mbar_init(&s.sh->op_full[i], 2 * 4);     // a group of either CTA
             mbar_init(&s.sh->op_empty[i], 1);
         }
-        mbar_init(&s.sh->acc_full, 1);
-        mbar_init(&s.sh->sums_full, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.sh->acc_full[i], 1);
+            mbar_init(&s.sh->acc_empty[i], 2 * 4);
+        }
+        mbar_init(&s.sh->sums_full, 4 * MXT_GROUPS);
         mbar_init(&s.sh->sums_empty, 1);
-        mbar_init(&s.sh->acc_empty, 2 * MXT_WORKERS);
         s.sh->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == MXT_WORKERS) tc_alloc<2>(&s.sh->tmem_base, 512u);
+    if (warp == MXT_EPILOGUE + 4) tc_alloc<2>(&s.sh->tmem_base, 512u);
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // the other CTA's barriers are initialised and its TMEM is allocated
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
     sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
-    // 640 threads start with 96 registers each; the four warpgroups of workers, which hold 64 sums a thread, go to 104 and the fifth one
-    // to 64: 4 x 104 + 64 = 5 x 96
-    if (warp < MXT_WORKERS) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-        mxt_work<TN, FMT>(a, s, warp, lane);
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == MXT_WORKERS && s.rank == 0) mxt_mma<TN>(a, s);
-        else if (warp == MXT_WORKERS + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
-        else if (TN && warp >= MXT_WORKERS + 2 && a.colsum) mxt_sums(a, s, warp - (MXT_WORKERS + 2), lane);
-    }
+    if (warp < MXT_EPILOGUE) mxt_work<TN, FMT>(a, s, warp, lane);
+    else if (warp < MXT_EPILOGUE + 4) mxt_results<TN>(a, s, warp - MXT_EPILOGUE, lane);
+    else if (warp > MXT_EPILOGUE + 4) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
+    else if (s.rank == 0) mxt_mma<TN>(a, s);
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // neither CTA's shared memory or TMEM is in use by the other any more
-    if (warp == MXT_WORKERS) {
+    if (warp == MXT_EPILOGUE + 4) {
         tc_fence_after();
         tc_dealloc<2>(s.tmem, 512u);
     }
@@ -630,7 +601,7 @@ sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, co
     a.C = C;
     a.by_x = ldc;
     a.by_q = 1;
-    SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, W->rows, m, (int64_t)lda * 4, MXT_KB, bn / 2, CU_TENSOR_MAP_SWIZZLE_128B));
+    SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, W->rows, m, (int64_t)lda * 4, MXT_KB, bn / 2, CU_TENSOR_MAP_SWIZZLE_NONE));
     return W->format == SAT_MX8 ? mxt_launch<false, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<false, SAT_MX4>(ctx, map_x, map_q, a);
 }
 
@@ -664,7 +635,7 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
         a.by_q = 1;
         a.colsum = colsum ? a.C + splits * a.split : nullptr;
     }
-    SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, B, n, A->rows, (int64_t)ldb * 4, 32, MXT_KB, CU_TENSOR_MAP_SWIZZLE_128B));
+    SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, B, n, A->rows, (int64_t)ldb * 4, bn / 2, MXT_KB, CU_TENSOR_MAP_SWIZZLE_NONE));
     SAT_TRY((A->format == SAT_MX8 ? mxt_launch<true, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<true, SAT_MX4>(ctx, map_x, map_q, a)));
     if (splits == 1) return SAT_OK;
     if (cdiv64(n, 8) > 65535) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: shape is too large");
