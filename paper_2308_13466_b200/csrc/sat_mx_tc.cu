@@ -6,8 +6,9 @@
 // kind::f16 with bf16 operands then give exact products, and all that is rounded is the sum.
 //
 // The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts: 612257 terms in 74
-// splits were off by 1e-5 of the result.  TN therefore takes the accumulator out every MXT_RUN stages (24 instructions) and adds it, rounded to
-// nearest, to a sum that is kept in tensor memory too: 5e-7, an fp32 FMA loop's being 1e-6.  NN has a few hundred terms, which one accumulator takes.
+// splits were off by 1e-5 of the result.  Only the products with hi matter for that; with TN those with mid and lo, 2^-8 of them, have an accumulator of
+// their own, and the one of hi is taken out every 12 stages (24 instructions) and added up in registers, rounded to nearest: 5e-7, an fp32 FMA loop's
+// being 1e-6.  NN has a few hundred terms, which one accumulator takes (1e-7).
 //
 // A pair of CTAs shares a tile of 256 columns of Q (the M side, 128 lanes of TMEM in either CTA) by up to 256 columns (TN) or rows (NN) of
 // X.  What bounds it besides memory is shared memory, at 128 bytes a clock: per stage of 32 terms a CTA takes in 16 KB of X and 4 KB of codes
@@ -15,16 +16,14 @@
 // stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  (With single CTAs and X as the M side it
 // was 183 KB for as many products.  Loading straight into registers takes 40 KB less, but what it can keep in flight does not cover the latency.)
 //
-// 22 warps: 0..15 convert, four groups on stages in turn; 16..19 take results out of the accumulators; 20, of the first CTA, issues the MMAs; 21 the
-// loads.
+// Groups of four warps convert stages in turn; others take results out of the accumulators, and with TN hold the sums of the runs; one warp, of the
+// first CTA, issues the MMAs, one the loads, and with TN one adds up the column sums that the converters made on the way.
 #include "sat_mx.h"
 #include "sat_ptx.h"
 
 #include <algorithm>
 
-#define MXT_GROUPS 4                 /* groups of four converting warps; each has a raw and an operand stage of its own */
-#define MXT_EPILOGUE (4 * MXT_GROUPS)   /* first of the four warps that take results out */
-#define MXT_THREADS ((MXT_EPILOGUE + 6) * 32)
+#define MXT_SLOTS 4                  /* stages of raw and of converted tiles */
 #define MXT_KB 32                    /* terms per stage */
 #define MXT_Q_TILE (128 * MXT_KB * 2)
 #define MXT_X_PLANE (128 * MXT_KB * 2)
@@ -33,20 +32,23 @@
 #define MXT_Q_RAW (128 * MXT_KB)
 #define MXT_RAW_STAGE (MXT_X_RAW + MXT_Q_RAW)
 #define MXT_SCALES (MXT_KB * 4)       /* of a stage: four groups a term */
-// stages that are added up in an accumulator
-template <bool TN> struct MxtRun { static constexpr int32_t stages = TN ? 4 : 16; };
+// groups: of four converting warps, a divisor of the slots; run: stages that are added up in an accumulator; takers: warps that take results out, the first
+// behind the converters; then the one that issues the MMAs, the one that loads, and (TN) the one with the column sums
+template <bool TN> struct Mxt;
+template <> struct Mxt<true> { static constexpr int32_t groups = 2, run = 12, takers = 8, workers = 4 * groups, mma = workers + takers, threads = 20 * 32; };
+template <> struct Mxt<false> { static constexpr int32_t groups = 4, run = 16, takers = 4, workers = 4 * groups, mma = workers + takers, threads = (mma + 2) * 32; };
 
 struct MxtShared {
-    float sums[4 * MXT_GROUPS][128];
+    float sums[Mxt<true>::workers][128];
     uint64_t sums_full, sums_empty;
-    uint8_t scales[MXT_GROUPS][MXT_SCALES];
-    uint64_t raw_full[MXT_GROUPS], raw_empty[MXT_GROUPS];   // TMA bytes and scales have landed; the group has read them
-    uint64_t op_full[MXT_GROUPS], op_empty[MXT_GROUPS];     // (first CTA) both CTAs' groups have written the tiles; the MMAs have read them
+    uint8_t scales[MXT_SLOTS][MXT_SCALES];
+    uint64_t raw_full[MXT_SLOTS], raw_empty[MXT_SLOTS];   // TMA bytes and scales have landed; the group has read them
+    uint64_t op_full[MXT_SLOTS], op_empty[MXT_SLOTS];     // (first CTA) both CTAs' groups have written the tiles; the MMAs have read them
     uint64_t acc_full[2], acc_empty[2];                     // an accumulator holds a run; (first CTA) both CTAs have taken it out
     uint32_t tmem_base;
     int dead;
 };
-#define MXT_SMEM (1024 + MXT_GROUPS * (MXT_STAGE + MXT_RAW_STAGE) + (int)sizeof(MxtShared))
+#define MXT_SMEM (1024 + MXT_SLOTS * (MXT_STAGE + MXT_RAW_STAGE) + (int)sizeof(MxtShared))
 static_assert(MXT_SMEM <= 227 * 1024, "shared memory");
 
 struct MxtArgs {
@@ -236,11 +238,8 @@ struct MxtMem {
     int32_t rank;              // CTA of the pair
     int32_t unit, units;       // pair, and pairs
 };
-// Tensor memory: an accumulator and the sum of the runs (TN), or two accumulators by turns
-#define MXT_SUM 256u
-template <bool TN> __device__ __forceinline__ uint32_t mxt_buf(uint32_t run) { return TN ? 0u : run & 1u; }
-template <bool TN> __device__ __forceinline__ uint32_t mxt_phase(uint32_t run) { return TN ? run & 1u : (run >> 1) & 1u; }
-
+// Tensor memory.  TN: one accumulator for the products with hi, from column 256 on one for the rest, which is taken out with the last run of an item.  NN:
+// two accumulators for all products, by turns.
 template <bool TN>
 __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
 {
@@ -254,26 +253,49 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
     uint32_t st = 0, ph = 0, run = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
-        for (int32_t k0 = 0; k0 < stages; k0 += MxtRun<TN>::stages, ++run) {
-            const uint32_t buf = mxt_buf<TN>(run), acc = s.tmem + 256u * buf;
-            if (!mxt_wait(&s.sh->acc_empty[buf], mxt_phase<TN>(run) ^ 1u, dead, a.status)) return;
-            const int32_t n = min(stages - k0, MxtRun<TN>::stages);
+        for (int32_t k0 = 0; k0 < stages; k0 += Mxt<TN>::run, ++run) {
+            const uint32_t buf = TN ? 0u : run & 1u, hi = s.tmem + 256u * buf, rest = TN ? s.tmem + 256u : hi;
+            const uint32_t taken = (TN ? run & 1u : (run >> 1) & 1u) ^ 1u;   // phase of acc_empty in which what was there before has been taken out
+            // (within an item, mid and lo go ahead while the hi accumulator is still being read)
+            const bool wait_late = TN && k0 > 0;
+            if (!wait_late && !mxt_wait(&s.sh->acc_empty[buf], taken, dead, a.status)) return;
+            const int32_t n = min(stages - k0, Mxt<TN>::run);
             for (int32_t k = 0; k < n; ++k) {
                 if (!mxt_wait(&s.sh->op_full[st], ph, dead, a.status)) return;
                 tc_fence_after();
                 const uint64_t q = q0 + (uint64_t)(st * (MXT_STAGE >> 4)), x = x0 + (uint64_t)(st * (MXT_STAGE >> 4));
-                if (elect_one()) {
+                if (!wait_late || k > 0) {
+                    if (elect_one()) {
 #pragma unroll
-                    for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {   // the tile of Q stays in the collector for its three products
-                        tc_mma_f16<1, 2>(acc, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, k > 0 || ks > 0 ? 1u : 0u);
-                        tc_mma_f16<3, 2>(acc, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
-                        tc_mma_f16<2, 2>(acc, q + ks * q_step, x + ks * x_step, idesc, 1u);
+                        for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {   // the tile of Q stays in the collector for its three products
+                            tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, (TN && k0 > 0) || k > 0 || ks > 0 ? 1u : 0u);
+                            tc_mma_f16<3, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
+                            tc_mma_f16<2, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, !TN || k > 0 || ks > 0 ? 1u : 0u);
+                        }
                     }
+                } else {
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {
+                            tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, 1u);
+                            tc_mma_f16<2, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
+                        }
+                    }
+                    __syncwarp();
+                    if (!mxt_wait(&s.sh->acc_empty[buf], taken, dead, a.status)) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) tc_mma_f16<0, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, ks > 0 ? 1u : 0u);
+                    }
+                }
+                __syncwarp();
+                if (elect_one()) {
                     tc_commit<2>(&s.sh->op_empty[st]);
                     if (k + 1 == n) tc_commit<2>(&s.sh->acc_full[buf]);
                 }
                 __syncwarp();
-                if (++st == MXT_GROUPS) st = 0, ph ^= 1u;
+                if (++st == MXT_SLOTS) st = 0, ph ^= 1u;
             }
         }
     }
@@ -305,7 +327,7 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
             const bool there = has_q && k + lane < it.k1;   // (else four zero bytes and nothing read)
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(s.sh->scales[st] + 4 * lane)), "l"(there ? scales : a.scales), "r"(there ? 4u : 0u) : "memory");
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-            if (++st == MXT_GROUPS) st = 0, ph ^= 1u;
+            if (++st == MXT_SLOTS) st = 0, ph ^= 1u;
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -315,25 +337,25 @@ template <bool TN, int FMT>
 __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
+    constexpr int32_t groups = Mxt<TN>::groups;
     const int32_t group = warp >> 2, w = warp & 3, half = a.bn / 2;
-    const uint32_t raw = smem_u32(s.raw) + (uint32_t)group * MXT_RAW_STAGE, op = smem_u32(s.op) + (uint32_t)group * MXT_STAGE;
-    // Per thread and stage: eight times four values of X and two times 16 elements of Q.
+    // Per thread and stage: eight times four values of X and two times 16 elements of Q (all places relative to the stage's).
     // TN: columns 4 lane .. of the terms w + 4 i; a warp reads a term's 512 bytes, half of it writes 128 of a block of 64 columns.
     // NN: terms 4 (lane % 8) .. of the rows 4 w + lane / 8 + 16 i; eight lanes read 128 bytes of a row and write its 64.
     const int32_t x_row = TN ? w : 4 * w + (lane >> 3), x_col = TN ? 4 * lane : 4 * (lane & 7);
     constexpr int32_t x_apart = TN ? 4 : 16;
-    const uint32_t x_raw = raw + (uint32_t)x_row * (TN ? (uint32_t)half * 4u : 128u) + (uint32_t)x_col * 4u;
     const uint32_t x_next = (uint32_t)x_apart * (TN ? (uint32_t)half * 4u : 128u);
-    const uint32_t x_op = op + MXT_Q_TILE + (TN ? (uint32_t)(lane >> 4) * (MXT_KB * 128) + (uint32_t)x_row * 128u + ((uint32_t)(((lane & 15) >> 1) ^ x_row) << 4)
-                                          : (uint32_t)x_row * 64u + ((uint32_t)(((lane & 7) >> 1) ^ ((x_row >> 1) & 3)) << 4)) + (uint32_t)(lane & 1) * 8u;
+    const uint32_t x_raw = smem_u32(s.raw) + (uint32_t)x_row * (TN ? (uint32_t)half * 4u : 128u) + (uint32_t)x_col * 4u;
+    const uint32_t x_op = smem_u32(s.op) + MXT_Q_TILE + (TN ? (uint32_t)(lane >> 4) * (MXT_KB * 128) + (uint32_t)x_row * 128u + ((uint32_t)(((lane & 15) >> 1) ^ x_row) << 4)
+                                                            : (uint32_t)x_row * 64u + ((uint32_t)(((lane & 7) >> 1) ^ ((x_row >> 1) & 3)) << 4)) + (uint32_t)(lane & 1) * 8u;
     // Q: elements 16 place .. of the terms term + 16 i.  Eight lanes write a term's two halves of 128 bytes: those of the second half its 16-byte pieces in
     // the other order, so that they meet no bank twice
     const int32_t place = lane & 7, term = 4 * w + (lane >> 3), other = place >> 2;
-    const uint32_t q_raw = raw + MXT_X_RAW + (uint32_t)(term * 128 + 16 * place) * FMT / 8, scales = smem_u32(s.sh->scales[group]) + 4u * (uint32_t)term + ((uint32_t)place >> 1);
-    const uint32_t q_op = op + (uint32_t)other * (MXT_KB * 128) + (uint32_t)term * 128u;
-    const uint32_t q_at = (uint32_t)((2 * (place & 3) + other) ^ (term & 7)) << 4;
+    const uint32_t q_raw = smem_u32(s.raw) + MXT_X_RAW + (uint32_t)(term * 128 + 16 * place) * FMT / 8;
+    const uint32_t scales = smem_u32(s.sh->scales[0]) + 4u * (uint32_t)term + ((uint32_t)place >> 1);
+    const uint32_t q_op = smem_u32(s.op) + (uint32_t)other * (MXT_KB * 128) + (uint32_t)term * 128u + ((uint32_t)((2 * (place & 3) + other) ^ (term & 7)) << 4);
 
-    uint32_t ph = 0, turn = 0;
+    uint32_t st = (uint32_t)group, ph = 0, turn = 0;
     int32_t base = 0;   // stages before this item, modulo the groups
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
@@ -341,153 +363,199 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         const bool sums = TN && a.colsum && it.d0 == 0, has_q = it.d0 + s.rank * 128 + 16 * place < a.D;
         // how many of this thread's rows there are (NN), or whether its columns are (TN)
         const int32_t end = min(half, a.N - x0), has_x = TN ? (x_col < end ? 8 : 0) : (x_row < end ? (end - 1 - x_row) / x_apart + 1 : 0);
-        float4 total = make_float4(0.f, 0.f, 0.f, 0.f);
+        float2 total[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
-        for (int32_t k = (group - base) & (MXT_GROUPS - 1); k < it.stages; k += MXT_GROUPS, ph ^= 1u) {
-            if (!mxt_wait(&s.sh->raw_full[group], ph, dead, a.status)) return;
-            float4 x[8];
-            uint32_t c[2][4], byte[2];
+        for (int32_t k = (group - base) & (groups - 1); k < it.stages; k += groups) {
+            if (!mxt_wait(&s.sh->raw_full[st], ph, dead, a.status)) return;
+            if (!mxt_wait(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
+            const uint32_t raw = st * MXT_RAW_STAGE, op = st * MXT_STAGE;
+            float4 x[4];   // four in flight
 #pragma unroll
-            for (int h = 0; h < 8; ++h)
-                if (h < has_x) x[h] = lds_f4(x_raw + h * x_next);
-            if (has_q)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    byte[h] = lds_u1(scales + 64 * h);
-                    if (FMT == SAT_MX8) {
-                        const uint4 t = lds_u4(q_raw + h * (16 * 128));
-                        c[h][0] = t.x, c[h][1] = t.y, c[h][2] = t.z, c[h][3] = t.w;
-                    } else {
-                        const uint2 t = lds_u2(q_raw + h * (16 * 64));
-                        c[h][0] = t.x, c[h][2] = t.y, c[h][1] = c[h][3] = 0u;
-                    }
-                }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->raw_empty[group]);
-            if (sums && has_x) {
-                total.x += ((x[0].x + x[1].x) + (x[2].x + x[3].x)) + ((x[4].x + x[5].x) + (x[6].x + x[7].x));
-                total.y += ((x[0].y + x[1].y) + (x[2].y + x[3].y)) + ((x[4].y + x[5].y) + (x[6].y + x[7].y));
-                total.z += ((x[0].z + x[1].z) + (x[2].z + x[3].z)) + ((x[4].z + x[5].z) + (x[6].z + x[7].z));
-                total.w += ((x[0].w + x[1].w) + (x[2].w + x[3].w)) + ((x[4].w + x[5].w) + (x[6].w + x[7].w));
-            }
-            if (!mxt_wait(&s.sh->op_empty[group], ph ^ 1u, dead, a.status)) return;
+            for (int h = 0; h < 4; ++h)
+                if (h < has_x) x[h] = lds_f4(x_raw + raw + h * x_next);
 #pragma unroll
             for (int h = 0; h < 8; ++h)
                 if (h < has_x) {
                     uint2 hi, mid, lo;
-                    mxt_split4(x[h], hi, mid, lo);
+                    const float4 v = x[h & 3];
+                    if (h + 4 < 8 && h + 4 < has_x) x[h & 3] = lds_f4(x_raw + raw + (h + 4) * x_next);
+                    mxt_split4(v, hi, mid, lo);
+                    if (sums) {
+                        total[0] = __fadd2_rn(total[0], make_float2(v.x, v.y));
+                        total[1] = __fadd2_rn(total[1], make_float2(v.z, v.w));
+                    }
                     // TN: the term four on has the other half of a row's swizzle
-                    const uint32_t o = TN ? (x_op ^ (uint32_t)((h & 1) << 6)) + h * 512 : x_op + h * 1024;
+                    const uint32_t o = op + (TN ? (x_op ^ (uint32_t)((h & 1) << 6)) + h * 512 : x_op + h * 1024);
                     sts_u2(o, hi);
                     sts_u2(o + MXT_X_PLANE, mid);
                     sts_u2(o + 2 * MXT_X_PLANE, lo);
                 }
-            if (has_q)
+            if (has_q) {
+                uint32_t c[2][4], byte[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    byte[h] = lds_u1(scales + st * MXT_SCALES + 64 * h);
+                    if (FMT == SAT_MX8) {
+                        const uint4 t = lds_u4(q_raw + raw + h * (16 * 128));
+                        c[h][0] = t.x, c[h][1] = t.y, c[h][2] = t.z, c[h][3] = t.w;
+                    } else {
+                        const uint2 t = lds_u2(q_raw + raw + h * (16 * 64));
+                        c[h][0] = t.x, c[h][2] = t.y, c[h][1] = c[h][3] = 0u;
+                    }
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const MxtScale<FMT> sc(byte[h]);
                     // the half that is written first: the upper one for lanes of the second block
-                    const uint32_t a0 = other ? c[h][2] : c[h][0], a1 = other ? c[h][3] : c[h][1], b0 = other ? c[h][0] : c[h][2], b1 = other ? c[h][1] : c[h][3];
-                    uint4 v0 = mxt_decode8<FMT>(a0, a1, sc), v1 = mxt_decode8<FMT>(b0, b1, sc);
+                    uint4 v0 = mxt_decode8<FMT>(other ? c[h][2] : c[h][0], other ? c[h][3] : c[h][1], sc), v1 = mxt_decode8<FMT>(other ? c[h][0] : c[h][2], other ? c[h][1] : c[h][3], sc);
                     if (sc.two) v0 = bf16x8_mul(v0, sc.second), v1 = bf16x8_mul(v1, sc.second);
-                    sts_u4(q_op + h * 2048 + q_at, v0);
-                    sts_u4(q_op + h * 2048 + (q_at ^ 16u), v1);
+                    sts_u4(q_op + op + h * 2048, v0);
+                    sts_u4((q_op ^ 16u) + op + h * 2048, v1);
                 }
+            }
             fence_async_smem();
-            mbar_arrive_warp<2>(&s.sh->op_full[group], lane);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
+            mbar_arrive_warp<2>(&s.sh->op_full[st], lane);
+            if ((st += groups) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
         }
         base += it.stages;
-        if (sums) {   // the sixteen warps' sums of a column are added up by the warp that writes them
+        if (sums) {   // the warps' sums of a column are added up by the warp that writes them
             if (!mxt_wait(&s.sh->sums_empty, (turn & 1u) ^ 1u, dead, a.status)) return;
-            *reinterpret_cast<float4 *>(s.sh->sums[warp] + 4 * lane) = total;
+            *reinterpret_cast<float4 *>(s.sh->sums[warp] + 4 * lane) = make_float4(total[0].x, total[0].y, total[1].x, total[1].y);
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->sums_full);
             ++turn;
         }
     }
     // the pair's MMAs have signalled this group's stages: nothing arrives here any more once both CTAs may exit
-    (void)mxt_wait(&s.sh->op_empty[group], ph ^ 1u, dead, a.status);
+    for (int h = 0; h < MXT_SLOTS; h += groups) {
+        if (!mxt_wait(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
+        if ((st += groups) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
+    }
 }
 
-// A lane has a column of Q, a register a column or row of X: consecutive lanes write consecutive floats.  Without a sum in tensor memory (NN) runs behind
-// the first of an item are added to what that one wrote.
-template <bool TN>
+// (TN) Adds up the runs: a lane has a column of Q, a register a column of X.  Eight warps, two to a quarter of the lanes, with half the columns each.
+__device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int warp, int lane)
+{
+    volatile int *dead = &s.sh->dead;
+    const int32_t c0 = (warp >> 2) * 128, chunks = min(4, (a.bn - c0 + 31) / 32);
+    const uint32_t lanes = s.tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c0;
+    uint32_t run = 0;
+    float acc[128];
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
+        const int32_t stages = mxt_item(a, i).stages;
+#pragma unroll
+        for (int e = 0; e < 128; ++e) acc[e] = 0.f;
+        for (int32_t k0 = 0; k0 < stages; k0 += Mxt<true>::run, ++run) {
+            if (!mxt_wait<50>(&s.sh->acc_full[0], run & 1u, dead, a.status)) return;
+            tc_fence_after();
+            const bool last = k0 + Mxt<true>::run >= stages;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c < 2 * chunks) {
+                    uint32_t r[16];
+                    tc_ld16(lanes + 16u * c, r);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[16 * c + e] += __uint_as_float(r[e]);
+                    if (last) {
+                        tc_ld16(lanes + 256u + 16u * c, r);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[16 * c + e] += __uint_as_float(r[e]);
+                    }
+                }
+            tc_fence_before();
+            mbar_arrive_warp<2>(&s.sh->acc_empty[0], lane);
+        }
+        const MxtItem it = mxt_item(a, i);
+        const int32_t col = it.d0 + s.rank * 128 + (warp & 3) * 32 + lane, n = min(a.bn, a.N - it.n0) - c0;
+        float *o = a.C + it.split * a.split + (it.n0 + c0) * a.by_x + col * a.by_q;
+        if (col < a.D) {
+#pragma unroll
+            for (int e = 0; e < 128; ++e, o += a.by_x)
+                if (e < n) *o = a.add ? *o + acc[e] : acc[e];
+        }
+    }
+}
+
+// (TN) The column sums of an item
+__device__ __forceinline__ void mxt_totals(const MxtArgs &a, const MxtMem &s, int lane)
+{
+    const int32_t half = a.bn / 2;
+    uint32_t turn = 0;
+    for (int32_t i = s.unit; i < a.items; i += s.units) {
+        const MxtItem it = mxt_item(a, i);
+        if (it.d0 != 0) continue;
+        if (!mxt_wait<200>(&s.sh->sums_full, turn & 1u, &s.sh->dead, a.status)) return;
+        for (int32_t c = lane; c < half; c += 32) {
+            double sum = 0.;
+            for (int h = 0; h < Mxt<true>::workers; ++h) sum += (double)s.sh->sums[h][c];
+            const int32_t at = it.n0 + s.rank * half + c;
+            if (at >= a.N) continue;
+            float *out = a.colsum + (int64_t)it.split * a.N + at;
+            *out = a.add ? (float)((double)*out + sum) : (float)sum;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.sh->sums_empty);
+        ++turn;
+    }
+}
+
+// (NN) A lane has a column of Q, a register a row of X: consecutive lanes write consecutive floats.  Runs behind the first of an item are added to what
+// that one wrote.
 __device__ __forceinline__ void mxt_results(const MxtArgs &a, const MxtMem &s, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
     const uint32_t lanes = s.tmem + ((uint32_t)(warp * 32) << 16);
-    uint32_t run = 0, turn = 0;
+    uint32_t run = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         const int32_t col = it.d0 + s.rank * 128 + warp * 32 + lane, n = min(a.bn, a.N - it.n0);
-        for (int32_t k0 = 0; k0 < it.stages; k0 += MxtRun<TN>::stages, ++run) {
-            const uint32_t buf = mxt_buf<TN>(run);
-            const bool write = !TN || k0 + MxtRun<TN>::stages >= it.stages, add = a.add || (!TN && k0 > 0);
-            if (!mxt_wait<100>(&s.sh->acc_full[buf], mxt_phase<TN>(run), dead, a.status)) return;
+        for (int32_t k0 = 0; k0 < it.stages; k0 += Mxt<false>::run, ++run) {
+            const uint32_t buf = run & 1u;
+            if (!mxt_wait<100>(&s.sh->acc_full[buf], (run >> 1) & 1u, dead, a.status)) return;
             tc_fence_after();
-            float *o = a.C + it.split * a.split + it.n0 * a.by_x + col * a.by_q;
+            float *o = a.C + it.n0 * a.by_x + col;
             for (int32_t c = 0; c < a.bn; c += 16) {
-                uint32_t r[16], t[16];
+                uint32_t r[16];
                 tc_ld16(lanes + 256u * buf + (uint32_t)c, r);
-                if (TN && k0 > 0) tc_ld16(lanes + MXT_SUM + (uint32_t)c, t);
                 tc_wait_ld();
                 if (c + 16 >= a.bn) {   // the accumulator has been read
                     tc_fence_before();
                     mbar_arrive_warp<2>(&s.sh->acc_empty[buf], lane);
                 }
-                if (TN && k0 > 0) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + __uint_as_float(t[e]));
-                }
-                if (!write) {
-                    tc_st16(lanes + MXT_SUM + (uint32_t)c, r);
-                    continue;
-                }
                 if (col >= a.D) continue;
-                if (c + 16 <= n && !add) {
+                if (c + 16 <= n && k0 == 0) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e, o += a.by_x) *o = __uint_as_float(r[e]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e, o += a.by_x)
-                        if (c + e < n) *o = add ? *o + __uint_as_float(r[e]) : __uint_as_float(r[e]);
+                        if (c + e < n) *o = k0 > 0 ? *o + __uint_as_float(r[e]) : __uint_as_float(r[e]);
                 }
             }
-            if (!write) tc_wait_st();
-        }
-        if (TN && a.colsum && it.d0 == 0 && warp == 0) {
-            if (!mxt_wait(&s.sh->sums_full, turn & 1u, dead, a.status)) return;
-            for (int32_t c = lane; c < a.bn / 2; c += 32) {
-                double sum = 0.;
-                for (int h = 0; h < 4 * MXT_GROUPS; ++h) sum += (double)s.sh->sums[h][c];
-                const int32_t at = it.n0 + s.rank * (a.bn / 2) + c;
-                if (at >= a.N) continue;
-                float *out = a.colsum + (int64_t)it.split * a.N + at;
-                *out = a.add ? (float)((double)*out + sum) : (float)sum;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sh->sums_empty);
-            ++turn;
         }
     }
 }
 
 template <bool TN, int FMT>
-__global__ void __launch_bounds__(MXT_THREADS, 1)
+__global__ void __launch_bounds__(Mxt<TN>::threads, 1)
 k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ MxtArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     MxtMem s;
     s.op = smem;
-    s.raw = smem + MXT_GROUPS * MXT_STAGE;
-    s.sh = (MxtShared *)(s.raw + MXT_GROUPS * MXT_RAW_STAGE);
+    s.raw = smem + MXT_SLOTS * MXT_STAGE;
+    s.sh = (MxtShared *)(s.raw + MXT_SLOTS * MXT_RAW_STAGE);
     s.rank = (int32_t)(blockIdx.x & 1u);
     s.unit = (int32_t)(blockIdx.x >> 1);
     s.units = (int32_t)(gridDim.x >> 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < MXT_GROUPS; ++i) {
+        for (int i = 0; i < MXT_SLOTS; ++i) {
             mbar_init(&s.sh->raw_full[i], 1 + 32);   // the TMA's issuer and the scales' lanes
             mbar_init(&s.sh->raw_empty[i], 4);
             mbar_init(&s.sh->op_full[i], 2 * 4);     // a group of either CTA
@@ -495,29 +563,44 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.sh->acc_full[i], 1);
-            mbar_init(&s.sh->acc_empty[i], 2 * 4);
+            mbar_init(&s.sh->acc_empty[i], 2 * Mxt<TN>::takers);
         }
-        mbar_init(&s.sh->sums_full, 4 * MXT_GROUPS);
+        mbar_init(&s.sh->sums_full, Mxt<TN>::workers);
         mbar_init(&s.sh->sums_empty, 1);
         s.sh->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == MXT_EPILOGUE + 4) tc_alloc<2>(&s.sh->tmem_base, 512u);
+    if (warp == Mxt<TN>::mma) tc_alloc<2>(&s.sh->tmem_base, 512u);
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // the other CTA's barriers are initialised and its TMEM is allocated
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
     sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
-    if (warp < MXT_EPILOGUE) mxt_work<TN, FMT>(a, s, warp, lane);
-    else if (warp < MXT_EPILOGUE + 4) mxt_results<TN>(a, s, warp - MXT_EPILOGUE, lane);
-    else if (warp > MXT_EPILOGUE + 4) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
-    else if (s.rank == 0) mxt_mma<TN>(a, s);
+    // TN: 640 threads start with 96 registers each; the two warpgroups that add up the runs, 128 sums a thread, go to 152, the converters' two to 72 and the
+    // fifth one to 32: 2 x 152 + 2 x 72 + 32 = 5 x 96
+    if (warp < Mxt<TN>::workers) {
+        if (TN) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        mxt_work<TN, FMT>(a, s, warp, lane);
+    } else if (warp < Mxt<TN>::mma) {
+        if (TN) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+            mxt_runs(a, s, warp - Mxt<TN>::workers, lane);
+        } else {
+            mxt_results(a, s, warp - Mxt<TN>::workers, lane);
+        }
+    } else {
+        if (TN) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if (warp == Mxt<TN>::mma) {
+            if (s.rank == 0) mxt_mma<TN>(a, s);
+        } else if (warp == Mxt<TN>::mma + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
+        else if (TN && warp == Mxt<TN>::mma + 2 && a.colsum) mxt_totals(a, s, lane);
+    }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // neither CTA's shared memory or TMEM is in use by the other any more
-    if (warp == MXT_EPILOGUE + 4) {
+    if (warp == Mxt<TN>::mma) {
         tc_fence_after();
         tc_dealloc<2>(s.tmem, 512u);
     }
@@ -567,7 +650,7 @@ static sat_status mxt_launch(sat_ctx *ctx, const CUtensorMap &map_x, const CUten
         SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_gemm<TN, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MXT_SMEM));
         attr.mark(ctx->device);
     }
-    sat_pdl(ctx->stream, k_mx_gemm<TN, FMT>, 2u * (unsigned)std::min(a.items, ctx->sms / 2), MXT_THREADS, MXT_SMEM, 2)(map_x, map_q, a);
+    sat_pdl(ctx->stream, k_mx_gemm<TN, FMT>, 2u * (unsigned)std::min(a.items, ctx->sms / 2), Mxt<TN>::threads, MXT_SMEM, 2)(map_x, map_q, a);
     SAT_LAUNCHED(ctx);
     return SAT_OK;
 }
