@@ -315,7 +315,7 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
         const uint32_t bytes = (has_x ? (uint32_t)half * 128u : 0u) + (has_q ? 128u * MXT_KB * FMT / 8 : 0u);
         const uint8_t *scales = a.scales + (int64_t)(it.k0 + lane) * a.ld_scales + q0 / MX_GROUP;   // four bytes, of which some may lie behind the row's last
         for (int32_t k = it.k0; k < it.k1; k += MXT_KB, scales += MXT_KB * a.ld_scales) {
-            if (!mxt_wait<40>(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
+            if (!mxt_wait<100>(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
             uint64_t *bar = &s.sh->raw_full[st];
             if (lane == 0) {
                 uint8_t *x = s.raw + st * MXT_RAW_STAGE;
@@ -366,8 +366,8 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         float2 total[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
         for (int32_t k = (group - base) & (groups - 1); k < it.stages; k += groups) {
-            if (!mxt_wait(&s.sh->raw_full[st], ph, dead, a.status)) return;
-            if (!mxt_wait(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
+            if (!mxt_wait<20>(&s.sh->raw_full[st], ph, dead, a.status)) return;
+            if (!mxt_wait<20>(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
             const uint32_t raw = st * MXT_RAW_STAGE, op = st * MXT_STAGE;
             float4 x[4];   // four in flight
 #pragma unroll
@@ -448,7 +448,7 @@ __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int 
 #pragma unroll
         for (int e = 0; e < 128; ++e) acc[e] = 0.f;
         for (int32_t k0 = 0; k0 < stages; k0 += Mxt<true>::run, ++run) {
-            if (!mxt_wait<50>(&s.sh->acc_full[0], run & 1u, dead, a.status)) return;
+            if (!mxt_wait<250>(&s.sh->acc_full[0], run & 1u, dead, a.status)) return;
             tc_fence_after();
             const bool last = k0 + Mxt<true>::run >= stages;
 #pragma unroll
@@ -488,7 +488,7 @@ __device__ __forceinline__ void mxt_totals(const MxtArgs &a, const MxtMem &s, in
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         if (it.d0 != 0) continue;
-        if (!mxt_wait<200>(&s.sh->sums_full, turn & 1u, &s.sh->dead, a.status)) return;
+        if (!mxt_wait<1000>(&s.sh->sums_full, turn & 1u, &s.sh->dead, a.status)) return;
         for (int32_t c = lane; c < half; c += 32) {
             double sum = 0.;
             for (int h = 0; h < Mxt<true>::workers; ++h) sum += (double)s.sh->sums[h][c];
@@ -515,7 +515,7 @@ __device__ __forceinline__ void mxt_results(const MxtArgs &a, const MxtMem &s, i
         const int32_t col = it.d0 + s.rank * 128 + warp * 32 + lane, n = min(a.bn, a.N - it.n0);
         for (int32_t k0 = 0; k0 < it.stages; k0 += Mxt<false>::run, ++run) {
             const uint32_t buf = run & 1u;
-            if (!mxt_wait<100>(&s.sh->acc_full[buf], (run >> 1) & 1u, dead, a.status)) return;
+            if (!mxt_wait<250>(&s.sh->acc_full[buf], (run >> 1) & 1u, dead, a.status)) return;
             tc_fence_after();
             float *o = a.C + it.n0 * a.by_x + col;
             for (int32_t c = 0; c < a.bn; c += 16) {
