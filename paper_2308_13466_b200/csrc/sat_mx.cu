@@ -149,6 +149,7 @@ k_mx_quantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, in
         float4 v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float4 *>(mine + slot * MXB_BOX + t * 128 + ((i ^ (t & 7)) << 4));
+        fence_async_smem();   // these loads are done before the TMA writes there again (a barrier alone lets it overtake them)
         mxb_sync(wg);
         load((int)slot, b + MXB_SLOTS * step);
         if (++slot == MXB_SLOTS) slot = 0, ph ^= 1u;

@@ -180,6 +180,7 @@ __device__ __forceinline__ void nt_rows(const NtArgs &p, const NtMem &s, int war
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float4 *>(x + ((i ^ (row & 7)) << 4));
                 byte = mx_quantise32<SAT_MX4>(v, c);
+                fence_async_smem();   // the loads are done before the TMA writes there again (an arrival alone lets it overtake them)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s.sh->raw_empty[g][slot]);
                 if (++slot == NT_RAW) slot = 0, rph ^= 1u;

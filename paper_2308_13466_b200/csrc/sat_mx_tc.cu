@@ -6,9 +6,8 @@
 // kind::f16 with bf16 operands then give exact products, and all that is rounded is the sum.
 //
 // The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts: 612257 terms in 74
-// splits were off by 1e-5 of the result.  Only the products with hi matter for that; with TN those with mid and lo, 2^-8 of them, have an accumulator of
-// their own, and the one of hi is taken out every 12 stages (24 instructions) and added up in registers, rounded to nearest: 5e-7, an fp32 FMA loop's
-// being 1e-6.  NN has a few hundred terms, which one accumulator takes (1e-7).
+// splits were off by 1e-5 of the result.  Only the products with hi matter for that; those with mid and lo, 2^-8 of them, have an accumulator of their own,
+// and the one of hi is taken out every 12 stages (24 instructions; NN: 16) and added up in registers, rounded to nearest: 5e-7, an fp32 FMA loop's being 1e-6.
 //
 // A pair of CTAs shares a tile of 256 columns of Q (the M side, 128 lanes of TMEM in either CTA) by up to 256 columns (TN) or rows (NN) of
 // X.  What bounds it besides memory is shared memory, at 128 bytes a clock: per stage of 32 terms a CTA takes in 16 KB of X and 4 KB of codes
@@ -16,8 +15,12 @@
 // stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  (With single CTAs and X as the M side it
 // was 183 KB for as many products.  Loading straight into registers takes 40 KB less, but what it can keep in flight does not cover the latency.)
 //
-// Groups of four warps convert stages in turn; others take results out of the accumulators, and with TN hold the sums of the runs; one warp, of the
-// first CTA, issues the MMAs, one the loads, and with TN one adds up the column sums that the converters made on the way.
+// (For NN, one accumulator of all three products, two of them by turns, taken out by four warps that write at once: 90000 x 512 x 512 108 us instead of 128, but
+// 96 chopped additions, 1.3e-6.)
+//
+// Two groups of four warps convert stages in turn; eight warps take the accumulators out and hold the sums of the runs (converters that held them as well had no
+// registers left to work with); one, of the first CTA, issues the MMAs, one the loads, and with TN one adds up the column sums that the converters made on the
+// way.
 #include "sat_mx.h"
 #include "sat_ptx.h"
 
@@ -32,19 +35,20 @@
 #define MXT_Q_RAW (128 * MXT_KB)
 #define MXT_RAW_STAGE (MXT_X_RAW + MXT_Q_RAW)
 #define MXT_SCALES (MXT_KB * 4)       /* of a stage: four groups a term */
-// groups: of four converting warps, a divisor of the slots; run: stages that are added up in an accumulator; takers: warps that take results out, the first
-// behind the converters; then the one that issues the MMAs, the one that loads, and (TN) the one with the column sums
-template <bool TN> struct Mxt;
-template <> struct Mxt<true> { static constexpr int32_t groups = 2, run = 12, takers = 8, workers = 4 * groups, mma = workers + takers, threads = 20 * 32; };
-template <> struct Mxt<false> { static constexpr int32_t groups = 4, run = 16, takers = 4, workers = 4 * groups, mma = workers + takers, threads = (mma + 2) * 32; };
+#define MXT_GROUPS 2                 /* groups of four converting warps, a divisor of the slots */
+template <bool TN> constexpr int32_t MXT_RUN = TN ? 12 : 16;   /* stages between two reads of the hi accumulator: 24 instructions, or 32 (one read for 512 terms) */
+#define MXT_WORKERS (4 * MXT_GROUPS)
+#define MXT_TAKERS 8                 /* warps that add up the runs, behind the converters; then one for the MMAs, for the loads, for the column sums */
+#define MXT_MMA (MXT_WORKERS + MXT_TAKERS)
+#define MXT_THREADS ((MXT_MMA + 4) * 32)
 
 struct MxtShared {
-    float sums[Mxt<true>::workers][128];
+    float sums[MXT_WORKERS][128];
     uint64_t sums_full, sums_empty;
     uint8_t scales[MXT_SLOTS][MXT_SCALES];
     uint64_t raw_full[MXT_SLOTS], raw_empty[MXT_SLOTS];   // TMA bytes and scales have landed; the group has read them
     uint64_t op_full[MXT_SLOTS], op_empty[MXT_SLOTS];     // (first CTA) both CTAs' groups have written the tiles; the MMAs have read them
-    uint64_t acc_full[2], acc_empty[2];                     // an accumulator holds a run; (first CTA) both CTAs have taken it out
+    uint64_t acc_full, acc_empty;                           // the hi accumulator holds a run; (first CTA) both CTAs have taken it out
     uint32_t tmem_base;
     int dead;
 };
@@ -238,8 +242,7 @@ struct MxtMem {
     int32_t rank;              // CTA of the pair
     int32_t unit, units;       // pair, and pairs
 };
-// Tensor memory.  TN: one accumulator for the products with hi, from column 256 on one for the rest, which is taken out with the last run of an item.  NN:
-// two accumulators for all products, by turns.
+// Tensor memory: the accumulator of the products with hi, from column 256 on that of the rest, which is taken out with the last run of an item
 template <bool TN>
 __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
 {
@@ -253,13 +256,11 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
     uint32_t st = 0, ph = 0, run = 0;
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
-        for (int32_t k0 = 0; k0 < stages; k0 += Mxt<TN>::run, ++run) {
-            const uint32_t buf = TN ? 0u : run & 1u, hi = s.tmem + 256u * buf, rest = TN ? s.tmem + 256u : hi;
-            const uint32_t taken = (TN ? run & 1u : (run >> 1) & 1u) ^ 1u;   // phase of acc_empty in which what was there before has been taken out
-            // (within an item, mid and lo go ahead while the hi accumulator is still being read)
-            const bool wait_late = TN && k0 > 0;
-            if (!wait_late && !mxt_wait(&s.sh->acc_empty[buf], taken, dead, a.status)) return;
-            const int32_t n = min(stages - k0, Mxt<TN>::run);
+        for (int32_t k0 = 0; k0 < stages; k0 += MXT_RUN<TN>, ++run) {
+            const uint32_t hi = s.tmem, rest = s.tmem + 256u, taken = (run & 1u) ^ 1u;   // phase of acc_empty in which what was there before has been taken out
+            const bool wait_late = k0 > 0;   // within an item, mid and lo go ahead while the hi accumulator is still being read
+            if (!wait_late && !mxt_wait(&s.sh->acc_empty, taken, dead, a.status)) return;
+            const int32_t n = min(stages - k0, MXT_RUN<TN>);
             for (int32_t k = 0; k < n; ++k) {
                 if (!mxt_wait(&s.sh->op_full[st], ph, dead, a.status)) return;
                 tc_fence_after();
@@ -268,9 +269,9 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
                     if (elect_one()) {
 #pragma unroll
                         for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {   // the tile of Q stays in the collector for its three products
-                            tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, (TN && k0 > 0) || k > 0 || ks > 0 ? 1u : 0u);
+                            tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, k0 > 0 || k > 0 || ks > 0 ? 1u : 0u);
                             tc_mma_f16<3, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
-                            tc_mma_f16<2, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, !TN || k > 0 || ks > 0 ? 1u : 0u);
+                            tc_mma_f16<2, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, k > 0 || ks > 0 ? 1u : 0u);
                         }
                     }
                 } else {
@@ -282,7 +283,7 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
                         }
                     }
                     __syncwarp();
-                    if (!mxt_wait(&s.sh->acc_empty[buf], taken, dead, a.status)) return;
+                    if (!mxt_wait(&s.sh->acc_empty, taken, dead, a.status)) return;
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
@@ -292,7 +293,7 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
                 __syncwarp();
                 if (elect_one()) {
                     tc_commit<2>(&s.sh->op_empty[st]);
-                    if (k + 1 == n) tc_commit<2>(&s.sh->acc_full[buf]);
+                    if (k + 1 == n) tc_commit<2>(&s.sh->acc_full);
                 }
                 __syncwarp();
                 if (++st == MXT_SLOTS) st = 0, ph ^= 1u;
@@ -337,7 +338,6 @@ template <bool TN, int FMT>
 __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    constexpr int32_t groups = Mxt<TN>::groups;
     const int32_t group = warp >> 2, w = warp & 3, half = a.bn / 2;
     // Per thread and stage: eight times four values of X and two times 16 elements of Q (all places relative to the stage's).
     // TN: columns 4 lane .. of the terms w + 4 i; a warp reads a term's 512 bytes, half of it writes 128 of a block of 64 columns.
@@ -365,7 +365,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         const int32_t end = min(half, a.N - x0), has_x = TN ? (x_col < end ? 8 : 0) : (x_row < end ? (end - 1 - x_row) / x_apart + 1 : 0);
         float2 total[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
-        for (int32_t k = (group - base) & (groups - 1); k < it.stages; k += groups) {
+        for (int32_t k = (group - base) & (MXT_GROUPS - 1); k < it.stages; k += MXT_GROUPS) {
             if (!mxt_wait<20>(&s.sh->raw_full[st], ph, dead, a.status)) return;
             if (!mxt_wait<20>(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
             const uint32_t raw = st * MXT_RAW_STAGE, op = st * MXT_STAGE;
@@ -417,7 +417,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
             mbar_arrive_warp<2>(&s.sh->op_full[st], lane);
-            if ((st += groups) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
+            if ((st += MXT_GROUPS) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
         }
         base += it.stages;
         if (sums) {   // the warps' sums of a column are added up by the warp that writes them
@@ -429,53 +429,62 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         }
     }
     // the pair's MMAs have signalled this group's stages: nothing arrives here any more once both CTAs may exit
-    for (int h = 0; h < MXT_SLOTS; h += groups) {
+    for (int h = 0; h < MXT_SLOTS; h += MXT_GROUPS) {
         if (!mxt_wait(&s.sh->op_empty[st], ph ^ 1u, dead, a.status)) return;
-        if ((st += groups) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
+        if ((st += MXT_GROUPS) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
     }
 }
 
-// (TN) Adds up the runs: a lane has a column of Q, a register a column of X.  Eight warps, two to a quarter of the lanes, with half the columns each.
+// Adds up the runs: a lane has a column of Q, a register a column or row of X, so that consecutive lanes write consecutive floats.  Eight warps, two to a
+// quarter of the lanes, with half the columns each.
+template <bool TN>
 __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int warp, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    const int32_t c0 = (warp >> 2) * 128, chunks = min(4, (a.bn - c0 + 31) / 32);
+    const int32_t c0 = (warp >> 2) * 128, here = min(8, (a.bn - c0) / 16);   // 16 columns at a time
     const uint32_t lanes = s.tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c0;
     uint32_t run = 0;
-    float acc[128];
+    uint32_t acc[128];   // bits of the sums
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
-#pragma unroll
-        for (int e = 0; e < 128; ++e) acc[e] = 0.f;
-        for (int32_t k0 = 0; k0 < stages; k0 += Mxt<true>::run, ++run) {
-            if (!mxt_wait<250>(&s.sh->acc_full[0], run & 1u, dead, a.status)) return;
+#pragma unroll 1
+        for (int32_t k0 = 0; k0 < stages; k0 += MXT_RUN<TN>, ++run) {
+            if (!mxt_wait<250>(&s.sh->acc_full, run & 1u, dead, a.status)) return;
             tc_fence_after();
-            const bool last = k0 + Mxt<true>::run >= stages;
+            const bool last = k0 + MXT_RUN<TN> >= stages;
+            if (k0 == 0) {   // straight to where it stays
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-                if (c < 2 * chunks) {
-                    uint32_t r[16];
-                    tc_ld16(lanes + 16u * c, r);
-                    tc_wait_ld();
+                for (int c = 0; c < 8; ++c)
+                    if (c < here) tc_ld16(lanes + 16u * c, acc + 16 * c);
+                tc_wait_ld();
+            }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[16 * c + e] += __uint_as_float(r[e]);
-                    if (last) {
-                        tc_ld16(lanes + 256u + 16u * c, r);
-                        tc_wait_ld();
+            for (int half = 0; half < 2; ++half)   // the run, then the rest
+                if (half ? last : k0 > 0) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[16 * c + e] += __uint_as_float(r[e]);
-                    }
+                    for (int c = 0; c < 8; ++c)
+                        if (c < here) {
+                            uint32_t r[16];
+                            tc_ld16(lanes + 256u * half + 16u * c, r);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) acc[16 * c + e] = __float_as_uint(__uint_as_float(acc[16 * c + e]) + __uint_as_float(r[e]));
+                        }
                 }
             tc_fence_before();
-            mbar_arrive_warp<2>(&s.sh->acc_empty[0], lane);
+            mbar_arrive_warp<2>(&s.sh->acc_empty, lane);
         }
         const MxtItem it = mxt_item(a, i);
         const int32_t col = it.d0 + s.rank * 128 + (warp & 3) * 32 + lane, n = min(a.bn, a.N - it.n0) - c0;
         float *o = a.C + it.split * a.split + (it.n0 + c0) * a.by_x + col * a.by_q;
-        if (col < a.D) {
+        if (col >= a.D) continue;
+        if (n >= 128 && !a.add) {
+#pragma unroll
+            for (int e = 0; e < 128; ++e, o += a.by_x) *o = __uint_as_float(acc[e]);
+        } else {
 #pragma unroll
             for (int e = 0; e < 128; ++e, o += a.by_x)
-                if (e < n) *o = a.add ? *o + acc[e] : acc[e];
+                if (e < n) *o = a.add ? *o + __uint_as_float(acc[e]) : __uint_as_float(acc[e]);
         }
     }
 }
@@ -491,7 +500,7 @@ __device__ __forceinline__ void mxt_totals(const MxtArgs &a, const MxtMem &s, in
         if (!mxt_wait<1000>(&s.sh->sums_full, turn & 1u, &s.sh->dead, a.status)) return;
         for (int32_t c = lane; c < half; c += 32) {
             double sum = 0.;
-            for (int h = 0; h < Mxt<true>::workers; ++h) sum += (double)s.sh->sums[h][c];
+            for (int h = 0; h < MXT_WORKERS; ++h) sum += (double)s.sh->sums[h][c];
             const int32_t at = it.n0 + s.rank * half + c;
             if (at >= a.N) continue;
             float *out = a.colsum + (int64_t)it.split * a.N + at;
@@ -503,45 +512,8 @@ __device__ __forceinline__ void mxt_totals(const MxtArgs &a, const MxtMem &s, in
     }
 }
 
-// (NN) A lane has a column of Q, a register a row of X: consecutive lanes write consecutive floats.  Runs behind the first of an item are added to what
-// that one wrote.
-__device__ __forceinline__ void mxt_results(const MxtArgs &a, const MxtMem &s, int warp, int lane)
-{
-    volatile int *dead = &s.sh->dead;
-    const uint32_t lanes = s.tmem + ((uint32_t)(warp * 32) << 16);
-    uint32_t run = 0;
-    for (int32_t i = s.unit; i < a.items; i += s.units) {
-        const MxtItem it = mxt_item(a, i);
-        const int32_t col = it.d0 + s.rank * 128 + warp * 32 + lane, n = min(a.bn, a.N - it.n0);
-        for (int32_t k0 = 0; k0 < it.stages; k0 += Mxt<false>::run, ++run) {
-            const uint32_t buf = run & 1u;
-            if (!mxt_wait<250>(&s.sh->acc_full[buf], (run >> 1) & 1u, dead, a.status)) return;
-            tc_fence_after();
-            float *o = a.C + it.n0 * a.by_x + col;
-            for (int32_t c = 0; c < a.bn; c += 16) {
-                uint32_t r[16];
-                tc_ld16(lanes + 256u * buf + (uint32_t)c, r);
-                tc_wait_ld();
-                if (c + 16 >= a.bn) {   // the accumulator has been read
-                    tc_fence_before();
-                    mbar_arrive_warp<2>(&s.sh->acc_empty[buf], lane);
-                }
-                if (col >= a.D) continue;
-                if (c + 16 <= n && k0 == 0) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e, o += a.by_x) *o = __uint_as_float(r[e]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e, o += a.by_x)
-                        if (c + e < n) *o = k0 > 0 ? *o + __uint_as_float(r[e]) : __uint_as_float(r[e]);
-                }
-            }
-        }
-    }
-}
-
 template <bool TN, int FMT>
-__global__ void __launch_bounds__(Mxt<TN>::threads, 1)
+__global__ void __launch_bounds__(MXT_THREADS, 1)
 k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ MxtArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -561,46 +533,40 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
             mbar_init(&s.sh->op_full[i], 2 * 4);     // a group of either CTA
             mbar_init(&s.sh->op_empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&s.sh->acc_full[i], 1);
-            mbar_init(&s.sh->acc_empty[i], 2 * Mxt<TN>::takers);
-        }
-        mbar_init(&s.sh->sums_full, Mxt<TN>::workers);
+        mbar_init(&s.sh->acc_full, 1);
+        mbar_init(&s.sh->acc_empty, 2 * MXT_TAKERS);
+        mbar_init(&s.sh->sums_full, MXT_WORKERS);
         mbar_init(&s.sh->sums_empty, 1);
         s.sh->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == Mxt<TN>::mma) tc_alloc<2>(&s.sh->tmem_base, 512u);
+    if (warp == MXT_MMA) tc_alloc<2>(&s.sh->tmem_base, 512u);
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // the other CTA's barriers are initialised and its TMEM is allocated
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
     sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
-    // TN: 640 threads start with 96 registers each; the two warpgroups that add up the runs, 128 sums a thread, go to 152, the converters' two to 72 and the
-    // fifth one to 32: 2 x 152 + 2 x 72 + 32 = 5 x 96
-    if (warp < Mxt<TN>::workers) {
-        if (TN) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // 640 threads start with 96 registers each; the two warpgroups that add up the runs, 128 sums a thread, go to 152, the converters' two to 72 and the fifth
+    // one to 32: 2 x 152 + 2 x 72 + 32 = 5 x 96
+    if (warp < MXT_WORKERS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         mxt_work<TN, FMT>(a, s, warp, lane);
-    } else if (warp < Mxt<TN>::mma) {
-        if (TN) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
-            mxt_runs(a, s, warp - Mxt<TN>::workers, lane);
-        } else {
-            mxt_results(a, s, warp - Mxt<TN>::workers, lane);
-        }
+    } else if (warp < MXT_MMA) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+        mxt_runs<TN>(a, s, warp - MXT_WORKERS, lane);
     } else {
-        if (TN) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-        if (warp == Mxt<TN>::mma) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if (warp == MXT_MMA) {
             if (s.rank == 0) mxt_mma<TN>(a, s);
-        } else if (warp == Mxt<TN>::mma + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
-        else if (TN && warp == Mxt<TN>::mma + 2 && a.colsum) mxt_totals(a, s, lane);
+        } else if (warp == MXT_MMA + 1) mxt_load<TN, FMT>(a, s, &map_x, &map_q, lane);
+        else if (TN && warp == MXT_MMA + 2 && a.colsum) mxt_totals(a, s, lane);
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // neither CTA's shared memory or TMEM is in use by the other any more
-    if (warp == Mxt<TN>::mma) {
+    if (warp == MXT_MMA) {
         tc_fence_after();
         tc_dealloc<2>(s.tmem, 512u);
     }
@@ -650,7 +616,7 @@ static sat_status mxt_launch(sat_ctx *ctx, const CUtensorMap &map_x, const CUten
         SAT_CUDA(ctx, cudaFuncSetAttribute(k_mx_gemm<TN, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MXT_SMEM));
         attr.mark(ctx->device);
     }
-    sat_pdl(ctx->stream, k_mx_gemm<TN, FMT>, 2u * (unsigned)std::min(a.items, ctx->sms / 2), Mxt<TN>::threads, MXT_SMEM, 2)(map_x, map_q, a);
+    sat_pdl(ctx->stream, k_mx_gemm<TN, FMT>, 2u * (unsigned)std::min(a.items, ctx->sms / 2), MXT_THREADS, MXT_SMEM, 2)(map_x, map_q, a);
     SAT_LAUNCHED(ctx);
     return SAT_OK;
 }

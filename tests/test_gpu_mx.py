@@ -159,6 +159,54 @@ def test_places_beyond_32_bits(B, ctx):
     assert not bool(x[:-100].any())
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows,d", [(58241, 602), (40000, 290), (150000, 64)])
+def test_the_same_codes_every_time(B, ctx, bits, rows, d):
+    """Passes behind one another, on matrices long enough that every stage of shared memory is filled many times."""
+    import torch
+    x = torch.randn((rows, (d + 3) // 4 * 4), device="cuda")[:, :d] * torch.exp(torch.randn((rows, 1), device="cuda"))
+    x = x.contiguous() if d % 4 == 0 else torch.nn.functional.pad(x, (0, -d % 4))[:, :d]
+    q, y = B.new_mx(rows, d, B.SAT_MX8 if bits == 8 else B.SAT_MX4), torch.zeros((rows, (d + 3) // 4 * 4), device="cuda")[:, :d]
+    for t in q._keep:
+        t.zero_()
+    B.sat_mx_quantise(ctx, x, q)
+    B.sat_mx_dequantise(ctx, q, y)
+    part = np.r_[0:50, rows // 2:rows // 2 + 50, rows - 50:rows]
+    c, s = mx.quantise(x.cpu().numpy()[part], bits)
+    assert np.array_equal(q._keep[0].cpu().numpy()[part][:, :c.shape[1]], c) and np.array_equal(_np(y)[part], mx.dequantise(c, s, d, bits))
+    first = [t.clone() for t in (*q._keep, y)]
+    for _ in range(60):
+        for t in (*q._keep, y):
+            t.zero_()
+        for _ in range(2):
+            B.sat_mx_quantise(ctx, x, q)
+            B.sat_mx_dequantise(ctx, q, y)
+        assert all(bool(torch.equal(a, b)) for a, b in zip(first, (*q._keep, y)))
+
+
+@pytest.mark.parametrize("m,n,k", [(60000, 256, 256), (30000, 100, 602)])
+def test_the_same_results_every_time(B, ctx, m, n, k):
+    import torch
+    x, g = torch.randn((m, (k + 3) // 4 * 4), device="cuda")[:, :k], torch.randn((m, n), device="cuda")
+    w8, w4, kept = B.new_mx(n, k, B.SAT_MX8), B.new_mx(n, k, B.SAT_MX4), B.new_mx(m, k, B.SAT_MX4)
+    for t in (w8, w4):
+        B.sat_mx_quantise(ctx, torch.nn.functional.pad(torch.randn((n, k), device="cuda"), (0, -k % 4))[:, :k], t)
+    for t in kept._keep:
+        t.zero_()
+    y, gx, gw, gb = torch.zeros((m, n), device="cuda"), torch.zeros((m, (k + 3) // 4 * 4), device="cuda")[:, :k], torch.zeros((k, n), device="cuda"), torch.zeros(n, device="cuda")
+    outs, first = (y, gx, gw, gb, *kept._keep), None
+    for _ in range(40):
+        for t in outs:
+            t.zero_()
+        for _ in range(2):
+            B.sat_mx_dense_nt(ctx, x, w4, None, y, kept)
+            B.sat_mx_dense_nn(ctx, g, w8, gx)
+            B.sat_mx_dense_tn(ctx, kept, g, gw, gb)
+        if first is None:
+            first = [t.clone() for t in outs]
+        assert all(bool(torch.equal(a, b)) for a, b in zip(first, outs))
+
+
 # ---- contractions ---------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("m,n,k,extra", [(1, 1, 1, 0), (1, 512, 512, 0), (2, 40, 33, 4), (9, 17, 64, 0), (16, 130, 2050, 4), (33, 300, 129, 0), (127, 72, 50, 4), (128, 256, 256, 0),
                                          (129, 257, 31, 0), (1000, 47, 602, 0), (300, 600, 1030, 0), (4096, 128, 100, 0), (20000, 256, 256, 0), (19001, 40, 300, 4)])
