@@ -657,6 +657,7 @@ sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, co
 sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
 {
     const int32_t tiles_n = (int32_t)cdiv64(n, 256), bn = (int32_t)cdiv64(cdiv64(n, tiles_n), 64) * 64;
+    if (cdiv64(n, 8) > 65535) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: shape is too large");
     MxtArgs a{};
     CUtensorMap map_x, map_q;
     SAT_TRY(mxt_args(ctx, A, n, bn, &a, &map_q));
@@ -687,7 +688,6 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
     SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, B, n, A->rows, (int64_t)ldb * 4, bn / 2, MXT_KB, CU_TENSOR_MAP_SWIZZLE_NONE));
     SAT_TRY((A->format == SAT_MX8 ? mxt_launch<true, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<true, SAT_MX4>(ctx, map_x, map_q, a)));
     if (splits == 1) return SAT_OK;
-    if (cdiv64(n, 8) > 65535) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: shape is too large");
     sat_pdl(ctx->stream, k_mx_reduce, dim3((unsigned)cdiv64(a.D, 32), (unsigned)cdiv64(n, 8)), 1024, 0)(a.C, a.colsum, splits, a.D, n, accumulate, C, colsum);
     SAT_LAUNCHED(ctx);
     return SAT_OK;

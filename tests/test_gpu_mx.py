@@ -209,7 +209,8 @@ def test_the_same_results_every_time(B, ctx, m, n, k):
 
 # ---- contractions ---------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("m,n,k,extra", [(1, 1, 1, 0), (1, 512, 512, 0), (2, 40, 33, 4), (9, 17, 64, 0), (16, 130, 2050, 4), (33, 300, 129, 0), (127, 72, 50, 4), (128, 256, 256, 0),
-                                         (129, 257, 31, 0), (1000, 47, 602, 0), (300, 600, 1030, 0), (4096, 128, 100, 0), (20000, 256, 256, 0), (19001, 40, 300, 4)])
+                                         (129, 257, 31, 0), (1000, 47, 602, 0), (300, 600, 1030, 0), (4096, 128, 100, 0), (20000, 256, 256, 0), (19001, 40, 300, 4),
+                                         (3001, 8, 64, 0), (301, 40, 10, 4), (40, 3, 2, 0), (5000, 1, 33, 0), (19, 1, 1, 0)])
 @pytest.mark.parametrize("source", ["fp32", "kept", "codes"])
 def test_product_of_4_bit_operands(B, ctx, m, n, k, extra, source):
     import torch
@@ -239,7 +240,8 @@ def test_product_of_4_bit_operands(B, ctx, m, n, k, extra, source):
 
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("m,n,k,extra", [(1, 1, 1, 0), (1, 512, 512, 0), (5, 33, 40, 4), (128, 256, 32, 0), (129, 100, 47, 0), (301, 100, 47, 4), (64, 257, 1000, 0), (1000, 600, 700, 0),
-                                         (20000, 256, 40, 0), (19001, 300, 256, 4)])
+                                         (20000, 256, 40, 0), (19001, 300, 256, 4),
+                                         (30001, 1, 413, 0), (20001, 7, 5, 4), (2630, 2, 570, 0), (40000, 33, 1, 0), (1, 448, 49, 0)])
 def test_rows_times_stored_weights(B, ctx, bits, m, n, k, extra):
     import torch
     rng = np.random.default_rng(m + 3 * n + 5 * k)
@@ -257,7 +259,8 @@ def test_rows_times_stored_weights(B, ctx, bits, m, n, k, extra):
 
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("rows,m,n,extra", [(1, 1, 1, 0), (1, 300, 40, 0), (5, 33, 17, 4), (31, 64, 128, 0), (32, 256, 16, 0), (33, 100, 129, 0), (301, 100, 47, 4), (2048, 32, 16, 0),
-                                            (1000, 602, 256, 0), (5000, 257, 130, 0), (30000, 256, 256, 4), (41001, 40, 300, 0)])
+                                            (1000, 602, 256, 0), (5000, 257, 130, 0), (30000, 256, 256, 4), (41001, 40, 300, 0),
+                                            (20000, 64, 3, 0), (50001, 17, 192, 4), (30000, 1, 1, 0), (49, 1, 300, 4), (90, 300, 2, 0)])
 def test_weight_and_bias_gradient_from_a_checkpoint(B, ctx, bits, rows, m, n, extra):
     import torch
     rng = np.random.default_rng(rows + 3 * m + 5 * n)
