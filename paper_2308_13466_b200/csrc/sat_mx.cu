@@ -234,8 +234,11 @@ k_mx_dequantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, 
     if (t == 0) tma_store_wait_all();
 }
 
-// From which size on boxes are used
-#define MXB_LEAST(ctx) (4 * (int64_t)(ctx)->sms)
+// From how many boxes on boxes are used, against threads that each take a group from memory.  Measured, threads against boxes, 256 columns:
+// quantising 1000 rows (64 boxes) 2.2 / 2.4 us, 4000 rows (256) 3.6 / 2.5 us, 40000 rows (2504) 14.3 / 8.1 us;
+// back to fp32 1000 rows 1.6 / 3.3 us, 9472 rows (592) 3.5 / 3.4 us, 20000 rows (1256) 5.7 / 6.5 us, 40000 rows in 4 bits 10.1 / 8.7 us.
+#define MXB_LEAST_QUANTISE(ctx) ((int64_t)(ctx)->sms)
+#define MXB_LEAST_DEQUANTISE(ctx) (16 * (int64_t)(ctx)->sms)
 
 template <typename K, typename... A>
 static sat_status mx_launch_boxes(sat_ctx *ctx, PerDeviceOnce &attr, K kernel, int64_t boxes, const A &...args)
@@ -255,7 +258,7 @@ sat_status sat_mx_quantise_rows(sat_ctx *ctx, const float *x, int32_t ld, const 
     const int32_t groups = mx_groups(q->d);
     const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8), boxes = cdiv64(q->rows, 128) * groups;
     ProfScope prof(ctx, SATK_MX, (double)q->rows * (4.0 * q->d + mx_row_bytes(q) + groups), 0.0);
-    if (boxes >= MXB_LEAST(ctx)) {
+    if (boxes >= MXB_LEAST_QUANTISE(ctx)) {
         static PerDeviceOnce attr8, attr4;
         CUtensorMap map;
         SAT_TRY(sat_tensor_map(ctx, &map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, x, q->d, q->rows, (int64_t)ld * 4, MX_GROUP, 128, CU_TENSOR_MAP_SWIZZLE_128B));
@@ -285,7 +288,7 @@ extern "C" sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, fl
     const int32_t groups = mx_groups(q->d);
     const int64_t total = q->rows * groups, blocks = std::min<int64_t>(cdiv64(total, 32), (int64_t)ctx->sms * 8), boxes = cdiv64(q->rows, 128) * groups;
     ProfScope prof(ctx, SATK_MX, (double)q->rows * (4.0 * q->d + mx_row_bytes(q) + groups), 0.0);
-    if (boxes >= MXB_LEAST(ctx)) {
+    if (boxes >= MXB_LEAST_DEQUANTISE(ctx)) {
         static PerDeviceOnce attr8, attr4;
         CUtensorMap map;
         SAT_TRY(sat_tensor_map(ctx, &map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, x, q->d, q->rows, (int64_t)ld * 4, MX_GROUP, 128, CU_TENSOR_MAP_SWIZZLE_128B));

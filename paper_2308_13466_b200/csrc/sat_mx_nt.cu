@@ -398,8 +398,10 @@ k_mx_nt_few(const float *__restrict__ A, int64_t lda, int32_t m, int32_t n, int3
     }
 }
 
-// whether the bytes of A and their exponents fit
-static bool nt_few(int64_t m, int32_t groups) { return m <= NT_FEW && m * groups * 34 <= NT_FEW_SMEM; }
+// Whether the rows are few: the tiles take the same time for 1 to 64 rows, this kernel time in proportion to rows x groups.  Measured, this kernel
+// against tiles: n = 256, k = 100 1.8 / 5.8 us with one row, 5.7 / 5.9 with 16, 7.8 / 5.9 with 24; 512 x 512 1.9 / 9.0 with one, 8.6 / 9.0 with 12,
+// 11.0 / 9.0 with 16; 1024 x 1024 2.6 / 13.6 with one, 11.9 / 13.6 with 8, 17.0 / 13.6 with 12.  The bytes of A and their exponents have to fit.
+static bool nt_few(int64_t m, int32_t groups) { return m <= NT_FEW && m * groups <= 120 + 5 * (int64_t)groups && m * groups * 34 <= NT_FEW_SMEM; }
 
 static sat_status nt_launch_few(sat_ctx *ctx, int32_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias, float *C, int32_t ldc)
 {
