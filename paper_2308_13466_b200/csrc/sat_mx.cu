@@ -372,13 +372,11 @@ k_mx_simple(MxSimple p)
     if (OP == MX_TN && p.cs && blockIdx.x == 0 && threadIdx.x < 64 && j0 + (int32_t)threadIdx.x < p.N) p.cs[(int64_t)blockIdx.z * p.N + j0 + threadIdx.x] = cs;
 }
 
-// Which contractions run on the tensor cores: all of any length, however narrow, since a 64 x 64 tile of k_mx_simple pays its loads' latency once
-// per 16 terms. Measured, k_mx_simple against the tensor cores: A W^ of 1000 x 256 by 256 x 256 in 8 bits 38.4 against 12.2 us, of 83947 x 413 by
-// 413 x 1 290 against 52; A^T B of 50758 x 17 by 50758 x 192 100 against 32, of 20000 x 64 by 20000 x 3 19.0 against 20.7; A^ W^T of 17 rows,
-// 133 by 160, 16.5 against 7.0, of 3000 x 64 by 8 16.1 against 4.2. Few terms in few tiles are done before a pair of SMs has set up its
-// accumulators: A W^ of 1 x 40 by 40 x 256 6.2 against 8.3 us, of 1000 x 40 by 40 x 256 8.7 against 9.7, of 2048 x 16 by 16 x 32 4.1 against 9.0,
-// of 301 x 47 by 47 x 100 8.7 against 9.5; A^T B of 3 x 448 by 3 x 18 4.6 against 8.0, of 30 x 100 by 30 x 18 7.8 against 8.0.
-static bool mx_tc(int64_t terms, int64_t tiles) { return sat_use_tc(16, 16) && (terms > 48 || tiles > 300); }
+// All contractions run on the tensor cores, however narrow and short, where the environment does not say otherwise.  Measured, k_mx_simple against them:
+// A W^ of 1000 x 256 by 256 x 256 in 8 bits 38.4 / 8.0 us, of 1 x 40 by 40 x 256 6.1 / 4.3, of 83947 x 413 by 413 x 1 290 / 47; A^T B of 50758 x 17 by
+// 50758 x 192 100 / 29, of 30 x 100 by 30 x 18 7.6 / 5.0; A^ W^T of 3000 x 64 by 8 16.1 / 4.2.  Where there is least to do k_mx_simple would save a little:
+// A W^ of 2048 x 16 by 16 x 32 4.1 / 5.0 us, A^T B of 3 x 448 by 3 x 18 4.6 / 5.3.
+static bool mx_tc() { return sat_use_tc(16, 16); }
 static sat_status mx_grid(sat_ctx *ctx, int64_t M, int32_t N, int64_t splits, dim3 *grid)
 {
     if (cdiv64(N, 64) > 65535 || splits > 65535 || cdiv64(M, 64) > INT32_MAX) return sat_fail(ctx, SAT_EINVAL, "microscaled contraction: shape is too large");
@@ -400,7 +398,7 @@ extern "C" sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, i
         return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nt: null / misaligned tensor or bad leading dimension");
     if (m == 0) return SAT_OK;
     ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
-    if (sat_use_tc(16, 16)) return sat_mx_tc_nt(ctx, m, A, lda, Aq, W, bias, C, ldc);
+    if (mx_tc()) return sat_mx_tc_nt(ctx, m, A, lda, Aq, W, bias, C, ldc);
     sat_mx_matrix tmp;
     if (!Aq) {
         const int32_t groups = mx_groups(k), lds = (groups + 3) & ~3, ldq = groups * 16;
@@ -426,7 +424,7 @@ extern "C" sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, i
         return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_nn: null / misaligned tensor or bad shape");
     if (m == 0) return SAT_OK;
     ProfScope prof(ctx, SATK_MX, 4.0 * (double)m * (k + n), 2.0 * (double)m * n * k);
-    if (k > 0 && mx_tc(k, cdiv64(m, 64) * cdiv64(n, 64))) return sat_mx_tc_nn(ctx, m, A, lda, W, C, ldc);
+    if (k > 0 && mx_tc()) return sat_mx_tc_nn(ctx, m, A, lda, W, C, ldc);
     dim3 grid;
     SAT_TRY(mx_grid(ctx, m, n, 1, &grid));
     const MxSimple p{MxView{}, mx_view(W), A, lda, m, k, k, n, nullptr, C, nullptr, ldc};
@@ -439,7 +437,7 @@ sat_status sat_mx_gradient(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, cons
 {
     const int32_t m = A->d;
     ProfScope prof(ctx, SATK_MX, (double)A->rows * (mx_row_bytes(A) + mx_groups(m) + 4.0 * n), 2.0 * (double)A->rows * m * n);
-    if (A->rows > 0 && mx_tc(A->rows, cdiv64(m, 64) * cdiv64(n, 64))) return sat_mx_tc_tn(ctx, A, n, B, ldb, C, colsum, accumulate);
+    if (A->rows > 0 && mx_tc()) return sat_mx_tc_tn(ctx, A, n, B, ldb, C, colsum, accumulate);
     const int64_t rows = A->rows > 0 ? A->rows : 1, tiles = cdiv64(m, 64) * cdiv64(n, 64);
     int64_t splits = std::max<int64_t>(cdiv64(rows, 4096), std::min<int64_t>(cdiv64(4 * ctx->sms, tiles), cdiv64(rows, 64)));
     if (splits > 1024) splits = 1024;

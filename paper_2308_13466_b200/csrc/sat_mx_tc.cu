@@ -309,6 +309,7 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
     volatile int *dead = &s.sh->dead;
     const int32_t half = a.bn / 2;
     uint32_t st = 0, ph = 0;
+    if (lane == 0) tma_prefetch(map_x), tma_prefetch(map_q);
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         const int32_t x0 = it.n0 + s.rank * half, q0 = it.d0 + s.rank * 128;
@@ -317,6 +318,7 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
         const uint8_t *scales = a.scales + (int64_t)(it.k0 + lane) * a.ld_scales + q0 / MX_GROUP;   // four bytes, of which some may lie behind the row's last
         for (int32_t k = it.k0; k < it.k1; k += MXT_KB, scales += MXT_KB * a.ld_scales) {
             if (!mxt_wait<100>(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
+            if (i == s.unit && k == it.k0) sat_grid_wait();   // (what comes before is set-up; the converters and the MMAs touch no global memory, the other roles wait as well)
             uint64_t *bar = &s.sh->raw_full[st];
             if (lane == 0) {
                 uint8_t *x = s.raw + st * MXT_RAW_STAGE;
@@ -444,12 +446,13 @@ __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int 
     const int32_t c0 = (warp >> 2) * 128, here = min(8, (a.bn - c0) / 16);   // 16 columns at a time
     const uint32_t lanes = s.tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c0;
     uint32_t run = 0;
+    sat_grid_wait();
     uint32_t acc[128];   // bits of the sums
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const int32_t stages = mxt_item(a, i).stages;
 #pragma unroll 1
         for (int32_t k0 = 0; k0 < stages; k0 += MXT_RUN<TN>, ++run) {
-            if (!mxt_wait<250>(&s.sh->acc_full, run & 1u, dead, a.status)) return;
+            if (!mxt_wait<60>(&s.sh->acc_full, run & 1u, dead, a.status)) return;
             tc_fence_after();
             const bool last = k0 + MXT_RUN<TN> >= stages;
             if (k0 == 0) {   // straight to where it stays
@@ -501,6 +504,7 @@ __device__ __forceinline__ void mxt_totals(const MxtArgs &a, const MxtMem &s, in
 {
     const int32_t half = a.bn / 2;
     uint32_t turn = 0;
+    sat_grid_wait();
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
         if (it.d0 != 0) continue;
@@ -553,7 +557,6 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     cluster_sync();   // the other CTA's barriers are initialised and its TMEM is allocated
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
-    sat_grid_wait();   // everything above is set-up of this block; no global memory has been touched
     // 640 threads start with 96 registers each; the two warpgroups that add up the runs, 128 sums a thread, go to 152, the converters' two to 72 and the fifth
     // one to 32: 2 x 152 + 2 x 72 + 32 = 5 x 96
     if (warp < MXT_WORKERS) {

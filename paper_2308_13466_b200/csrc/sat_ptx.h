@@ -58,6 +58,7 @@ __device__ __forceinline__ bool mbar_wait_all(uint64_t *bar, uint32_t parity, vo
 {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, dead, status));
 }
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tma_load_2d(void *smem_dst, const CUtensorMap *map, uint64_t *bar, int32_t x, int32_t y)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
