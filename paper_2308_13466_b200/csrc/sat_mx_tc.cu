@@ -63,10 +63,9 @@ struct MxtArgs {
     int32_t K, kps;            // terms, and terms of a split (a multiple of MXT_KB)
     int32_t bn, tiles_d, tiles_n;
     int32_t items;             // tiles times splits, the tiles of a split next to each other
-    float *C;                  // element (column j of Q, column or row i of X) of split z at C + z split + i by_x + j by_q
-    int64_t split, by_x, by_q;
+    float *C;                  // element (column j of Q, column or row i of X) of split z at C + z split + i by_x + j
+    int64_t split, by_x;
     float *colsum;             // TN: [splits][N] column sums of X, or none
-    int add;                   // to what is there
     int *status;
 };
 // A tile and its terms [k0, k1)
@@ -479,21 +478,21 @@ __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int 
         }
         const MxtItem it = mxt_item(a, i);
         const int32_t col = it.d0 + s.rank * 128 + (warp & 3) * 32 + lane, n = min(a.bn, a.N - it.n0) - c0;
-        float *o = a.C + it.split * a.split + (it.n0 + c0) * a.by_x + col * a.by_q;
+        float *o = a.C + it.split * a.split + (it.n0 + c0) * a.by_x + col;
         if (col >= a.D) continue;
         // 16 at a time, those that are there: one warp a scheduler waits for every instruction, so what does not have to be looked at counts (301 x 100 by 301 x 47:
-        // 8100 clocks of 18000 went by here while each of the 128 was asked whether it is there and to be added)
+        // 8100 clocks of 18000 went by here while each of the 128 was asked whether it is there)
 #pragma unroll
         for (int c = 0; c < 8; ++c, o += 16 * a.by_x) {
             if (16 * c >= n) break;
             float *e = o;
-            if (16 * c + 16 <= n && !a.add) {
+            if (16 * c + 16 <= n) {
 #pragma unroll
                 for (int h = 0; h < 16; ++h, e += a.by_x) *e = __uint_as_float(acc[16 * c + h]);
             } else {
 #pragma unroll
                 for (int h = 0; h < 16; ++h, e += a.by_x)
-                    if (16 * c + h < n) *e = a.add ? *e + __uint_as_float(acc[16 * c + h]) : __uint_as_float(acc[16 * c + h]);
+                    if (16 * c + h < n) *e = __uint_as_float(acc[16 * c + h]);
             }
         }
     }
@@ -515,7 +514,7 @@ __device__ __forceinline__ void mxt_totals(const MxtArgs &a, const MxtMem &s, in
             const int32_t at = it.n0 + s.rank * half + c;
             if (at >= a.N) continue;
             float *out = a.colsum + (int64_t)it.split * a.N + at;
-            *out = a.add ? (float)((double)*out + sum) : (float)sum;
+            *out = (float)sum;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.sh->sums_empty);
@@ -608,12 +607,14 @@ k_mx_reduce(const float *__restrict__ part, const float *__restrict__ part_cs, i
             float *o = C + (int64_t)c * N + r;
             *o = add ? *o + sum : sum;
         }
-    } else if (threadIdx.x < 264 && blockIdx.x == 0 && colsum) {
-        const int32_t r = (int32_t)blockIdx.y * 8 + (int32_t)threadIdx.x - 256;
+    } else if (threadIdx.x < 512 && blockIdx.x == 0 && colsum) {   // a warp a column (one thread that took the splits in turn was what the launch waited for)
+        const int32_t r = (int32_t)blockIdx.y * 8 + ((int32_t)threadIdx.x >> 5) - 8;
         if (r < N) {
             double sum = 0.;
-            for (int32_t z = 0; z < splits; ++z) sum += (double)__ldg(part_cs + (int64_t)z * N + r);
-            colsum[r] = add ? (float)((double)colsum[r] + sum) : (float)sum;
+            for (int32_t z = lane; z < splits; z += 32) sum += (double)__ldg(part_cs + (int64_t)z * N + r);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) colsum[r] = add ? (float)((double)colsum[r] + sum) : (float)sum;
         }
     }
 }
@@ -664,7 +665,6 @@ sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, co
     SAT_TRY(mxt_args(ctx, W, m, bn, &a, &map_q));
     a.C = C;
     a.by_x = ldc;
-    a.by_q = 1;
     SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, A, W->rows, m, (int64_t)lda * 4, MXT_KB, bn / 2, CU_TENSOR_MAP_SWIZZLE_NONE));
     return W->format == SAT_MX8 ? mxt_launch<false, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<false, SAT_MX4>(ctx, map_x, map_q, a);
 }
@@ -687,23 +687,15 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
     a.kps = (int32_t)std::min<int64_t>(cdiv64(stages, best) * MXT_KB, INT32_MAX & ~(MXT_KB - 1));
     const int32_t splits = (int32_t)cdiv64(A->rows, a.kps);
     a.items *= splits;
-    if (splits == 1) {
-        a.C = C;
-        a.by_x = 1;
-        a.by_q = n;
-        a.add = accumulate;
-        a.colsum = colsum;
-    } else {
-        a.split = (int64_t)a.D * n;
-        SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)splits * (size_t)(a.split + n) * sizeof(float)));
-        a.C = (float *)ctx->buf_splitk.p;
-        a.by_x = a.D;
-        a.by_q = 1;
-        a.colsum = colsum ? a.C + splits * a.split : nullptr;
-    }
+    // One split goes through memory as well, as Q^^T X turned round: a lane holds a column of Q, so writing C itself takes 32 pieces of 32 lines an instruction (40 rows
+    // of 256 by 256: 30 us against 9.8; 30 of 100 by 18 5.0 against 6.1)
+    a.split = (int64_t)a.D * n;
+    SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)splits * (size_t)(a.split + n) * sizeof(float)));
+    a.C = (float *)ctx->buf_splitk.p;
+    a.by_x = a.D;
+    a.colsum = colsum ? a.C + splits * a.split : nullptr;
     SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, B, n, A->rows, (int64_t)ldb * 4, bn / 2, MXT_KB, CU_TENSOR_MAP_SWIZZLE_NONE));
     SAT_TRY((A->format == SAT_MX8 ? mxt_launch<true, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<true, SAT_MX4>(ctx, map_x, map_q, a)));
-    if (splits == 1) return SAT_OK;
     sat_pdl(ctx->stream, k_mx_reduce, dim3((unsigned)cdiv64(a.D, 32), (unsigned)cdiv64(n, 8)), 1024, 0)(a.C, a.colsum, splits, a.D, n, accumulate, C, colsum);
     SAT_LAUNCHED(ctx);
     return SAT_OK;
