@@ -136,8 +136,10 @@ k_mx_quantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, in
     const int64_t step = (int64_t)gridDim.x * 4;
     int64_t b = (int64_t)blockIdx.x * 4 + wg;
     uint8_t *mine = smem + wg * MXB_SLOTS * MXB_BOX;
+    uint32_t issued = 0;
     auto load = [&](int slot, int64_t box) {
-        if (t != 0 || box >= boxes) return;
+        if (t != 0 || box >= boxes || *(volatile int *)&sh.dead) return;
+        ++issued;
         const int64_t tile = sat_div(box, groups);
         mbar_expect_tx(&sh.full[wg][slot], MXB_BOX);
         tma_load_2d(mine + slot * MXB_BOX, &map_x, &sh.full[wg][slot], (int32_t)(box - tile * groups) * MX_GROUP, (int32_t)tile * 128);
@@ -170,6 +172,7 @@ k_mx_quantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, in
             q.scales[r * q.ld_scales + g] = (uint8_t)byte;
         }
     }
+    if (t == 0 && *(volatile int *)&sh.dead) mbar_settle(sh.full[wg], MXB_SLOTS, issued);
 }
 
 template <int FMT>

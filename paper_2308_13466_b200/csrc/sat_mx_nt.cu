@@ -106,27 +106,31 @@ __device__ __forceinline__ void nt_issue(const NtArgs &p, const NtMem &s)
 __device__ __forceinline__ void nt_load_a(const NtArgs &p, const NtMem &s, const CUtensorMap *map_a)
 {
     volatile int *dead = &s.sh->dead;
-    uint32_t slot = 0, ph = 0;
+    uint32_t slot = 0, ph = 0, issued = 0;
+    auto settle = [&](int g0) {   // the rings below g0 have had one more
+        for (int g = 0; g < 4; ++g) mbar_settle(s.sh->raw_full[g], NT_RAW, issued + (g < g0 ? 1u : 0u));
+    };
     for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
         const int32_t m0 = t / p.tiles_n * 128;
-        for (int32_t k = 0; k < p.stages; ++k) {
+        for (int32_t k = 0; k < p.stages; ++k, ++issued) {
             for (int g = 0; g < 4; ++g) {
-                if (!mbar_wait(&s.sh->raw_empty[g][slot], ph ^ 1u, dead, p.status)) return;
+                if (!mbar_wait(&s.sh->raw_empty[g][slot], ph ^ 1u, dead, p.status)) return settle(g);
                 mbar_expect_tx(&s.sh->raw_full[g][slot], NT_BOX);
                 tma_load_2d(s.raw + (g * NT_RAW + slot) * NT_BOX, map_a, &s.sh->raw_full[g][slot], k * NT_KB + 32 * g, m0);
             }
             if (++slot == NT_RAW) slot = 0, ph ^= 1u;
         }
     }
+    if (*dead) settle(0);
 }
 
 __device__ __forceinline__ void nt_load_w(const NtArgs &p, const NtMem &s, const CUtensorMap *map_w, int lane)
 {
     volatile int *dead = &s.sh->dead;
-    uint32_t st = 0, ph = 0;
+    uint32_t st = 0, ph = 0, issued = 0;
     for (int32_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
         const int32_t n0 = t % p.tiles_n * p.bn;
-        for (int32_t k = 0; k < p.stages; ++k) {
+        for (int32_t k = 0; k < p.stages; ++k, ++issued) {
             // four scales of each of up to eight rows; one where there is no such row or group
             uint32_t f[8];
             const int32_t left = p.groups - 4 * k;
@@ -137,7 +141,7 @@ __device__ __forceinline__ void nt_load_w(const NtArgs &p, const NtMem &s, const
                 f[i] = 0x7F7F7F7Fu;
                 if (r < p.bn && n0 + r < p.n) f[i] = (__ldg(reinterpret_cast<const uint32_t *>(p.w.scales + (int64_t)(n0 + r) * p.w.ld_scales) + k) & keep) | (0x7F7F7F7Fu & ~keep);
             }
-            if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, p.status)) return;
+            if (!mbar_wait_all(&s.sh->op_empty[st], ph ^ 1u, dead, p.status)) return mbar_settle(s.sh->op_full, NT_OP, issued);
             uint8_t *op = s.op + st * NT_STAGE;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -151,6 +155,7 @@ __device__ __forceinline__ void nt_load_w(const NtArgs &p, const NtMem &s, const
             if (++st == NT_OP) st = 0, ph ^= 1u;
         }
     }
+    if (*dead) mbar_settle(s.sh->op_full, NT_OP, issued);
 }
 
 template <bool STORED>

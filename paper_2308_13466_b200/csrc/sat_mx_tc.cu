@@ -307,7 +307,7 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
 {
     volatile int *dead = &s.sh->dead;
     const int32_t half = a.bn / 2;
-    uint32_t st = 0, ph = 0;
+    uint32_t st = 0, ph = 0, issued = 0;
     if (lane == 0) tma_prefetch(map_x), tma_prefetch(map_q);
     for (int32_t i = s.unit; i < a.items; i += s.units) {
         const MxtItem it = mxt_item(a, i);
@@ -316,7 +316,10 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
         const uint32_t bytes = (has_x ? (uint32_t)half * 128u : 0u) + (has_q ? 128u * MXT_KB * FMT / 8 : 0u);
         const uint8_t *scales = a.scales + (int64_t)(it.k0 + lane) * a.ld_scales + q0 / MX_GROUP;   // four bytes, of which some may lie behind the row's last
         for (int32_t k = it.k0; k < it.k1; k += MXT_KB, scales += MXT_KB * a.ld_scales) {
-            if (!mxt_wait<100>(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) return;
+            if (!mxt_wait<100>(&s.sh->raw_empty[st], ph ^ 1u, dead, a.status)) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                return mbar_settle(s.sh->raw_full, MXT_SLOTS, issued);
+            }
             if (i == s.unit && k == it.k0) sat_grid_wait();   // (what comes before is set-up; the converters and the MMAs touch no global memory, the other roles wait as well)
             uint64_t *bar = &s.sh->raw_full[st];
             if (lane == 0) {
@@ -330,9 +333,11 @@ __device__ __forceinline__ void mxt_load(const MxtArgs &a, const MxtMem &s, cons
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(s.sh->scales[st] + 4 * lane)), "l"(there ? scales : a.scales), "r"(there ? 4u : 0u) : "memory");
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
             if (++st == MXT_SLOTS) st = 0, ph ^= 1u;
+            ++issued;
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (*dead) mbar_settle(s.sh->raw_full, MXT_SLOTS, issued);
 }
 
 template <bool TN, int FMT>

@@ -43,6 +43,26 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     atomicOr(status, 1);
     return false;
 }
+// For a thread that gave up: the loads that are still on their way into a ring of `slots` stages land before the shared memory goes to somebody else.  `issued`
+// of them went to the slots in turn, each a phase of its slot's barrier; 100 ns at least a look, 2 ms at least a slot.
+__device__ __forceinline__ void mbar_settle(uint64_t *bars, uint32_t slots, uint32_t issued)
+{
+    for (uint32_t i = issued > slots ? issued - slots : 0u; i < issued; ++i)
+        for (uint32_t it = 0; it < 20000u; ++it) {
+            uint32_t ok;
+            asm volatile(
+                "{\n\t"
+                ".reg .pred p;\n\t"
+                "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t"
+                "}"
+                : "=r"(ok)
+                : "r"(smem_u32(bars + i % slots)), "r"((i / slots) & 1u)
+                : "memory");
+            if (ok) break;
+            __nanosleep(100);
+        }
+}
 // whole-warp wait: lane 0 polls, then every lane observes the completed phase itself (one immediate try_wait each), so
 // that a waiting warp issues one poll per round instead of 32
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, volatile int *dead, int *status, int lane)
