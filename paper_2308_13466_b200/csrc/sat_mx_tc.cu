@@ -163,14 +163,14 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t *r)
                  : "r"(taddr)
                  : "memory");
 }
-__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t *r)
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t *r)
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
-                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
                  : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared memory by its own addresses (through generic pointers, a conversion took a third more instructions)
 __device__ __forceinline__ float4 lds_f4(uint32_t at)
@@ -469,13 +469,13 @@ __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int 
             for (int half = 0; half < 2; ++half)   // the run, then the rest
                 if (half ? last : k0 > 0) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        if (c < here) {
-                            uint32_t r[16];
-                            tc_ld16(lanes + 256u * half + 16u * c, r);
+                    for (int c = 0; c < 16; ++c)
+                        if (c < 2 * here) {
+                            uint32_t r[8];
+                            tc_ld8(lanes + 256u * half + 8u * c, r);
                             tc_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) acc[16 * c + e] = __float_as_uint(__uint_as_float(acc[16 * c + e]) + __uint_as_float(r[e]));
+                            for (int e = 0; e < 8; ++e) acc[8 * c + e] = __float_as_uint(__uint_as_float(acc[8 * c + e]) + __uint_as_float(r[e]));
                         }
                 }
             tc_fence_before();
@@ -561,13 +561,13 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     cluster_sync();   // the other CTA's barriers are initialised and its TMEM is allocated
     tc_fence_after();
     s.tmem = s.sh->tmem_base;
-    // 640 threads start with 96 registers each; the two warpgroups that add up the runs, 128 sums a thread, go to 152, the converters' two to 72 and the fifth
-    // one to 32: 2 x 152 + 2 x 72 + 32 = 5 x 96
+    // 640 threads start with 96 registers each; the two warpgroups that add up the runs, 128 sums a thread, go to 160, the converters' two to 64 and the fifth
+    // one to 32: 2 x 160 + 2 x 64 + 32 = 5 x 96
     if (warp < MXT_WORKERS) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         mxt_work<TN, FMT>(a, s, warp, lane);
     } else if (warp < MXT_MMA) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         mxt_runs<TN>(a, s, warp - MXT_WORKERS, lane);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
