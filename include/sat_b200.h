@@ -556,7 +556,8 @@ sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int
  * their 24 bits (what lies below 2^-133 is dropped).  An infinity or a NaN in an fp32 operand makes NaN of every result that it reaches.  Results are bit-reproducible.
  * Empty sums (no rows, W without rows) are zero, or the bias.  Calls on one context share its workspaces like all calls of this
  * header: two captured graphs with calls of one context must not run at the same time, and the first call of a size may allocate (make
- * it before a capture). */
+ * it before a capture).  A later, larger call may move a workspace that a captured graph writes to: capture again behind it, or make the
+ * largest call first. */
 sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *Aq, const sat_mx_matrix *W, const float *bias,
                            float *C, int32_t ldc);
 sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc);

@@ -478,8 +478,13 @@ _lib.sat_mx_dense_tn.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, 
 def _rows(t):
     """Pointer and row stride of a CUDA fp32 matrix with contiguous rows."""
     (r, c), (s0, s1) = t.shape, t.stride()
-    assert t.is_cuda and (s1 == 1 or c <= 1)
+    assert t.is_cuda and t.dtype.itemsize == 4 and t.is_floating_point() and (s1 == 1 or c <= 1)
     return t.data_ptr(), s0 if r > 1 else max(s0, c)
+
+
+def _dense(t):
+    """Whether t is a CUDA fp32 tensor without gaps."""
+    return t.is_cuda and t.dtype.itemsize == 4 and t.is_floating_point() and t.is_contiguous()
 
 
 def new_mx(rows: int, d: int, fmt: int, device=None) -> sat_mx_matrix:
@@ -513,7 +518,7 @@ def sat_mx_dense_nt(ctx, A, W: sat_mx_matrix, bias, out, kept: sat_mx_matrix | N
         (m, k), (a, lda) = A.shape, _rows(A)
         assert kept is None or (kept.rows, kept.d) == (m, k)
     assert k == W.d and out.shape == (m, W.rows)
-    assert bias is None or (bias.is_cuda and bias.is_contiguous() and bias.numel() == W.rows)
+    assert bias is None or (_dense(bias) and bias.numel() == W.rows)
     _check(ctx, _lib.sat_mx_dense_nt(ctx, m, a, lda, None if kept is None else C.byref(kept), C.byref(W), None if bias is None else bias.data_ptr(), *_rows(out)))
 
 
@@ -527,8 +532,8 @@ def sat_mx_dense_nn(ctx, A, W: sat_mx_matrix, out):
 def sat_mx_dense_tn(ctx, A: sat_mx_matrix, Bm, out, colsum=None, accumulate: bool = False):
     """out[A.d, n] (+)= A^^T Bm[A.rows, n], colsum[n] (+)= column sums of Bm (out dense)"""
     n = Bm.shape[1]
-    assert out.is_cuda and out.is_contiguous() and Bm.shape[0] == A.rows and out.shape == (A.d, n)
-    assert colsum is None or (colsum.is_cuda and colsum.is_contiguous() and colsum.numel() == n)
+    assert _dense(out) and Bm.shape[0] == A.rows and out.shape == (A.d, n)
+    assert colsum is None or (_dense(colsum) and colsum.numel() == n)
     _check(ctx, _lib.sat_mx_dense_tn(ctx, C.byref(A), n, *_rows(Bm), out.data_ptr(), None if colsum is None else colsum.data_ptr(), 1 if accumulate else 0))
 
 

@@ -474,3 +474,16 @@ def test_refusals(B, ctx):
         B.sat_mx_dense_tn(ctx, q4, x[:10], out)
     B.sat_sync_status(ctx)
     assert bool((out == 2).all())
+
+
+def test_other_types_are_refused(B, ctx):
+    import torch
+    x, g, w = torch.zeros((40, 64), device="cuda"), torch.zeros((40, 8), device="cuda"), B.new_mx(8, 64, B.SAT_MX4)
+    q, gw, gb, y = B.new_mx(40, 64, B.SAT_MX4), torch.zeros((64, 8), device="cuda"), torch.zeros(8, device="cuda"), torch.zeros((40, 8), device="cuda")
+    for t in (torch.float64, torch.float16, torch.bfloat16, torch.int32):
+        for call in (lambda: B.sat_mx_quantise(ctx, x.to(t), q), lambda: B.sat_mx_dequantise(ctx, q, x.to(t)), lambda: B.sat_mx_dense_nt(ctx, x.to(t), w, None, y),
+                     lambda: B.sat_mx_dense_nt(ctx, x, w, gb.to(t), y), lambda: B.sat_mx_dense_nt(ctx, x, w, None, y.to(t)), lambda: B.sat_mx_dense_nn(ctx, g.to(t), w, x),
+                     lambda: B.sat_mx_dense_nn(ctx, g, w, x.to(t)), lambda: B.sat_mx_dense_tn(ctx, q, g.to(t), gw), lambda: B.sat_mx_dense_tn(ctx, q, g, gw.to(t)),
+                     lambda: B.sat_mx_dense_tn(ctx, q, g, gw, gb.to(t))):
+            with pytest.raises(AssertionError):
+                call()
