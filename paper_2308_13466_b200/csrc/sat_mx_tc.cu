@@ -586,41 +586,47 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
     }
 }
 
-// C[j][i] (+)= sum over the splits of part[z][i][j], cs[i] (+)= that of part_cs[z][i], in a fixed order: 32 columns of Q by eight of X per block,
-// four threads to an element
-__global__ void __launch_bounds__(1024)
-k_mx_reduce(const float *__restrict__ part, const float *__restrict__ part_cs, int32_t splits, int32_t D, int32_t N, int add, float *__restrict__ C, float *__restrict__ colsum)
+// C[j][i] (+)= sum over the splits of part[z][i][j], cs[i] (+)= that of part_cs[z][i], in a fixed order: 128 columns of Q by R of X per block, four columns to
+// a lane, every 16 / R-th split to a warp.  Bound by the L2 and its latency: R = 1 where
+// splits are many, for more loads at once, else 4, for longer pieces of C.  Measured with 1 / 4, gradient included: 73 splits of 256 x 256 18.0 / 21.5 us, of 100 x 128
+// 80.5 / 93; 24 splits of 602 x 256 18.3 / 17.5, 9 of 1024 x 512 58.8 / 53.3.
+template <int R>
+__global__ void __launch_bounds__(512)
+k_mx_reduce(const float *__restrict__ part, const float *__restrict__ part_cs, int32_t splits, int32_t D, int32_t N, int64_t ld, int add, float *__restrict__ C,
+            float *__restrict__ colsum)
 {
+    constexpr int Z = 16 / R;
     sat_grid_wait();
-    __shared__ float red[4][8][33];
-    const int lane = threadIdx.x & 31, i = (threadIdx.x >> 5) & 7, z4 = threadIdx.x >> 8;
-    const int32_t col = (int32_t)blockIdx.x * 32 + lane, row = (int32_t)blockIdx.y * 8 + i;
-    const int64_t plane = (int64_t)D * N;
-    float t = 0.f;
+    __shared__ float red[Z][R][132];
+    const int lane = threadIdx.x & 31, i = (threadIdx.x >> 5) % R, z0 = (threadIdx.x >> 5) / R;
+    const int32_t tiles = (D + 127) / 128, tile = (int32_t)(blockIdx.x % (uint32_t)tiles), col = tile * 128 + 4 * lane, row0 = (int32_t)(blockIdx.x / (uint32_t)tiles) * R, row = row0 + i;
+    const int64_t plane = ld * N;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
     if (col < D && row < N) {
-        const float *p = part + (int64_t)row * D + col;
+        const float *p = part + (int64_t)row * ld + col;
 #pragma unroll 8
-        for (int32_t z = z4; z < splits; z += 4) t += __ldg(p + z * plane);
+        for (int32_t z = z0; z < splits; z += Z) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(p + z * plane));
+            t = make_float4(t.x + v.x, t.y + v.y, t.z + v.z, t.w + v.w);
+        }
     }
-    red[z4][i][lane] = t;
-    __syncthreads();
-    if (threadIdx.x < 256) {
-        const int jj = threadIdx.x >> 3, ii = threadIdx.x & 7;   // eight lanes write eight consecutive floats of a row of C
-        const int32_t c = (int32_t)blockIdx.x * 32 + jj, r = (int32_t)blockIdx.y * 8 + ii;
-        if (c < D && r < N) {
-            const float sum = (red[0][ii][jj] + red[1][ii][jj]) + (red[2][ii][jj] + red[3][ii][jj]);
-            float *o = C + (int64_t)c * N + r;
-            *o = add ? *o + sum : sum;
-        }
-    } else if (threadIdx.x < 512 && blockIdx.x == 0 && colsum) {   // a warp a column (one thread that took the splits in turn was what the launch waited for)
-        const int32_t r = (int32_t)blockIdx.y * 8 + ((int32_t)threadIdx.x >> 5) - 8;
-        if (r < N) {
-            double sum = 0.;
-            for (int32_t z = lane; z < splits; z += 32) sum += (double)__ldg(part_cs + (int64_t)z * N + r);
+    *reinterpret_cast<float4 *>(&red[z0][i][4 * lane]) = t;
+    if (z0 == Z - 1 && tile == 0 && colsum && row < N) {   // a warp a column (one thread that took the splits in turn was what the launch waited for)
+        double sum = 0.;
+        for (int32_t z = lane; z < splits; z += 32) sum += (double)__ldg(part_cs + (int64_t)z * N + row);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if (lane == 0) colsum[r] = add ? (float)((double)colsum[r] + sum) : (float)sum;
-        }
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) colsum[row] = add ? (float)((double)colsum[row] + sum) : (float)sum;
+    }
+    __syncthreads();
+    const int j = threadIdx.x / R, ii = threadIdx.x % R;   // R lanes write R consecutive floats of a row of C
+    const int32_t c = tile * 128 + j, r = row0 + ii;
+    if (j < 128 && c < D && r < N) {
+        float sum = 0.f;
+#pragma unroll
+        for (int z = 0; z < Z; ++z) sum += red[z][ii][j];
+        float *o = C + (int64_t)c * N + r;
+        *o = add ? *o + sum : sum;
     }
 }
 
@@ -677,7 +683,6 @@ sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, co
 sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate)
 {
     const int32_t tiles_n = (int32_t)cdiv64(n, 256), bn = (int32_t)cdiv64(cdiv64(n, tiles_n), 64) * 64;
-    if (cdiv64(n, 8) > 65535) return sat_fail(ctx, SAT_EINVAL, "sat_mx_dense_tn: shape is too large");
     MxtArgs a{};
     CUtensorMap map_x, map_q;
     SAT_TRY(mxt_args(ctx, A, n, bn, &a, &map_q));
@@ -694,14 +699,17 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
     a.items *= splits;
     // One split goes through memory as well, as Q^^T X turned round: a lane holds a column of Q, so writing C itself takes 32 pieces of 32 lines an instruction (40 rows
     // of 256 by 256: 30 us against 9.8; 30 of 100 by 18 5.0 against 6.1)
-    a.split = (int64_t)a.D * n;
+    a.by_x = (a.D + 3) & ~3;
+    a.split = a.by_x * n;
     SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)splits * (size_t)(a.split + n) * sizeof(float)));
     a.C = (float *)ctx->buf_splitk.p;
-    a.by_x = a.D;
     a.colsum = colsum ? a.C + splits * a.split : nullptr;
     SAT_TRY(sat_tensor_map(ctx, &map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, B, n, A->rows, (int64_t)ldb * 4, bn / 2, MXT_KB, CU_TENSOR_MAP_SWIZZLE_NONE));
     SAT_TRY((A->format == SAT_MX8 ? mxt_launch<true, SAT_MX8>(ctx, map_x, map_q, a) : mxt_launch<true, SAT_MX4>(ctx, map_x, map_q, a)));
-    sat_pdl(ctx->stream, k_mx_reduce, dim3((unsigned)cdiv64(a.D, 32), (unsigned)cdiv64(n, 8)), 1024, 0)(a.C, a.colsum, splits, a.D, n, accumulate, C, colsum);
+    if (splits > 32)
+        sat_pdl(ctx->stream, k_mx_reduce<1>, (unsigned)(cdiv64(a.D, 128) * n), 512, 0)(a.C, a.colsum, splits, a.D, n, a.by_x, accumulate, C, colsum);
+    else
+        sat_pdl(ctx->stream, k_mx_reduce<4>, (unsigned)(cdiv64(a.D, 128) * cdiv64(n, 4)), 512, 0)(a.C, a.colsum, splits, a.D, n, a.by_x, accumulate, C, colsum);
     SAT_LAUNCHED(ctx);
     return SAT_OK;
 }
