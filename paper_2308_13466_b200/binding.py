@@ -478,13 +478,13 @@ _lib.sat_mx_dense_tn.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, 
 def _rows(t):
     """Pointer and row stride of a CUDA fp32 matrix with contiguous rows."""
     (r, c), (s0, s1) = t.shape, t.stride()
-    assert t.is_cuda and t.dtype.itemsize == 4 and t.is_floating_point() and (s1 == 1 or c <= 1)
+    assert t.is_cuda and (f := t.dtype).itemsize == 4 and f.is_floating_point and (s1 == 1 or c <= 1)
     return t.data_ptr(), s0 if r > 1 else max(s0, c)
 
 
 def _dense(t):
     """Whether t is a CUDA fp32 tensor without gaps."""
-    return t.is_cuda and t.dtype.itemsize == 4 and t.is_floating_point() and t.is_contiguous()
+    return t.is_cuda and (f := t.dtype).itemsize == 4 and f.is_floating_point and t.is_contiguous()
 
 
 def new_mx(rows: int, d: int, fmt: int, device=None) -> sat_mx_matrix:
