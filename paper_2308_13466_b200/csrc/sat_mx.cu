@@ -213,22 +213,23 @@ k_mx_dequantise_boxes(const __grid_constant__ CUtensorMap map_x, int64_t boxes, 
         uint8_t *box = mine + slot * MXB_BOX;
         if (t == 0) tma_store_wait_read<MXB_SLOTS - 1>();   // the box that was here has left
         mxb_sync(wg);
+        // A bulk store writes whole 16 bytes: those of a row that are left are written from here
+        const int64_t tile = sat_div(b, groups), r = tile * 128 + t;
+        const int32_t col = (int32_t)(b - tile * groups) * MX_GROUP, left = r < rows ? d - (d & ~3) : 0, last = (d & ~3) - col;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t w = FMT == SAT_MX8 ? c[i % FMT] : c[(i / 2) % FMT] >> (16 * (i & 1));
             const float2 lo = mx_unpack(mx_decode2<FMT>(w)), hi = mx_unpack(mx_decode2<FMT>(w >> (FMT == SAT_MX8 ? 16 : 8)));
-            *reinterpret_cast<float4 *>(box + t * 128 + ((i ^ (t & 7)) << 4)) = make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
+            const float4 v = make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
+            *reinterpret_cast<float4 *>(box + t * 128 + ((i ^ (t & 7)) << 4)) = v;
+            if (4 * i == last) {
+                float *o = x + r * ld + (d & ~3);
+                if (left > 0) o[0] = v.x;
+                if (left > 1) o[1] = v.y;
+                if (left > 2) o[2] = v.z;
+            }
         }
-        const int64_t tile = sat_div(b, groups);
-        const int32_t col = (int32_t)(b - tile * groups) * MX_GROUP;
-        if (col + MX_GROUP > d && (d & 3)) {   // a bulk store writes the last 16 bytes of a row whole
-            mxb_sync(wg);
-            for (int i = t >> 5; i < 128; i += 4)
-                if (tile * 128 + i < rows && col + (t & 31) < d)
-                    x[(tile * 128 + i) * ld + col + (t & 31)] = *reinterpret_cast<const float *>(box + i * 128 + ((((t & 31) >> 2) ^ (i & 7)) << 4) + (t & 3) * 4);
-            mxb_sync(wg);
-            continue;
-        }
+        if (last == 0) continue;
         fence_async_smem();
         mxb_sync(wg);
         if (t == 0) tma_store_2d(&map_x, box, col, (int32_t)tile * 128);
@@ -294,7 +295,7 @@ extern "C" sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, fl
     if (boxes >= MXB_LEAST_DEQUANTISE(ctx)) {
         static PerDeviceOnce attr8, attr4;
         CUtensorMap map;
-        SAT_TRY(sat_tensor_map(ctx, &map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, x, q->d, q->rows, (int64_t)ld * 4, MX_GROUP, 128, CU_TENSOR_MAP_SWIZZLE_128B));
+        SAT_TRY(sat_tensor_map(ctx, &map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, x, std::max(q->d & ~3, 4), q->rows, (int64_t)ld * 4, MX_GROUP, 128, CU_TENSOR_MAP_SWIZZLE_128B));
         if (q->format == SAT_MX8) return mx_launch_boxes(ctx, attr8, k_mx_dequantise_boxes<SAT_MX8>, boxes, map, boxes, groups, q->rows, q->d, mx_view(q), x, (int64_t)ld);
         return mx_launch_boxes(ctx, attr4, k_mx_dequantise_boxes<SAT_MX4>, boxes, map, boxes, groups, q->rows, q->d, mx_view(q), x, (int64_t)ld);
     }

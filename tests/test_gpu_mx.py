@@ -487,3 +487,21 @@ def test_other_types_are_refused(B, ctx):
                      lambda: B.sat_mx_dense_tn(ctx, q, g, gw, gb.to(t))):
             with pytest.raises(AssertionError):
                 call()
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows,d,extra", [(310001, 1, 0), (310000, 3, 4), (160000, 33, 0), (155000, 61, 4), (110000, 66, 0), (152000, 64, 8)])
+def test_long_matrices_back_to_fp32(B, ctx, bits, rows, d, extra):
+    """Widths whose last elements fill no 16 bytes: every value exact, nothing written behind a row's end."""
+    import torch
+    a = _rows(np.random.default_rng(rows + d), rows, d, 3.0)
+    q, values = _mx(B, a, bits)
+    out = _out(rows, d, extra)
+    B.sat_mx_dequantise(ctx, q, out)
+    B.sat_sync_status(ctx)
+    assert np.array_equal(_np(out), values.astype(np.float32)) and _untouched(out, d)
+    again = B.new_mx(rows, d, B.SAT_MX8 if bits == 8 else B.SAT_MX4)
+    B.sat_mx_quantise(ctx, _dev(a, extra), again)
+    second = _out(rows, d, extra)
+    B.sat_mx_dequantise(ctx, again, second)
+    assert bool(torch.equal(out, second))
