@@ -13,8 +13,8 @@
 // X.  What bounds it besides memory is shared memory, at 128 bytes a clock: per stage of 32 terms a CTA takes in 16 KB of X and 4 KB of codes
 // (written by TMA, read once), writes 24 KB and 8 KB of bf16, and the tensor core reads 32 KB (each CTA holds one half of X, and a tile of Q
 // stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  (With single CTAs and X as the M side it
-// was 183 KB for as many products.  Measured: 1,020 clocks a stage with TN, 1,130 without; 612257 x 256 by 256 225 us, 179250 x 512 x 512 274, at the 1.64 GHz that
-// the power limit leaves.  Loading straight into registers takes 40 KB less, but what it can keep in flight does not cover the latency.)
+// was 183 KB for as many products.  Loading straight into registers takes 40 KB less, but what it can keep in flight does not cover the latency.)
+// Measured: 1,020 clocks a stage with TN, 1,130 without; 612257 x 256 by 256 225 us, 179250 x 512 x 512 274, at the 1.64 GHz that the power limit leaves.
 //
 // (For NN, one accumulator of all three products, two of them by turns, taken out by four warps that write at once: 90000 x 512 x 512 108 us instead of 128, but
 // 96 chopped additions, 1.3e-6.)
