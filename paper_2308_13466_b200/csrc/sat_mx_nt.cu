@@ -390,8 +390,10 @@ k_mx_nt_few(const float *__restrict__ A, int64_t lda, int32_t m, int32_t n, int3
                 int32_t sum = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = __dp4a((int32_t)x[i], (int32_t)b[i], __dp4a((int32_t)x[i], (int32_t)neg[i], sum));
-                const int32_t e = we + exps[r * groups + g], half = e >> 1;   // in two steps: neither leaves the range before the product does
-                const float p = __int_as_float((half + 127) << 23), q = __int_as_float((e - half + 127) << 23);
+                // 2^e in two steps, neither of which leaves the range before the product does.  A sum is at most 32 x 144, so what lies below 2^-252 is
+                // 0 in fp32; two groups of zeros, whose scales are the least, come to -256
+                const int32_t e = we + exps[r * groups + g], f = max(e, -252), half = f >> 1;
+                const float p = __int_as_float((half + 127) << 23), q = __int_as_float((f - half + 127) << 23);
                 acc[r] += e > 500 ? __int_as_float(0x7FFFFFFF) : (float)sum * p * q;
             }
         }

@@ -1,0 +1,110 @@
+"""Microscaled contractions at the ends of their formats: groups of zeros and of the least and largest scales, elements and groups that are no
+numbers, sums of very many terms.  References in 64 bits; bounds as in test_gpu_mx.py, with what underflows counted apart.
+"""
+import numpy as np
+import pytest
+
+from oracle import mx_ref as mx
+from tests.test_gpu_mx import U, _bound, _dev, _mx, _np, _out, _rows
+
+pytestmark = pytest.mark.gpu
+FEW = (1, 4, 5, 16)               # rows of a product that a kernel of its own takes; 17 and 300 go by tiles
+
+
+@pytest.fixture(scope="module")
+def B():
+    import paper_2308_13466_b200.binding as binding
+    return binding
+
+
+@pytest.fixture(scope="module")
+def ctx(B):
+    c = B.sat_create(0, 0)
+    yield c
+    B.sat_destroy(c)
+
+
+def _lost(m, k):
+    """What may be lost to underflow: a few rows are rounded to the least fp32 number once a group; tiles may drop a product below the least normal one."""
+    return ((k + 31) // 32) * 2.0 ** -149 if m in FEW else k * 2.0 ** -126
+
+
+# largest element of a group and the 4-bit scale byte that it gets
+SIZES = [(0.0, 0), (2.0 ** -128, 0), (6 * 2.0 ** -127, 0), (6 * 2.0 ** -126, 1), (6 * 2.0 ** -20, 107), (5.0, 127), (6 * 2.0 ** 30, 157), (3.4 * 2.0 ** 126, 253)]
+
+
+def _group(rng, size, signed):
+    g = size * rng.uniform(0.1, 1.0, 32)
+    g[rng.integers(32)] = size
+    return (g * rng.choice([-1.0, 1.0], 32) if signed else g).astype(np.float32)
+
+
+@pytest.mark.parametrize("m", [1, 4, 5, 16, 17, 300])
+@pytest.mark.parametrize("stored", [False, True])
+def test_every_pair_of_scales(B, ctx, m, stored):
+    """One group to a row, so that a result comes from one pair of scales; all elements positive, so that what is too large has a sign."""
+    rng = np.random.default_rng(m)
+    w = np.stack([_group(rng, s, False) for s, _ in SIZES for _ in range(3)])
+    wq, wv = _mx(B, w, 4)
+    for shift in range(0, len(SIZES), m):
+        which = [SIZES[(shift + r) % len(SIZES)] for r in range(m)]
+        a = np.stack([_group(rng, s, False) for s, _ in which])
+        assert [int(b) for b in mx.quantise(a, 4)[1][:, 0]] == [b for _, b in which]
+        aq, av = _mx(B, a, 4)
+        out = _out(m, len(w))
+        B.sat_mx_dense_nt(ctx, aq if stored else _dev(a), wq, None, out)
+        B.sat_sync_status(ctx)
+        got, want = _np(out), av @ wv.T
+        there = want <= np.finfo(np.float32).max
+        assert np.all(np.abs(got - want)[there] <= (_bound(av, wv.T, 32) + _lost(m, 32))[there])
+        assert not np.isfinite(got[~there]).any()
+
+
+@pytest.mark.parametrize("m", [1, 4, 5, 16, 17, 300])
+@pytest.mark.parametrize("stored", [False, True])
+@pytest.mark.parametrize("k", [32, 150])
+def test_zero_and_tiny_groups_beside_others(B, ctx, m, stored, k):
+    import torch
+    rng = np.random.default_rng(100 * m + k)
+    n, groups = 70, (k + 31) // 32
+    sizes = np.array([0.0, 0.0, 2.0 ** -128, 6 * 2.0 ** -126, 1.0, 3.0])
+    make = lambda rows: np.concatenate([np.stack([_group(rng, s, True) for s in rng.choice(sizes, rows)]) for _ in range(groups)], axis=1)[:, :k]
+    a, w, bias = make(m), make(n), rng.normal(size=n).astype(np.float32)
+    a[0], w[3], w[n - 1] = 0.0, 0.0, 0.0                          # whole rows
+    aq, av = _mx(B, a, 4)
+    wq, wv = _mx(B, w, 4)
+    for b in (None, bias):
+        out, want = _out(m, n), av @ wv.T + (0.0 if b is None else b)
+        B.sat_mx_dense_nt(ctx, aq if stored else _dev(a), wq, None if b is None else torch.from_numpy(b).cuda(), out)
+        B.sat_sync_status(ctx)
+        got = _np(out)
+        assert np.isfinite(got).all()
+        assert np.all(np.abs(got - want) <= _bound(av, wv.T, k) + _lost(m, k) + (0.0 if b is None else U * (np.abs(want) + np.abs(b))))
+        empty = np.zeros(n) if b is None else bias.astype(np.float64)
+        assert np.array_equal(got[0], empty) and (got[:, 3] == empty[3]).all() and (got[:, n - 1] == empty[n - 1]).all()
+
+
+@pytest.mark.parametrize("m", [1, 4, 5, 16, 17, 300])
+@pytest.mark.parametrize("stored", [False, True])
+def test_groups_that_are_no_numbers(B, ctx, m, stored):
+    """They reach their row or column of results and nothing else, groups of zeros on the other side included."""
+    rng = np.random.default_rng(m)
+    k, n = 96, 72
+    a, w = _rows(rng, m, k), rng.normal(size=(n, k)).astype(np.float32)
+    a[:, 32:64], w[9, 32:64] = 0.0, 0.0
+    bad = np.zeros((m, n), dtype=bool)
+    if m > 1:
+        a[m - 1, 70], a[m // 2, 5] = np.inf, np.nan
+        bad[[m - 1, m // 2]] = True
+    w[5, 40] = np.nan                                            # its group meets only zeros
+    w[71, 3] = -np.inf
+    bad[:, [5, 71]] = True
+    aq, av = _mx(B, a, 4)
+    wq, wv = _mx(B, w, 4)
+    out = _out(m, n)
+    B.sat_mx_dense_nt(ctx, aq if stored else _dev(a), wq, None, out)
+    B.sat_sync_status(ctx)
+    got, want = _np(out), av @ wv.T
+    assert np.array_equal(np.isnan(got), bad) and np.array_equal(np.isnan(want), bad)
+    av, wv = np.nan_to_num(av), np.nan_to_num(wv)
+    assert np.all(np.abs(got - want)[~bad] <= (_bound(av, wv.T, k) + _lost(m, k))[~bad])
