@@ -528,7 +528,8 @@ sat_status sat_cache_requantise(sat_ctx *ctx, int32_t layer, int32_t age, int32_
  *     SAT_MX8   q in e4m3 (1 sign, 4 exponent, 3 fraction bits, bias 7, largest 448)       SAT_MX4   q in e2m1 (0 .5 1 1.5 2 3 4 6)
  *     e = the smallest integer >= -127 with max_{x in G} |x| <= largest 2^e,      q = x 2^-e rounded to nearest, ties to even.
  * Nothing saturates, so an element is off by at most 2^-4 |x| (SAT_MX8) or 2^-2 |x| (SAT_MX4) or half the format's least step times 2^e
- * (2^-10 or 2^-2), whichever is more.  A group with an infinity or a NaN has the scale byte 255 and reads as NaN throughout.
+ * (2^-10 or 2^-2), whichever is more.  A group with an infinity or a NaN has the scale byte 255 and reads as NaN throughout.  The codes 0x7F and
+ * 0xFF of SAT_MX8, which sat_mx_quantise does not write but a matrix encoded elsewhere may hold, read as NaN one by one, in contractions too.
  *   codes    DEVICE, row r at byte r * ld_codes: one byte per element (SAT_MX8) or two elements a byte, the even one in the low half
  *            (SAT_MX4), the last group filled up with zeros.  16-byte aligned, ld_codes a multiple of 16 and >= 32 (16) bytes a group
  *   scales   DEVICE, row r at byte r * ld_scales: e + 127 per group.  4-byte aligned, ld_scales a multiple of 4 and >= the groups

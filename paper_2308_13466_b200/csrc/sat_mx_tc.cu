@@ -201,6 +201,18 @@ __device__ __forceinline__ uint32_t lds_u1(uint32_t at)
 __device__ __forceinline__ void sts_u2(uint32_t at, const uint2 &v) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(v.x), "r"(v.y) : "memory"); }
 __device__ __forceinline__ void sts_u4(uint32_t at, const uint4 &v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
 
+// e4m3's codes of no number (seven ones behind the sign), which the conversion above takes for 480: NaN in their places among the two times 16 elements that
+// a thread of mxt_work converts.  Codes of sat_mx_quantise have none.
+__device__ __forceinline__ void mxt_no_numbers(uint32_t raw, uint32_t op, int32_t other)
+{
+#pragma unroll 1
+    for (int32_t i = 0; i < 32; ++i) {
+        const uint32_t e = i & 15, h = i >> 4;
+        if ((lds_u1(raw + h * (16 * 128) + e) & 0x7Fu) != 0x7Fu) continue;
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"((op ^ (((e >> 3) ^ (uint32_t)other) << 4)) + h * 2048 + 2 * (e & 7)), "h"((uint16_t)0x7FFF) : "memory");
+    }
+}
+
 // bf16 operands, fp32 accumulation; Q is MN-major (its tile has a row per term), X is with TN
 template <bool TN>
 __device__ __forceinline__ uint32_t mxt_idesc(int32_t bn)
@@ -398,18 +410,21 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
                     sts_u2(o + 2 * MXT_X_PLANE, lo);
                 }
             if (has_q) {
-                uint32_t c[2][4], byte[2];
+                uint32_t c[2][4], byte[2], odd = 0u;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     byte[h] = lds_u1(scales + st * MXT_SCALES + 64 * h);
                     if (FMT == SAT_MX8) {
                         const uint4 t = lds_u4(q_raw + raw + h * (16 * 128));
                         c[h][0] = t.x, c[h][1] = t.y, c[h][2] = t.z, c[h][3] = t.w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) odd |= c[h][e] ^ (c[h][e] + 0x01010101u);   // a byte's top bit changes where the others are all ones
                     } else {
                         const uint2 t = lds_u2(q_raw + raw + h * (16 * 64));
                         c[h][0] = t.x, c[h][2] = t.y, c[h][1] = c[h][3] = 0u;
                     }
                 }
+                const bool no_numbers = FMT == SAT_MX8 && (odd & 0x80808080u);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const MxtScale<FMT> sc(byte[h]);
@@ -419,6 +434,7 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
                     sts_u4(q_op + op + h * 2048, v0);
                     sts_u4((q_op ^ 16u) + op + h * 2048, v1);
                 }
+                if (no_numbers) mxt_no_numbers(q_raw + raw, q_op + op, other);
             }
             fence_async_smem();
             __syncwarp();

@@ -108,3 +108,53 @@ def test_groups_that_are_no_numbers(B, ctx, m, stored):
     assert np.array_equal(np.isnan(got), bad) and np.array_equal(np.isnan(want), bad)
     av, wv = np.nan_to_num(av), np.nan_to_num(wv)
     assert np.all(np.abs(got - want)[~bad] <= (_bound(av, wv.T, k) + _lost(m, k))[~bad])
+
+
+# ---- e4m3's codes of no number --------------------------------------------------------------------------------------------------
+def _planted(B, x, where):
+    """The 8-bit codes of x with 0x7F (even columns) or 0xFF at `where`, on the GPU, and what they stand for."""
+    import torch
+    codes, scales = mx.quantise(x, 8)
+    rows, d = x.shape
+    c = codes[:, :d]
+    c[where] = np.broadcast_to(np.where(np.arange(d) % 2 == 0, 0x7F, 0xFF).astype(np.uint8), c.shape)[where]
+    st = torch.zeros((rows, (scales.shape[1] + 3) // 4 * 4), dtype=torch.uint8, device="cuda")
+    st[:, :scales.shape[1]] = torch.from_numpy(scales).cuda()
+    values = mx.dequantise(codes, scales, d, 8)
+    assert np.array_equal(np.isnan(values), where)
+    return B.make_mx(torch.from_numpy(codes).cuda(), st, d, B.SAT_MX8), values
+
+
+@pytest.mark.parametrize("rows,d,others", [(1, 1, 1), (5, 33, 9), (64, 300, 70), (200, 256, 300), (3000, 130, 40)])
+@pytest.mark.parametrize("phase", [0, 1, 2])
+def test_codes_of_no_number(B, ctx, rows, d, others, phase):
+    """Matrices encoded elsewhere may hold them.  They read as NaN wherever they are read and reach their column of the stored matrix only:
+    every column, every third one bad, each at another row."""
+    import torch
+    rng = np.random.default_rng(rows + d + phase)
+    x = rng.normal(size=(rows, d)).astype(np.float32) * 300
+    where = np.zeros((rows, d), dtype=bool)
+    cols = np.arange(phase % d, d, 3)
+    where[(7 * cols) % rows, cols] = True
+    q, values = _planted(B, x, where)
+    back = _out(rows, d)
+    B.sat_mx_dequantise(ctx, q, back)
+    assert np.array_equal(_np(back), values, equal_nan=True)
+    bad, clean = where.any(0), np.nan_to_num(values)
+    a = rng.normal(size=(others, rows)).astype(np.float32)
+    a[0] = 0.0                                                   # nothing times no number is no number
+    out = _out(others, d)
+    B.sat_mx_dense_nn(ctx, _dev(a), q, out)
+    got = _np(out)
+    assert np.array_equal(np.isnan(got), np.broadcast_to(bad, got.shape))
+    a = a.astype(np.float64)
+    assert np.all(np.abs(got - a @ clean)[:, ~bad] <= _bound(a, clean, rows)[:, ~bad] + 1e-44)
+    g = rng.normal(size=(rows, others)).astype(np.float32)
+    g[:, others - 1] = 0.0
+    gw, gb = torch.zeros((d, others), device="cuda"), torch.zeros(others, device="cuda")
+    B.sat_mx_dense_tn(ctx, q, _dev(g), gw, gb)
+    B.sat_sync_status(ctx)
+    got = _np(gw)
+    assert np.array_equal(np.isnan(got), np.broadcast_to(bad[:, None], got.shape)) and np.isfinite(_np(gb)).all()
+    g = g.astype(np.float64)
+    assert np.all(np.abs(got - clean.T @ g)[~bad] <= _bound(clean.T, g, rows)[~bad] + 1e-44)
