@@ -8,6 +8,7 @@
 // The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts: 612257 terms in 74
 // splits were off by 1e-5 of the result.  Only the products with hi matter for that; those with mid and lo, 2^-8 of them, have an accumulator of their own,
 // and the one of hi is taken out every 12 stages (24 instructions; NN: 16) and added up in registers, rounded to nearest: 5e-7, an fp32 FMA loop's being 1e-6.
+// The other one follows every 32 runs: a million terms of one sign in one split were off by 4e-5 where it was taken out at their end only.
 //
 // A pair of CTAs shares a tile of 256 columns of Q (the M side, 128 lanes of TMEM in either CTA) by up to 256 columns (TN) or rows (NN) of
 // X.  What bounds it besides memory is shared memory, at 128 bytes a clock: per stage of 32 terms a CTA takes in 16 KB of X and 4 KB of codes
@@ -38,6 +39,7 @@
 #define MXT_SCALES (MXT_KB * 4)       /* of a stage: four groups a term */
 #define MXT_GROUPS 2                 /* groups of four converting warps, a divisor of the slots */
 template <bool TN> constexpr int32_t MXT_RUN = TN ? 12 : 16;   /* stages between two reads of the hi accumulator: 24 instructions, or 32 (one read for 512 terms) */
+#define MXT_REST 32                  /* runs between two reads of the accumulator of mid and lo, which starts anew then */
 #define MXT_WORKERS (4 * MXT_GROUPS)
 #define MXT_TAKERS 8                 /* warps that add up the runs, behind the converters; then one for the MMAs, for the loads, for the column sums */
 #define MXT_MMA (MXT_WORKERS + MXT_TAKERS)
@@ -254,7 +256,8 @@ struct MxtMem {
     int32_t rank;              // CTA of the pair
     int32_t unit, units;       // pair, and pairs
 };
-// Tensor memory: the accumulator of the products with hi, from column 256 on that of the rest, which is taken out with the last run of an item
+// Tensor memory: the accumulator of the products with hi, from column 256 on that of the rest, which is taken out with every MXT_REST-th run and the last
+// one of an item
 template <bool TN>
 __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
 {
@@ -270,7 +273,7 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
         const int32_t stages = mxt_item(a, i).stages;
         for (int32_t k0 = 0; k0 < stages; k0 += MXT_RUN<TN>, ++run) {
             const uint32_t hi = s.tmem, rest = s.tmem + 256u, taken = (run & 1u) ^ 1u;   // phase of acc_empty in which what was there before has been taken out
-            const bool wait_late = k0 > 0;   // within an item, mid and lo go ahead while the hi accumulator is still being read
+            const bool wait_late = k0 % (MXT_REST * MXT_RUN<TN>) != 0;   // else both start anew; mid and lo go ahead while the hi accumulator is still being read
             if (!wait_late && !mxt_wait(&s.sh->acc_empty, taken, dead, a.status)) return;
             const int32_t n = min(stages - k0, MXT_RUN<TN>);
             for (int32_t k = 0; k < n; ++k) {
@@ -281,7 +284,7 @@ __device__ __forceinline__ void mxt_mma(const MxtArgs &a, const MxtMem &s)
                     if (elect_one()) {
 #pragma unroll
                         for (uint32_t ks = 0; ks < MXT_KB / 16; ++ks) {   // the tile of Q stays in the collector for its three products
-                            tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, k0 > 0 || k > 0 || ks > 0 ? 1u : 0u);
+                            tc_mma_f16<1, 2>(rest, q + ks * q_step, x + ks * x_step + 2 * plane, idesc, wait_late || k > 0 || ks > 0 ? 1u : 0u);
                             tc_mma_f16<3, 2>(rest, q + ks * q_step, x + ks * x_step + plane, idesc, 1u);
                             tc_mma_f16<2, 2>(hi, q + ks * q_step, x + ks * x_step, idesc, k > 0 || ks > 0 ? 1u : 0u);
                         }
@@ -475,7 +478,7 @@ __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int 
         for (int32_t k0 = 0; k0 < stages; k0 += MXT_RUN<TN>, ++run) {
             if (!mxt_wait<60>(&s.sh->acc_full, run & 1u, dead, a.status)) return;
             tc_fence_after();
-            const bool last = k0 + MXT_RUN<TN> >= stages;
+            const bool with_rest = k0 + MXT_RUN<TN> >= stages || (k0 / MXT_RUN<TN> + 1) % MXT_REST == 0;
             if (k0 == 0) {   // straight to where it stays
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
@@ -484,7 +487,7 @@ __device__ __forceinline__ void mxt_runs(const MxtArgs &a, const MxtMem &s, int 
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half)   // the run, then the rest
-                if (half ? last : k0 > 0) {
+                if (half ? with_rest : k0 > 0) {
 #pragma unroll
                     for (int c = 0; c < 16; ++c)
                         if (c < 2 * here) {

@@ -158,3 +158,43 @@ def test_codes_of_no_number(B, ctx, rows, d, others, phase):
     assert np.array_equal(np.isnan(got), np.broadcast_to(bad[:, None], got.shape)) and np.isfinite(_np(gb)).all()
     g = g.astype(np.float64)
     assert np.all(np.abs(got - clean.T @ g)[~bad] <= _bound(clean.T, g, rows)[~bad] + 1e-44)
+
+
+# ---- very long sums ----------------------------------------------------------------------------------------------------------------
+LONG, LONG_D, LONG_N = 1_000_000, 4609, 1793                     # 152 tiles: a pair of SMs has more than one each, so the terms are not split
+
+
+@pytest.fixture(scope="module")
+def long_gradient(B, ctx):
+    """Weight and bias gradient of a million rows.  Codes: 0.5 to 1.875, scales one; gradients 2^j (1 + 2^-7 - 2^-12), whose second bf16 term is as
+    large as it can be, the last column a third throughout."""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    groups = (LONG_D + 31) // 32
+    codes = torch.randint(0x30, 0x40, (LONG, 32 * groups), dtype=torch.uint8, device="cuda", generator=gen)
+    codes[:, LONG_D:] = 0
+    q = B.make_mx(codes, torch.full((LONG, (groups + 3) // 4 * 4), 127, dtype=torch.uint8, device="cuda"), LONG_D, B.SAT_MX8)
+    g = torch.zeros((LONG, (LONG_N + 3) // 4 * 4), device="cuda")[:, :LONG_N]
+    g.copy_(torch.randint(0, 3, (LONG, LONG_N), dtype=torch.uint8, device="cuda", generator=gen))
+    g.sub_(1).exp2_().mul_(1 + 2.0 ** -7 - 2.0 ** -12)
+    g[:, -1] = 1 / 3
+    gw, gb = torch.zeros((LONG_D, LONG_N), device="cuda"), torch.zeros(LONG_N, device="cuda")
+    B.sat_mx_dense_tn(ctx, q, g, gw, gb)
+    B.sat_sync_status(ctx)
+    yield codes, g, gw, gb
+
+
+def test_weight_gradient_of_a_million_rows_does_not_drift(long_gradient):
+    """All terms are positive, so that what is chopped adds up.  A run of the leading accumulator is 24 instructions, two units of 2^-23 each at
+    most; the accumulator of the lower terms, 2^-7 of the sum, is taken out every 384 stages of 4 instructions: 48 U + 2 * 1536 * 2^-7 U.  Runs are
+    added up rounded to nearest: no drift, 0.3 U sqrt(2605 / 3) = 9 U to an element, 9 / 20 U in the mean of 400 independent ones."""
+    import torch
+    codes, g, gw, _ = long_gradient
+    cols, rows = torch.linspace(0, LONG_D - 1, 40, device="cuda").long(), torch.linspace(0, LONG_N - 2, 10, device="cuda").long()
+    c = codes[:, cols].long()
+    a = (1 + (c % 8) / 8.0).double() * torch.exp2((c // 8 - 7).double())
+    want = a.T @ g[:, rows].double()
+    rel = (gw[cols][:, rows].double() - want) / want
+    assert abs(float(rel.mean())) <= (48 + 2 * 1536 * 2.0 ** -7 + 6 * 9 / 20) * U
+    assert float(rel.abs().max()) <= (48 + 2 * 1536 * 2.0 ** -7 + 6 * 9) * U
