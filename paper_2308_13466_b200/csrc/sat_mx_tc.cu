@@ -40,6 +40,7 @@
 #define MXT_GROUPS 2                 /* groups of four converting warps, a divisor of the slots */
 template <bool TN> constexpr int32_t MXT_RUN = TN ? 12 : 16;   /* stages between two reads of the hi accumulator: 24 instructions, or 32 (one read for 512 terms) */
 #define MXT_REST 32                  /* runs between two reads of the accumulator of mid and lo, which starts anew then */
+#define MXT_TOTAL 32                 /* stages of a group whose column sums are added up by themselves: 256 terms a thread */
 #define MXT_WORKERS (4 * MXT_GROUPS)
 #define MXT_TAKERS 8                 /* warps that add up the runs, behind the converters; then one for the MMAs, for the loads, for the column sums */
 #define MXT_MMA (MXT_WORKERS + MXT_TAKERS)
@@ -385,7 +386,8 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
         const bool sums = TN && a.colsum && it.d0 == 0, has_q = it.d0 + s.rank * 128 + 16 * place < a.D;
         // how many of this thread's rows there are (NN), or whether its columns are (TN)
         const int32_t end = min(half, a.N - x0), has_x = TN ? (x_col < end ? 8 : 0) : (x_row < end ? (end - 1 - x_row) / x_apart + 1 : 0);
-        float2 total[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        // column sums: of up to MXT_TOTAL stages of this group, and of those before, so that no chain of additions is long
+        float2 total[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, before[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
         for (int32_t k = (group - base) & (MXT_GROUPS - 1); k < it.stages; k += MXT_GROUPS) {
             if (!mxt_wait<20>(&s.sh->raw_full[st], ph, dead, a.status)) return;
@@ -443,12 +445,16 @@ __device__ __forceinline__ void mxt_work(const MxtArgs &a, const MxtMem &s, int 
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->raw_empty[st]);
             mbar_arrive_warp<2>(&s.sh->op_full[st], lane);
+            if (sums && (k + MXT_GROUPS) % (MXT_GROUPS * MXT_TOTAL) < MXT_GROUPS) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) before[h] = __fadd2_rn(before[h], total[h]), total[h] = make_float2(0.f, 0.f);
+            }
             if ((st += MXT_GROUPS) >= MXT_SLOTS) st -= MXT_SLOTS, ph ^= 1u;
         }
         base += it.stages;
         if (sums) {   // the warps' sums of a column are added up by the warp that writes them
             if (!mxt_wait(&s.sh->sums_empty, (turn & 1u) ^ 1u, dead, a.status)) return;
-            *reinterpret_cast<float4 *>(s.sh->sums[warp] + 4 * lane) = make_float4(total[0].x, total[0].y, total[1].x, total[1].y);
+            *reinterpret_cast<float4 *>(s.sh->sums[warp] + 4 * lane) = make_float4(before[0].x + total[0].x, before[0].y + total[0].y, before[1].x + total[1].x, before[1].y + total[1].y);
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.sh->sums_full);
             ++turn;

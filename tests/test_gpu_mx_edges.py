@@ -198,3 +198,10 @@ def test_weight_gradient_of_a_million_rows_does_not_drift(long_gradient):
     rel = (gw[cols][:, rows].double() - want) / want
     assert abs(float(rel.mean())) <= (48 + 2 * 1536 * 2.0 ** -7 + 6 * 9 / 20) * U
     assert float(rel.abs().max()) <= (48 + 2 * 1536 * 2.0 ** -7 + 6 * 9) * U
+
+
+def test_bias_gradient_of_a_million_rows(long_gradient):
+    """A thread adds up to 256 gradients before it adds that to a second sum, of at most a million / 8 / 256 = 489 terms: half a unit each."""
+    _, g, _, gb = long_gradient
+    want = g.double().sum(0)
+    assert float(((gb.double() - want) / want).abs().max()) <= (256 + 489 + 4) * U / 2
