@@ -62,7 +62,6 @@ static_assert(MXT_SMEM <= 227 * 1024, "shared memory");
 struct MxtArgs {
     const uint8_t *scales;
     int64_t ld_scales;
-    int32_t groups;            // of a row of Q
     int32_t D, N;              // columns of Q; columns (TN) or rows (NN) of X
     int32_t K, kps;            // terms, and terms of a split (a multiple of MXT_KB)
     int32_t bn, tiles_d, tiles_n;
@@ -674,7 +673,6 @@ static sat_status mxt_args(sat_ctx *ctx, const sat_mx_matrix *q, int64_t n, int3
 {
     a->scales = q->scales;
     a->ld_scales = q->ld_scales;
-    a->groups = mx_groups(q->d);
     a->D = q->d;
     a->N = (int32_t)n;
     a->K = a->kps = (int32_t)q->rows;
