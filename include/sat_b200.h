@@ -82,10 +82,10 @@ enum { SAT_ACT_NONE = 0, SAT_ACT_RELU = 1 };
  * sat_predict without parameters followed by the plain call, without the [sum_m b_m x d_in] copy.  Not together with the two flags above (SAT_EINVAL). */
 #define SAT_FWD_HALO_CACHED 0x800
 /* ... and SAT_FWD_KEEP8: what is kept of AGG for the backward call is its image in 8 bits (sat_mx_quantise, SAT_MX8), a quarter of the
- * memory.  h_out is the same; sat_layer_bwd then takes the weight gradient from the image (g_W = AGG^^T D, an unbiased few percent off
- * per element of AGG), everything else of it is the same.  The kept form of a layer is that of its last forward call; a change of the
- * flag drops what was kept for the other partitions.  Kept memory per layer: 33 to 36 bytes instead of 128 per 32 columns; one
- * scratch of the largest call's AGG is shared by all layers. */
+ * memory.  h_out is the same; sat_layer_bwd then takes the weight gradient from the image (g_W = AGG^^T D; its elements rounded to nearest, 2^-4 of
+ * themselves or 2^-10 2^e off at most), everything else of it is the same.  The kept form of a layer is that of its last forward call; a change of the
+ * flag drops what was kept for the other partitions.  Kept memory per layer: 33 to 36 bytes instead of 128 per 32 columns.  The context also
+ * holds one fp32 scratch for all layers, until sat_destroy: AGG of the largest call, so that calls for single partitions save the most. */
 #define SAT_FWD_KEEP8 0x1000
 enum { SAT_LOSS_SOFTMAX_CE = 0, SAT_LOSS_SIGMOID_BCE = 1 };
 enum { SAT_ROWS_INNER = 0, SAT_ROWS_HALO = 1 };          /* sat_gather_rows                      */
@@ -530,6 +530,8 @@ sat_status sat_cache_requantise(sat_ctx *ctx, int32_t layer, int32_t age, int32_
  * Nothing saturates, so an element is off by at most 2^-4 |x| (SAT_MX8) or 2^-2 |x| (SAT_MX4) or half the format's least step times 2^e
  * (2^-10 or 2^-2), whichever is more.  A group with an infinity or a NaN has the scale byte 255 and reads as NaN throughout.  The codes 0x7F and
  * 0xFF of SAT_MX8, which sat_mx_quantise does not write but a matrix encoded elsewhere may hold, read as NaN one by one, in contractions too.
+ * Just below 2^128 rounding may go up to q 2^e = 2^128, which fp32 does not hold: from (1 - 2^-5) 2^128 (SAT_MX8) or 0.875 2^128 (SAT_MX4) on an
+ * element reads as an infinity.
  *   codes    DEVICE, row r at byte r * ld_codes: one byte per element (SAT_MX8) or two elements a byte, the even one in the low half
  *            (SAT_MX4), the last group filled up with zeros.  16-byte aligned, ld_codes a multiple of 16 and >= 32 (16) bytes a group
  *   scales   DEVICE, row r at byte r * ld_scales: e + 127 per group.  4-byte aligned, ld_scales a multiple of 4 and >= the groups
@@ -542,7 +544,7 @@ typedef struct sat_mx_matrix {
     int32_t d, ld_codes, ld_scales;
     int32_t format;              /* SAT_MX8 or SAT_MX4 */
 } sat_mx_matrix;
-/* x [q.rows x ld] fp32 -> q, and back (the value nearest to q 2^e, which is itself).  Every finite fp32 value is taken, subnormal ones too. */
+/* x [q.rows x ld] fp32 -> q, and back (q 2^e itself).  Every finite fp32 value is taken, subnormal ones too. */
 sat_status sat_mx_quantise(sat_ctx *ctx, const float *x, int32_t ld, const sat_mx_matrix *q);
 sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int32_t ld);
 /* Contractions with microscaled operands, fp32 results (a hat marks what the codes stand for):
@@ -553,8 +555,9 @@ sat_status sat_mx_dequantise(sat_ctx *ctx, const sat_mx_matrix *q, float *x, int
  *                    C of the product above this is the gradient with respect to A^.
  *   sat_mx_dense_tn  C[A.d x n] (+)= A^^T B[A.rows x n], colsum[n] (+)= 1^T B: weight and bias gradient from a stored input.  C is
  *                    dense row-major, colsum may be NULL; accumulate = 1 adds to both.
- * sat_mx_dense_nt multiplies 4-bit codes exactly and adds in fp32; the other two split fp32 operands into terms that carry all of
- * their 24 bits (what lies below 2^-133 is dropped).  An infinity or a NaN in an fp32 operand makes NaN of every result that it reaches.  Results are bit-reproducible.
+ * sat_mx_dense_nt multiplies 4-bit codes exactly and adds in fp32, 64 products at a time and towards zero: a sum of one sign is low by up to 2^-23 of what
+ * it has come to for every 64 terms.  The other two split fp32 operands into terms that carry all of their 24 bits (what lies below 2^-133 is dropped, in stored operands
+ * too).  An infinity or a NaN in an fp32 operand makes NaN of every result that it reaches.  Results are bit-reproducible.
  * Empty sums (no rows, W without rows) are zero, or the bias.  Calls on one context share its workspaces like all calls of this
  * header: two captured graphs with calls of one context must not run at the same time, and the first call of a size may allocate (make
  * it before a capture).  A later, larger call may move a workspace that a captured graph writes to: capture again behind it, or make the
