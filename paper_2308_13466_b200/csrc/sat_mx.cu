@@ -378,9 +378,9 @@ k_mx_simple(MxSimple p)
 }
 
 // All contractions run on the tensor cores, however narrow and short, where the environment does not say otherwise.  Measured, k_mx_simple against them:
-// A W^ of 1000 x 256 by 256 x 256 in 8 bits 38.4 / 8.0 us, of 1 x 40 by 40 x 256 6.1 / 4.3, of 83947 x 413 by 413 x 1 290 / 47; A^T B of 50758 x 17 by
-// 50758 x 192 100 / 29, of 30 x 100 by 30 x 18 7.6 / 5.0; A^ W^T of 3000 x 64 by 8 16.1 / 4.2.  Where there is least to do k_mx_simple would save a little:
-// A W^ of 2048 x 16 by 16 x 32 4.1 / 5.0 us, A^T B of 3 x 448 by 3 x 18 4.6 / 5.3.
+// A W^ of 1000 x 256 by 256 x 256 in 8 bits 38.6 / 8.5 us, of 1 x 40 by 40 x 256 6.6 / 4.8, of 83947 x 413 by 413 x 1 294 / 51; A^T B of 50758 x 17 by
+// 50758 x 192 101 / 24, of 30 x 100 by 30 x 18 8.1 / 6.3; A^ W^T of 3000 x 64 by 8 16.8 / 4.7.  Where there is least to do k_mx_simple would save a little:
+// A W^ of 2048 x 16 by 16 x 32 4.7 / 5.2 us, A^T B of 3 x 448 by 3 x 18 5.1 / 6.4.
 static bool mx_tc() { return sat_use_tc(16, 16); }
 static sat_status mx_grid(sat_ctx *ctx, int64_t M, int32_t N, int64_t splits, dim3 *grid)
 {

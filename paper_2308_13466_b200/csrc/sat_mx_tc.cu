@@ -7,7 +7,8 @@
 //
 // The tensor core chops its running sum at every instruction (16 terms), always towards zero, so a sum in one accumulator drifts: 612257 terms in 74
 // splits were off by 1e-5 of the result.  Only the products with hi matter for that; those with mid and lo, 2^-8 of them, have an accumulator of their own,
-// and the one of hi is taken out every 12 stages (24 instructions; NN: 16) and added up in registers, rounded to nearest: 5e-7, an fp32 FMA loop's being 1e-6.
+// and the one of hi is taken out every 12 stages (24 instructions; NN: 16) and added up in registers, rounded to nearest: 5e-7 (2-norm against
+// 64 bits; an fp32 product of the library 9e-7).
 // The other one follows every 32 runs: a million terms of one sign in one split were off by 4e-5 where it was taken out at their end only.
 //
 // A pair of CTAs shares a tile of 256 columns of Q (the M side, 128 lanes of TMEM in either CTA) by up to 256 columns (TN) or rows (NN) of
@@ -15,7 +16,9 @@
 // (written by TMA, read once), writes 24 KB and 8 KB of bf16, and the tensor core reads 32 KB (each CTA holds one half of X, and a tile of Q
 // stays in the operand collector for its three products): 104 KB, 830 clocks, against 768 for the MMAs.  (With single CTAs and X as the M side it
 // was 183 KB for as many products.  Loading straight into registers takes 40 KB less, but what it can keep in flight does not cover the latency.)
-// Measured: 1,020 clocks a stage with TN, 1,130 without; 612257 x 256 by 256 225 us, 179250 x 512 x 512 274, at the 1.64 GHz that the power limit leaves.
+// Measured: 1,020 clocks a stage with TN, 1,130 without, the tensor pipe busy 72 and 64 % of the time; what fills the rest is the chain from a load to its MMAs, which
+// is as long for narrow tiles (no counter names one part of it).  612257 x 256 by 256 226 us, 179250 x 512 x 512 278, back to back under the power limit; 199 and 239
+// with pauses.
 //
 // (For NN, one accumulator of all three products, two of them by turns, taken out by four warps that write at once: 90000 x 512 x 512 108 us instead of 128, but
 // 96 chopped additions, 1.3e-6.)
@@ -613,8 +616,8 @@ k_mx_gemm(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUt
 
 // C[j][i] (+)= sum over the splits of part[z][i][j], cs[i] (+)= that of part_cs[z][i], in a fixed order: 128 columns of Q by R of X per block, four columns to
 // a lane, every 16 / R-th split to a warp.  Bound by the L2 and its latency: R = 1 where
-// splits are many, for more loads at once, else 4, for longer pieces of C.  Measured with 1 / 4, gradient included: 73 splits of 256 x 256 18.0 / 21.5 us, of 100 x 128
-// 80.5 / 93; 24 splits of 602 x 256 18.3 / 17.5, 9 of 1024 x 512 58.8 / 53.3.
+// splits are many, for more loads at once, else 4, for longer pieces of C.  Measured with 1 / 4, gradient included: 73 splits of 256 x 256 19.0 / 22.3 us, of 100 x 128
+// 80.0 / 83.9; 24 splits of 602 x 256 63.7 / 63.7, 9 of 1024 x 512 152.3 / 147.5.
 template <int R>
 __global__ void __launch_bounds__(512)
 k_mx_reduce(const float *__restrict__ part, const float *__restrict__ part_cs, int32_t splits, int32_t D, int32_t N, int64_t ld, int add, float *__restrict__ C,
@@ -688,7 +691,7 @@ static sat_status mxt_args(sat_ctx *ctx, const sat_mx_matrix *q, int64_t n, int3
 sat_status sat_mx_tc_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc)
 {
     // Rows a tile: what ends first.  A round of tiles of 256 rows takes a third longer than one of 64, since the codes are converted for either
-    // (512 terms: 12.5 and 9.5 us).  Measured with 64 / 256 rows: 2000 rows by 256 columns 15.8 / 17.6 us, 5000 rows 24.1 / 16.5, 18944 rows 44 / 17.7.
+    // (512 terms: 14.6 and 11.5 us).  Measured with 64 / 256 rows: 2000 rows by 256 columns 11.8 / 15.1 us, 5000 rows 19.0 / 15.5 (128 rows: 14.0), 18944 rows 38.0 / 18.6.
     int32_t bn = 64;
     int64_t best = INT64_MAX;
     for (int32_t b = 64; b <= 256; b *= 2) {
@@ -711,7 +714,7 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
     CUtensorMap map_x, map_q;
     SAT_TRY(mxt_args(ctx, A, n, bn, &a, &map_q));
     // Row splits: what takes the fewest stages in a row on the busiest pair, a split costing about six stages to set up and to add up
-    // (150000 rows of 602 by 256: 141 us, 147 where a split is taken to cost one stage; nothing in it from 20000 rows down)
+    // (150000 rows of 602 by 256: 138.8 us, 139.4 where a split is taken to cost one stage; nothing in it from 20000 rows down)
     const int64_t units = ctx->sms / 2, tiles = a.items, stages = cdiv64(A->rows, MXT_KB);
     int64_t best = 1, best_cost = INT64_MAX;
     for (int64_t s = 1; s <= std::min<int64_t>(2 * units / tiles + 1, cdiv64(stages, 4)); ++s) {
@@ -722,7 +725,7 @@ sat_status sat_mx_tc_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const f
     const int32_t splits = (int32_t)cdiv64(A->rows, a.kps);
     a.items *= splits;
     // One split goes through memory as well, as Q^^T X turned round: a lane holds a column of Q, so writing C itself takes 32 pieces of 32 lines an instruction (40 rows
-    // of 256 by 256: 30 us against 9.8; 30 of 100 by 18 5.0 against 6.1)
+    // of 256 by 256: 30 us against 9.7; 30 of 100 by 18 5.0 against 6.3)
     a.by_x = (a.D + 3) & ~3;
     a.split = a.by_x * n;
     SAT_TRY(sat_ensure(ctx, ctx->buf_splitk, (size_t)splits * (size_t)(a.split + n) * sizeof(float)));
