@@ -205,3 +205,62 @@ def test_bias_gradient_of_a_million_rows(long_gradient):
     _, g, _, gb = long_gradient
     want = g.double().sum(0)
     assert float(((gb.double() - want) / want).abs().max()) <= (256 + 489 + 4) * U / 2
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("m,n,k", [(70, 100, 40000), (300, 33, 16385), (1, 1, 16384)])
+def test_input_gradient_of_many_terms(B, ctx, bits, m, n, k):
+    """The accumulators of the input gradient are read and begun anew several times.  Terms of one sign: a run of 32 instructions is off by two units each
+    at most, the lower terms by 2048 instructions of theirs, 2^-7 of the sum, the runs by half a unit each."""
+    rng = np.random.default_rng(k + bits)
+    w = rng.choice([0.5, 1.0, 1.5, 2.0, 3.0], (k, n)).astype(np.float32)
+    a = (2.0 ** rng.integers(-1, 2, (m, k)) * (1 + 2.0 ** -7 - 2.0 ** -12)).astype(np.float32)
+    wq, wv = _mx(B, w, bits)
+    out = _out(m, n)
+    B.sat_mx_dense_nn(ctx, _dev(a), wq, out)
+    B.sat_sync_status(ctx)
+    want = a.astype(np.float64) @ wv
+    assert np.all(np.abs(_np(out) - want) <= (64 + 2 * 2048 * 2.0 ** -7 + (k / 512 + 3) / 2) * U * want)
+    a = _rows(rng, m, k)
+    B.sat_mx_dense_nn(ctx, _dev(a), wq, out)
+    B.sat_sync_status(ctx)
+    assert np.all(np.abs(_np(out) - a.astype(np.float64) @ wv) <= _bound(a.astype(np.float64), wv, k))
+
+
+@pytest.mark.parametrize("m", [1, 40])
+def test_product_of_many_terms(B, ctx, m):
+    """64 products an addition, in one accumulator (tiles) or a group at a time (a few rows)."""
+    rng = np.random.default_rng(m)
+    k, n = 92000, 45
+    a, w = _rows(rng, m, k), rng.normal(size=(n, k)).astype(np.float32)
+    aq, av = _mx(B, a, 4)
+    wq, wv = _mx(B, w, 4)
+    first, second = _out(m, n), _out(m, n)
+    B.sat_mx_dense_nt(ctx, _dev(a), wq, None, first)
+    B.sat_mx_dense_nt(ctx, aq, wq, None, second)
+    B.sat_sync_status(ctx)
+    assert np.array_equal(_np(first), _np(second))
+    assert np.all(np.abs(_np(first) - av @ wv.T) <= _bound(av, wv.T, k))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_rows_of_a_larger_matrix(B, ctx, bits):
+    """Descriptions of a part of the rows: the others are left as they were and read by nobody."""
+    import torch
+    rng = np.random.default_rng(bits)
+    a, g = _rows(rng, 500, 90), rng.normal(size=(500, 40)).astype(np.float32)
+    whole, values = _mx(B, a, bits)
+    codes, scales = whole._keep
+    fmt = B.SAT_MX8 if bits == 8 else B.SAT_MX4
+    part = B.make_mx(codes[133:400], scales[133:400], 90, fmt)
+    gw, gb, gt = torch.zeros((90, 40), device="cuda"), torch.zeros(40, device="cuda"), _dev(g)
+    B.sat_mx_dense_tn(ctx, part, gt[133:400], gw, gb)
+    want = values[133:400].T @ g[133:400].astype(np.float64)
+    assert np.all(np.abs(_np(gw) - want) <= _bound(values[133:400].T, g[133:400].astype(np.float64), 267))
+    before = codes.clone(), scales.clone()
+    B.sat_mx_quantise(ctx, _dev(2 * a)[133:400], part)
+    B.sat_sync_status(ctx)
+    c, s = mx.quantise(2 * a[133:400], bits)
+    assert np.array_equal(codes[133:400].cpu().numpy()[:, :c.shape[1]], c) and np.array_equal(scales[133:400].cpu().numpy()[:, :s.shape[1]], s)
+    for now, then in zip((codes, scales), before):
+        assert bool(torch.equal(now[:133], then[:133])) and bool(torch.equal(now[400:], then[400:]))
