@@ -14,7 +14,7 @@
  *     are caller-owned (allocated by the caller, e.g. through PyTorch), are never
  *     retained after the call, and must be 16-byte aligned with a leading dimension
  *     (`ld`, in floats) that is a multiple of 4 and >= the row width.
- *   - All floating tensors are fp32, row-major.
+ *   - All floating tensors are fp32, row-major (layer norm, embedding and distillation take rows of 16 bits as well, by their `type`).
  *   - Dense contractions run on the tensor cores with every fp32 operand split into two terms, fp32 accumulation.  Short ones keep
  *     2^-21 of each operand element.  Long ones (384 terms and more; 192 and more in graphs of at least 32,768 nodes; not the
  *     transform of layer 1 nor, up to 383 terms, one to more than 128 columns) and the LSTM's steps over cached projections keep
@@ -103,7 +103,7 @@ sat_status sat_destroy(sat_ctx *ctx);
 const char *sat_last_error(const sat_ctx *ctx);
 /* Waits for the stream and reads the device status word: SAT_ECUDA if any enqueued work failed or a tensor-core kernel
  * gave up waiting on one of its (bounded) barrier waits (sticky: the context is unusable afterwards); SAT_EDATA if
- * sat_codec_decode met a malformed row (reported once, the context stays usable). */
+ * sat_codec_decode met a malformed row, or a token, a teacher's entry or a label lay outside its range (reported once, the context stays usable). */
 sat_status sat_sync_status(sat_ctx *ctx);
 
 /* ---------------------------------------------------------------------------------------
@@ -567,6 +567,74 @@ sat_status sat_mx_dense_nt(sat_ctx *ctx, int64_t m, const float *A, int32_t lda,
 sat_status sat_mx_dense_nn(sat_ctx *ctx, int64_t m, const float *A, int32_t lda, const sat_mx_matrix *W, float *C, int32_t ldc);
 sat_status sat_mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, const float *B, int32_t ldb, float *C, float *colsum, int accumulate);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators beside the layer step (the paper has no counterpart): learned inputs, layer norm and a teacher's logits as the objective, for networks
+ * whose nodes have tokens in place of features, whose hidden rows are normalised, or which learn from a larger network.
+ *
+ * Rows are fp32, bf16 or fp16 (`type`); all arithmetic on them is in fp32, results are rounded once, to nearest.  Parameters, statistics, gradients of
+ * parameters and a teacher's logits are fp32.  Row tensors are DEVICE, 16-byte aligned, `ld` in elements and a multiple of 16 bytes; elements between a
+ * row's width and the next row are neither read nor written.  Results are the same bits every time (no floating-point atomics).  Workspaces are the
+ * context's: two captured graphs with calls of one context must not run at the same time, the first call of a size may allocate (make it before a
+ * capture), and a later, larger call may move a workspace that a captured graph uses (capture again behind it, or make the largest call first).
+ * ------------------------------------------------------------------------------------- */
+enum { SAT_F32 = 0, SAT_BF16 = 1, SAT_F16 = 2 };
+
+/* Layer norm of rows of d elements (1 <= d <= 16384):
+ *     mu = mean(x), s = (mean((x - mu)^2) + eps)^(-1/2), xh = (x - mu) s, y = xh gamma + beta
+ *   gamma, beta  DEVICE [d], 16-byte aligned; NULL: ones, zeros
+ *   mean, rstd   DEVICE [rows], written with mu and s for the backward call; either may be NULL
+ * y may be x.  A row with an infinity or a NaN becomes NaN, no other row does.  Magnitudes up to 2^60 / d are taken without overflow of the squares.
+ *
+ * Backward, from the same x and gamma, what the forward call left in mean and rstd, and g = gradient with respect to y:
+ *     u = g gamma, g_x = s (u - mean(u) - xh mean(u xh)), g_gamma (+)= sum over the rows of g xh, g_beta (+)= sum over the rows of g
+ * g_x may be g, and may be x; any of g_x, g_gamma [d], g_beta [d] may be NULL (not all).  accumulate = 1 adds to g_gamma and g_beta.  No rows: zero sums. */
+sat_status sat_layernorm_fwd(sat_ctx *ctx, int64_t rows, int32_t d, int type, const void *x, int32_t ld_x, const float *gamma, const float *beta, float eps,
+                             void *y, int32_t ld_y, float *mean, float *rstd);
+sat_status sat_layernorm_bwd(sat_ctx *ctx, int64_t rows, int32_t d, int type, const void *x, int32_t ld_x, const void *g, int32_t ld_g, const float *gamma,
+                             const float *mean, const float *rstd, void *g_x, int32_t ld_gx, float *g_gamma, float *g_beta, int accumulate);
+
+/* Embedding lookup: out[i] = scale table[tokens[i]], i < n, d elements a row.
+ *   tokens   DEVICE int32 [n] in [0, vocabulary).  `padding` (any number; -1 where no token pads) gives a row of zeros and has no gradient.  Any other
+ *            token gives a row of zeros too, has no gradient, and sat_sync_status returns SAT_EDATA once.
+ *   table    DEVICE [vocabulary x ld_table], of the same type as out
+ *
+ * sat_token_sort puts the positions of a batch in the order that its gradient is added up in: stable, by token.  The arrays are the caller's (DEVICE), one
+ * order serves any number of sat_embed_bwd calls, of tables of any width:
+ *   tokens [n], index [n]   the tokens in ascending order and where each of them stands in the batch; padding and tokens outside the vocabulary are
+ *                           listed last, as the token `vocabulary`
+ *   seen [vocabulary]       1 for tokens that occur, 0 for others
+ *
+ * sat_embed_bwd: g_table[v] (+)= scale times the sum of g[i] over the positions i of token v, in a fixed order.  g_table DEVICE fp32 [vocabulary x ld_gt],
+ * ld_gt a multiple of 4.  accumulate = 0 writes every row (zeros where a token does not occur), 1 adds to the rows of tokens that do. */
+typedef struct sat_token_order {
+    int32_t *tokens, *index;
+    uint8_t *seen;
+    int64_t n;                /* n < 2^31 - 1, vocabulary < 2^31 - 1 */
+    int32_t vocabulary;
+} sat_token_order;
+sat_status sat_embed_fwd(sat_ctx *ctx, int64_t n, const int32_t *tokens, int32_t vocabulary, int32_t padding, int32_t d, int type, const void *table,
+                         int32_t ld_table, float scale, void *out, int32_t ld_out);
+sat_status sat_token_sort(sat_ctx *ctx, const int32_t *tokens, int32_t padding, const sat_token_order *order);
+sat_status sat_embed_bwd(sat_ctx *ctx, const sat_token_order *order, int32_t d, int type, const void *g, int32_t ld_g, float scale, float *g_table, int32_t ld_gt,
+                         int accumulate);
+
+/* Distillation from a teacher's top logits, the loss and its gradient (beside sat_loss_grad, whose labels it takes as well):
+ *     p = softmax(t / T) over the entries (id, t) of a row, q = softmax(z / T)
+ *     loss_i = (1 - hard) T^2 sum_j p_j (log p_j - log q[id_j])  +  hard (-log softmax(z)[y])
+ *     *loss_sum += sum_i w_i loss_i,   row_loss[i] = loss_i,   g_i = w_i d loss_i / dz_i,   w_i = weight row_weight[i] (weight, without row_weight)
+ *   z            DEVICE [rows x ld_z] of `type`; g the same type, may be z
+ *   top_ids      DEVICE int32 [rows x k], dense, 0 <= k <= 256; a negative id, or a logit of -inf, is no entry.  A class may be named more than once:
+ *                its probabilities add up.  top_logits DEVICE fp32 [rows x k], dense.  A row without entries has no first term.
+ *   labels       DEVICE int32 [rows]; negative: no second term.  May be NULL with hard = 0.
+ *   row_weight   DEVICE [rows] or NULL.  A row of weight 0 has loss 0 and a gradient of zeros whatever its logits are.
+ *   loss_sum     DEVICE double or NULL; row_loss DEVICE [rows] or NULL; g may be NULL (not all three)
+ * 0.001 <= T <= 1000, 0 <= hard <= 1.  Ids and labels >= n_classes count as none and make sat_sync_status return SAT_EDATA once.
+ * Exponentials below 2^-126 of a row's largest are taken as zero.  A logit z of -inf is a
+ * class of probability 0 (an infinite loss where the teacher gives it weight); a row of them, or one with a NaN or +inf, gives NaN for that row. */
+sat_status sat_distill_grad(sat_ctx *ctx, int64_t rows, int32_t n_classes, int type, const void *z, int32_t ld_z, int32_t k, const int32_t *top_ids,
+                            const float *top_logits, float temperature, float hard, const int32_t *labels, const float *row_weight, float weight,
+                            double *loss_sum, float *row_loss, void *g, int32_t ld_g);
+
 /* Bounds-checking debug build (libsat_b200_dbg.so: the same sources compiled with -DSAT_DEBUG_BOUNDS; the paper has no
  * counterpart).  Every index the graph kernels (SpMM, halo-row products, row gather / scatter, per-slot sums) load from an
  * index array is compared with the extent of the matrix it addresses; an index outside it raises a bit of the device status
@@ -590,7 +658,8 @@ sat_status sat_launch_count(sat_ctx *ctx, int64_t *count);
  * so that a timed run can carry the events of one family only. */
 enum { SAT_PROF_SPMM_FWD = 0, SAT_PROF_SPMM_BWD, SAT_PROF_SPMM_HROW, SAT_PROF_GEMM_NN, SAT_PROF_GEMM_NT,
        SAT_PROF_GEMM_TN, SAT_PROF_LSTM_CELL, SAT_PROF_GATHER, SAT_PROF_SCATTER, SAT_PROF_LOSS, SAT_PROF_MASK,
-       SAT_PROF_GEMM_SIDE, SAT_PROF_CODEC, SAT_PROF_PRED_TRAIN, SAT_PROF_GAT, SAT_PROF_MX };
+       SAT_PROF_GEMM_SIDE, SAT_PROF_CODEC, SAT_PROF_PRED_TRAIN, SAT_PROF_GAT, SAT_PROF_MX,
+       SAT_PROF_NORM, SAT_PROF_EMBED };
 int32_t sat_profile_families(void);
 sat_status sat_profile_enable(sat_ctx *ctx, int enable);
 sat_status sat_profile_select(sat_ctx *ctx, uint64_t family_mask);

@@ -50,6 +50,12 @@ class sat_mx_matrix(C.Structure):
                 ("ld_scales", C.c_int32), ("format", C.c_int32)]
 
 
+class sat_token_order(C.Structure):
+    """The positions of a batch of tokens, sorted by token; `_keep` holds the tensors behind the pointers (tokens, index, seen)."""
+    _fields_ = [("tokens", C.c_void_p), ("index", C.c_void_p), ("seen", C.c_void_p), ("n", C.c_int64), ("vocabulary", C.c_int32)]
+
+
+SAT_F32, SAT_BF16, SAT_F16 = 0, 1, 2
 SAT_MX8, SAT_MX4 = 8, 4
 SAT_CELL_LSTM, SAT_CELL_GRU = 0, 1
 SAT_EPOCH_GRAD_HISTORY, SAT_EPOCH_COMMIT, SAT_EPOCH_STEP, SAT_EPOCH_CONTINUE, SAT_EPOCH_KEEP8 = 1, 2, 4, 8, 16
@@ -84,7 +90,7 @@ EXPORTS = [
     "sat_predict_state", "sat_layer_fwd", "sat_layer_bwd", "sat_cache_update", "sat_cache_commit", "sat_cache_state",
     "sat_cache_read", "sat_cache_export", "sat_cache_import", "sat_cache_set_state", "sat_loss_grad", "sat_sgd_step", "sat_sgd_steps",
     "sat_dense_nn", "sat_dense_nt", "sat_dense_tn", "sat_dense_tn_static", "sat_launch_count", "sat_profile_families", "sat_profile_enable", "sat_profile_select", "sat_profile_read",
-    "sat_epoch", "sat_codec_plan", "sat_codec_encode", "sat_codec_decode", "sat_cache_requantise", "sat_mx_quantise", "sat_mx_dequantise", "sat_mx_dense_nt", "sat_mx_dense_nn", "sat_mx_dense_tn", "sat_staleness", "sat_pred_grad", "sat_grad_history_read", "sat_grad_history_write", "sat_gat_fwd", "sat_gat_bwd", "sat_gat_scores", "sat_profile_l2_rates", "sat_debug_poke_index", "sat_spmm_plan",
+    "sat_epoch", "sat_codec_plan", "sat_codec_encode", "sat_codec_decode", "sat_cache_requantise", "sat_mx_quantise", "sat_mx_dequantise", "sat_mx_dense_nt", "sat_mx_dense_nn", "sat_mx_dense_tn", "sat_layernorm_fwd", "sat_layernorm_bwd", "sat_embed_fwd", "sat_token_sort", "sat_embed_bwd", "sat_distill_grad", "sat_staleness", "sat_pred_grad", "sat_grad_history_read", "sat_grad_history_write", "sat_gat_fwd", "sat_gat_bwd", "sat_gat_scores", "sat_profile_l2_rates", "sat_debug_poke_index", "sat_spmm_plan",
 ]
 
 
@@ -535,6 +541,105 @@ def sat_mx_dense_tn(ctx, A: sat_mx_matrix, Bm, out, colsum=None, accumulate: boo
     assert _dense(out) and Bm.shape[0] == A.rows and out.shape == (A.d, n)
     assert colsum is None or (_dense(colsum) and colsum.numel() == n)
     _check(ctx, _lib.sat_mx_dense_tn(ctx, C.byref(A), n, *_rows(Bm), out.data_ptr(), None if colsum is None else colsum.data_ptr(), 1 if accumulate else 0))
+
+
+# ---- learned inputs, layer norm, distillation (rows of fp32, bf16 or fp16) -------------------------------------------------------
+_P, _I, _L, _F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+_lib.sat_layernorm_fwd.argtypes = [_P, _L, _I, C.c_int, _P, _I, _P, _P, _F, _P, _I, _P, _P]
+_lib.sat_layernorm_bwd.argtypes = [_P, _L, _I, C.c_int, _P, _I, _P, _I, _P, _P, _P, _P, _I, _P, _P, C.c_int]
+_lib.sat_embed_fwd.argtypes = [_P, _L, _P, _I, _I, _I, C.c_int, _P, _I, _F, _P, _I]
+_lib.sat_token_sort.argtypes = [_P, _P, _I, _P]
+_lib.sat_embed_bwd.argtypes = [_P, _P, _I, C.c_int, _P, _I, _F, _P, _I, C.c_int]
+_lib.sat_distill_grad.argtypes = [_P, _L, _I, C.c_int, _P, _I, _I, _P, _P, _F, _F, _P, _P, _F, _P, _P, _P, _I]
+_ROW_TYPES = {"torch.float32": SAT_F32, "torch.bfloat16": SAT_BF16, "torch.float16": SAT_F16}
+
+
+def _row_type(t) -> int:
+    code = _ROW_TYPES.get(str(t.dtype))
+    assert code is not None, "rows are fp32, bf16 or fp16"
+    return code
+
+
+def _typed(t, like=None):
+    """Pointer and row stride of a CUDA matrix with contiguous rows; of the type and on the device of `like`, where given."""
+    (r, c), (s0, s1) = t.shape, t.stride()
+    assert t.is_cuda and (s1 == 1 or c <= 1) and (like is None or (t.dtype == like.dtype and t.device == like.device))
+    return t.data_ptr(), s0 if r > 1 else max(s0, c)
+
+
+def _f32(t, count: int, like):
+    """Pointer of a CUDA fp32 tensor of `count` elements without gaps, on the device of `like`; None stays None."""
+    if t is None:
+        return None
+    assert t.device == like.device and (f := t.dtype).itemsize == 4 and f.is_floating_point and t.is_contiguous() and t.numel() == count
+    return t.data_ptr()
+
+
+def _i32(t, count: int, like):
+    """... of an int32 tensor"""
+    if t is None:
+        return None
+    assert t.device == like.device and (f := t.dtype).itemsize == 4 and f.is_signed and not f.is_floating_point and t.is_contiguous() and t.numel() == count
+    return t.data_ptr()
+
+
+def sat_layernorm_fwd(ctx, x, gamma, beta, eps: float, y, mean=None, rstd=None):
+    """y = (x - mean(x)) / sqrt(var(x) + eps) gamma + beta by rows; mean and rstd [rows] receive what the backward call takes.  y may be x."""
+    rows, d = x.shape
+    assert y.shape == x.shape
+    _check(ctx, _lib.sat_layernorm_fwd(ctx, rows, d, _row_type(x), *_typed(x), _f32(gamma, d, x), _f32(beta, d, x), eps, *_typed(y, x), _f32(mean, rows, x),
+                                       _f32(rstd, rows, x)))
+
+
+def sat_layernorm_bwd(ctx, x, g, gamma, mean, rstd, g_x=None, g_gamma=None, g_beta=None, accumulate: bool = False):
+    """Gradients of sat_layernorm_fwd from that of y: g_x (may be g or x), and g_gamma, g_beta, overwritten or added to."""
+    rows, d = x.shape
+    assert g.shape == x.shape and (g_x is None or g_x.shape == x.shape)
+    _check(ctx, _lib.sat_layernorm_bwd(ctx, rows, d, _row_type(x), *_typed(x), *_typed(g, x), _f32(gamma, d, x), _f32(mean, rows, x), _f32(rstd, rows, x),
+                                       *((None, 0) if g_x is None else _typed(g_x, x)), _f32(g_gamma, d, x), _f32(g_beta, d, x), 1 if accumulate else 0))
+
+
+def sat_embed_fwd(ctx, tokens, table, scale: float, padding: int, out):
+    """out[i] = scale table[tokens[i]] (tokens: CUDA int32 [n]); a row of zeros where tokens[i] is `padding` (-1: no token pads)."""
+    n, d = out.shape
+    assert table.shape[1] == d
+    _check(ctx, _lib.sat_embed_fwd(ctx, n, _i32(tokens, n, out), table.shape[0], padding, d, _row_type(out), *_typed(table, out), scale, *_typed(out)))
+
+
+def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
+    """Room for the order of n tokens on `device` (default: the current CUDA device)."""
+    import torch
+    assert n >= 0 and vocabulary > 0
+    device = torch.device("cuda") if device is None else device
+    tokens, index = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(2))
+    seen = torch.empty(vocabulary, dtype=torch.uint8, device=device)
+    order = sat_token_order(tokens.data_ptr(), index.data_ptr(), seen.data_ptr(), n, vocabulary)
+    order._keep = (tokens, index, seen)
+    return order
+
+
+def sat_token_sort(ctx, tokens, padding: int, order: sat_token_order):
+    """order <- the positions of tokens (CUDA int32 [n]) by token"""
+    _check(ctx, _lib.sat_token_sort(ctx, _i32(tokens, order.n, order._keep[2]), padding, C.byref(order)))
+
+
+def sat_embed_bwd(ctx, order: sat_token_order, g, scale: float, g_table, accumulate: bool = False):
+    """g_table (CUDA fp32 [vocabulary, d]) (+)= scale times the sum of the rows of g by token"""
+    n, d = g.shape
+    assert n == order.n and g_table.shape == (order.vocabulary, d) and g_table.device == g.device
+    _check(ctx, _lib.sat_embed_bwd(ctx, C.byref(order), d, _row_type(g), *_typed(g), scale, *_rows(g_table), 1 if accumulate else 0))
+
+
+def sat_distill_grad(ctx, z, top_ids, top_logits, temperature: float, hard: float, labels, row_weight, weight: float, loss_sum=None, g=None, row_loss=None):
+    """Loss between the logits z and a teacher's top logits (CUDA int32 and fp32 [rows, k]) and, with weight `hard`, the labels (CUDA int32 [rows] or
+    None); loss_sum (CUDA float64 scalar) += the weighted sum, row_loss [rows] the rows' losses, g the gradient (may be z)."""
+    rows, classes = z.shape
+    k = 0 if top_ids is None else top_ids.shape[1]
+    assert (g is None or g.shape == z.shape) and (loss_sum is None or (loss_sum.device == z.device and loss_sum.dtype.itemsize == 8 and loss_sum.dtype.is_floating_point
+                                                                       and loss_sum.numel() == 1))
+    _check(ctx, _lib.sat_distill_grad(ctx, rows, classes, _row_type(z), *_typed(z), k, _i32(top_ids, rows * k, z), _f32(top_logits, rows * k, z), temperature, hard,
+                                      _i32(labels, rows, z), _f32(row_weight, rows, z), weight, None if loss_sum is None else loss_sum.data_ptr(),
+                                      _f32(row_loss, rows, z), *((None, 0) if g is None else _typed(g, z))))
 
 
 def sat_dense_tn_static(stream: int, A, Bm, out):

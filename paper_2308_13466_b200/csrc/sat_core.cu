@@ -211,6 +211,10 @@ extern "C" sat_status sat_destroy(sat_ctx *ctx)
     sat_free_buf(ctx->buf_misc);
     sat_free_buf(ctx->buf_mx);
     sat_free_buf(ctx->buf_agg);
+    sat_free_buf(ctx->buf_norm);
+    sat_free_buf(ctx->buf_tokens);
+    sat_free_buf(ctx->buf_embed);
+    sat_free_buf(ctx->buf_distill);
     sat_free_buf(ctx->buf_colsum);
     sat_free_buf(ctx->buf_dmask);
     sat_free_buf(ctx->buf_wsplit);
@@ -242,6 +246,10 @@ extern "C" sat_status sat_sync_status(sat_ctx *ctx)
     if (*ctx->h_flag & 1) {
         ctx->cuda_failed = true;
         return sat_fail(ctx, SAT_ECUDA, "a tensor-core kernel gave up waiting on a barrier (status %d)", *ctx->h_flag);
+    }
+    if (*ctx->h_flag & 8) {  // reported once, the other bits stay for the next call
+        SAT_CUDA(ctx, cudaMemsetAsync(ctx->d_flag + 1, *ctx->h_flag & 7, 1, ctx->stream));
+        return sat_fail(ctx, SAT_EDATA, "a token, an entry of a teacher's row or a label lies outside its range");
     }
     if (*ctx->h_flag & 4) {  // debug build only: an index outside its matrix was met (and replaced by 0); reported once
         SAT_CUDA(ctx, cudaMemsetAsync(ctx->d_flag + 1, 0, sizeof(int), ctx->stream));
@@ -285,7 +293,7 @@ extern "C" sat_status sat_launch_count(sat_ctx *ctx, int64_t *count)
 // per-family device timing
 // =====================================================================================
 static const char *k_family_names[SATK_COUNT] = {"spmm_fwd", "spmm_bwd", "spmm_hrow", "gemm_nn", "gemm_nt", "gemm_tn",
-                                                 "lstm_cell", "gather", "scatter", "loss", "mask", "gemm_side", "codec", "pred_train", "gat", "mx"};
+                                                 "lstm_cell", "gather", "scatter", "loss", "mask", "gemm_side", "codec", "pred_train", "gat", "mx", "norm", "embed"};
 
 static void prof_clear(sat_ctx *ctx)
 {

@@ -3,6 +3,7 @@
 #include <cstdlib>
 
 #include "sat_internal.h"
+#include "sat_loss.h"
 
 #include <algorithm>
 #include <cstdlib>
@@ -1079,43 +1080,6 @@ extern "C" sat_status sat_dense_tn(sat_ctx *ctx, int64_t rows, int32_t m, int32_
 // =====================================================================================
 // loss seed, parameter step
 // =====================================================================================
-// Loss kernels.  The rows go round-robin over the lane groups of at most LOSS_MAX_BLOCKS blocks (one resident wave).  Row losses
-// are summed in double per thread, then per warp, the warps of a block in fixed order, and the last block to finish adds the block
-// partials in fixed order: which rows a thread owns depends on the row count alone, so the total does not depend on scheduling.
-#define LOSS_MAX_BLOCKS(ctx) ((ctx)->sms * 6)
-
-__device__ __forceinline__ void loss_finish(double thread_sum, double *__restrict__ block_partial, int *__restrict__ ticket, double *total, int overwrite)
-{
-    __shared__ double red[256];
-    __shared__ int last;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int o = 16; o > 0; o >>= 1) thread_sum += __shfl_xor_sync(0xffffffffu, thread_sum, o);
-    if (lane == 0) red[warp] = thread_sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double s = 0.0;
-        for (int w = 0; w < 8; ++w) s += red[w];
-        block_partial[blockIdx.x] = s;
-        __threadfence();
-        last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double s = 0.0;
-    for (unsigned i = threadIdx.x; i < gridDim.x; i += 256) s += __ldcg(block_partial + i);
-    red[threadIdx.x] = s;
-    __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-        if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) {
-        *ticket = 0;   // the next launch on this stream starts from zero again
-        if (total) *total = overwrite ? red[0] : *total + red[0];
-    }
-}
-
 // Softmax cross-entropy, up to 8 CPL classes: eight lanes hold a row in registers, one exponential per class.  Bound by HBM (z in,
 // g out) and instruction issue; a warp per row spent most of its instructions in the two five-step reductions of a row
 // (612 k rows x 47 classes: 136 us).
