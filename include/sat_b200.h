@@ -572,8 +572,8 @@ sat_status sat_mx_dense_tn(sat_ctx *ctx, const sat_mx_matrix *A, int32_t n, cons
  * whose nodes have tokens in place of features, whose hidden rows are normalised, or which learn from a larger network.
  *
  * Rows are fp32, bf16 or fp16 (`type`); all arithmetic on them is in fp32, results are rounded once, to nearest.  Parameters, statistics, gradients of
- * parameters and a teacher's logits are fp32.  Row tensors are DEVICE, 16-byte aligned, `ld` in elements and a multiple of 16 bytes; elements between a
- * row's width and the next row are neither read nor written.  Results are the same bits every time (no floating-point atomics).  Workspaces are the
+ * parameters and a teacher's logits are fp32.  Row tensors are DEVICE, 16-byte aligned, `ld` in elements and a multiple of 16 bytes; what lies
+ * between a row's width and the next row is not written and does not matter.  Results are the same bits every time (no floating-point atomics).  Workspaces are the
  * context's: two captured graphs with calls of one context must not run at the same time, the first call of a size may allocate (make it before a
  * capture), and a later, larger call may move a workspace that a captured graph uses (capture again behind it, or make the largest call first).
  * ------------------------------------------------------------------------------------- */
@@ -602,13 +602,11 @@ sat_status sat_layernorm_bwd(sat_ctx *ctx, int64_t rows, int32_t d, int type, co
  * order serves any number of sat_embed_bwd calls, of tables of any width:
  *   tokens [n], index [n]   the tokens in ascending order and where each of them stands in the batch; padding and tokens outside the vocabulary are
  *                           listed last, as the token `vocabulary`
- *   seen [vocabulary]       1 for tokens that occur, 0 for others
  *
  * sat_embed_bwd: g_table[v] (+)= scale times the sum of g[i] over the positions i of token v, in a fixed order.  g_table DEVICE fp32 [vocabulary x ld_gt],
  * ld_gt a multiple of 4.  accumulate = 0 writes every row (zeros where a token does not occur), 1 adds to the rows of tokens that do. */
 typedef struct sat_token_order {
     int32_t *tokens, *index;
-    uint8_t *seen;
     int64_t n;                /* n < 2^31 - 1, vocabulary < 2^31 - 1 */
     int32_t vocabulary;
 } sat_token_order;

@@ -37,13 +37,11 @@ def embed_bwd(tokens, g, scale, padding, vocabulary):
 
 
 def token_order(tokens, padding, vocabulary):
-    """(sorted tokens, positions, seen): stable, padding and tokens outside the vocabulary last, as `vocabulary`"""
+    """(sorted tokens, positions): stable, padding and tokens outside the vocabulary last, as `vocabulary`"""
     ok = (tokens != padding) & (tokens >= 0) & (tokens < vocabulary)
     key = np.where(ok, tokens, vocabulary)
     index = np.argsort(key, kind="stable")
-    seen = np.zeros(vocabulary, dtype=np.uint8)
-    seen[tokens[ok]] = 1
-    return key[index], index, seen
+    return key[index], index
 
 
 def _log_softmax(v):

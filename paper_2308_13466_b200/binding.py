@@ -51,8 +51,8 @@ class sat_mx_matrix(C.Structure):
 
 
 class sat_token_order(C.Structure):
-    """The positions of a batch of tokens, sorted by token; `_keep` holds the tensors behind the pointers (tokens, index, seen)."""
-    _fields_ = [("tokens", C.c_void_p), ("index", C.c_void_p), ("seen", C.c_void_p), ("n", C.c_int64), ("vocabulary", C.c_int32)]
+    """The positions of a batch of tokens, sorted by token; `_keep` holds the tensors behind the pointers (tokens, index)."""
+    _fields_ = [("tokens", C.c_void_p), ("index", C.c_void_p), ("n", C.c_int64), ("vocabulary", C.c_int32)]
 
 
 SAT_F32, SAT_BF16, SAT_F16 = 0, 1, 2
@@ -612,15 +612,14 @@ def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
     assert n >= 0 and vocabulary > 0
     device = torch.device("cuda") if device is None else device
     tokens, index = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(2))
-    seen = torch.empty(vocabulary, dtype=torch.uint8, device=device)
-    order = sat_token_order(tokens.data_ptr(), index.data_ptr(), seen.data_ptr(), n, vocabulary)
-    order._keep = (tokens, index, seen)
+    order = sat_token_order(tokens.data_ptr(), index.data_ptr(), n, vocabulary)
+    order._keep = (tokens, index)
     return order
 
 
 def sat_token_sort(ctx, tokens, padding: int, order: sat_token_order):
     """order <- the positions of tokens (CUDA int32 [n]) by token"""
-    _check(ctx, _lib.sat_token_sort(ctx, _i32(tokens, order.n, order._keep[2]), padding, C.byref(order)))
+    _check(ctx, _lib.sat_token_sort(ctx, _i32(tokens, order.n, order._keep[0]), padding, C.byref(order)))
 
 
 def sat_embed_bwd(ctx, order: sat_token_order, g, scale: float, g_table, accumulate: bool = False):

@@ -76,35 +76,48 @@ extern "C" sat_status sat_embed_fwd(sat_ctx *ctx, int64_t n, const int32_t *toke
 
 // =====================================================================================
 // order of the tokens: digits of up to 11 bits from the lowest up, each pass stable
-//   k_tok_count   how often every digit occurs in each tile of keys, and (first pass) which tokens occur at all
+//   k_tok_count   how often every digit occurs in each tile of keys
 //   k_tok_prefix  running sums over the tiles, digit by digit
 //   k_tok_place   every key to its place
 // Keys that pad or lie outside the vocabulary take the place of the token `vocabulary`, behind all others.
 // =====================================================================================
-#define TOK_TILE 4096
+#define TOK_TILE 2048
 #define TOK_WARPS 8
 #define TOK_ROUNDS (TOK_TILE / (TOK_WARPS * 32))
 #define TOK_BITS 11
 
 struct TokPass {
     const int32_t *tokens;      // first pass: the caller's tokens
-    const int32_t *keys, *vals; // later ones: what the pass before left
-    int32_t *keys_out, *vals_out;
+    const int2 *pairs;          // later ones: {key, position} as the pass before left them
+    int32_t *keys_out, *vals_out;   // last pass
+    int2 *pairs_out;                // the others
     int64_t n;
     int32_t vocabulary, padding;
-    int shift, bits, first, last;
+    int shift, bits, first;
     int32_t tiles;
     int32_t *count;             // [digits][tiles]; k_tok_prefix: running sums
     int32_t *total;             // [digits]
-    uint8_t *seen;              // [vocabulary]
     int *status;
 };
 
-__device__ __forceinline__ int32_t tok_key(const TokPass &p, int64_t i)
+// {key, position} of entry i
+__device__ __forceinline__ int2 tok_pair(const TokPass &p, int64_t i)
 {
-    if (!p.first) return __ldg(p.keys + i);
+    if (!p.first) return __ldg(p.pairs + i);
     const int32_t t = __ldg(p.tokens + i);
-    return t == p.padding || (uint32_t)t >= (uint32_t)p.vocabulary ? p.vocabulary : t;
+    return make_int2(t == p.padding || (uint32_t)t >= (uint32_t)p.vocabulary ? p.vocabulary : t, (int32_t)i);
+}
+
+// lanes of the warp with the same digit (of `bits` bits; all lanes call)
+__device__ __forceinline__ unsigned tok_same(int digit, int bits)
+{
+    unsigned same = 0xffffffffu;
+    for (int b = 0; b <= bits; ++b) {   // one bit more: lanes without a key have it
+        const bool one = (digit >> b) & 1;
+        const unsigned with = __ballot_sync(0xffffffffu, one);
+        same &= one ? with : ~with;
+    }
+    return same;
 }
 
 __global__ void __launch_bounds__(TOK_WARPS * 32)
@@ -115,19 +128,26 @@ k_tok_count(TokPass p)
     const int digits = 1 << p.bits;
     for (int i = threadIdx.x; i < digits; i += TOK_WARPS * 32) tok_smem[i] = 0;
     __syncthreads();
-    if (p.first) {   // no token has been seen
-        const int64_t per = ((int64_t)p.vocabulary + p.tiles - 1) / p.tiles, lo = per * blockIdx.x, hi = lo + per < p.vocabulary ? lo + per : p.vocabulary;
-        for (int64_t i = lo + threadIdx.x; i < hi; i += TOK_WARPS * 32) p.seen[i] = 0;
-    }
-    for (int u = threadIdx.x; u < TOK_TILE; u += TOK_WARPS * 32) {
-        const int64_t i = (int64_t)blockIdx.x * TOK_TILE + u;
-        if (i >= p.n) break;
+    int32_t key[TOK_ROUNDS];
+    bool outside = false;
+#pragma unroll
+    for (int r = 0; r < TOK_ROUNDS; ++r) {
+        const int64_t i = (int64_t)blockIdx.x * TOK_TILE + r * (TOK_WARPS * 32) + threadIdx.x;
+        key[r] = -1;
+        if (i >= p.n) continue;
         if (p.first) {
-            const int32_t t = p.tokens[i];
-            if (t != p.padding && (uint32_t)t >= (uint32_t)p.vocabulary) atomicOr(p.status, 8);
+            const int32_t t = __ldg(p.tokens + i);
+            const bool none = (uint32_t)t >= (uint32_t)p.vocabulary;
+            outside |= none && t != p.padding;
+            key[r] = none || t == p.padding ? p.vocabulary : t;
+        } else {
+            key[r] = __ldg(p.pairs + i).x;
         }
-        atomicAdd(tok_smem + ((tok_key(p, i) >> p.shift) & (digits - 1)), 1);
     }
+    if (outside) atomicOr(p.status, 8);
+#pragma unroll
+    for (int r = 0; r < TOK_ROUNDS; ++r)
+        if (key[r] >= 0) atomicAdd(tok_smem + ((key[r] >> p.shift) & (digits - 1)), 1);
     __syncthreads();
     for (int i = threadIdx.x; i < digits; i += TOK_WARPS * 32) p.count[(int64_t)i * p.tiles + blockIdx.x] = tok_smem[i];
 }
@@ -164,34 +184,41 @@ k_tok_place(TokPass p)
     uint16_t *mine = reinterpret_cast<uint16_t *>(tok_smem + digits) + warp * digits;
     for (int i = lane; i < digits; i += 32) mine[i] = 0;
     __syncwarp();
+    // the digits that this thread has to place: how many keys have each, and how many of them lie in tiles before this one
+    constexpr int PER = (1 << TOK_BITS) / (TOK_WARPS * 32);
+    const int per = digits / (TOK_WARPS * 32) > 0 ? digits / (TOK_WARPS * 32) : 1, d0 = threadIdx.x * per;
+    int32_t total[PER], ahead[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool there = i < per && d0 + i < digits;
+        total[i] = there ? __ldcg(p.total + d0 + i) : 0;
+        ahead[i] = there ? __ldcg(p.count + (int64_t)(d0 + i) * p.tiles + blockIdx.x) : 0;
+    }
     // within the warp: keys of the same digit before this one, in this round and the rounds before
-    int32_t key[TOK_ROUNDS];
+    int32_t key[TOK_ROUNDS], val[TOK_ROUNDS];
     uint16_t rank[TOK_ROUNDS];
     const int64_t base = (int64_t)blockIdx.x * TOK_TILE + warp * (TOK_ROUNDS * 32);
 #pragma unroll
     for (int r = 0; r < TOK_ROUNDS; ++r) {
         const int64_t i = base + r * 32 + lane;
-        key[r] = i < p.n ? tok_key(p, i) : -1;
+        const int2 pair = i < p.n ? tok_pair(p, i) : make_int2(-1, 0);
+        key[r] = pair.x, val[r] = pair.y;
     }
 #pragma unroll
     for (int r = 0; r < TOK_ROUNDS; ++r) {
-        const int digit = key[r] < 0 ? -1 : (key[r] >> p.shift) & (digits - 1);
-        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        const int digit = key[r] < 0 ? digits : (key[r] >> p.shift) & (digits - 1);
+        const unsigned same = tok_same(digit, p.bits);
         const int before = __popc(same & ((1u << lane) - 1));
-        const int had = digit < 0 ? 0 : mine[digit];
+        const int had = key[r] < 0 ? 0 : mine[digit];
         __syncwarp();
-        if (digit >= 0 && before == 0) mine[digit] = (uint16_t)(had + __popc(same));
+        if (key[r] >= 0 && before == 0) mine[digit] = (uint16_t)(had + __popc(same));
         __syncwarp();
         rank[r] = (uint16_t)(had + before);
-        if (p.last) {   // (one lane for several of a kind, where they are side by side)
-            const int32_t left = __shfl_up_sync(0xffffffffu, key[r], 1);
-            if ((lane == 0 || left != key[r]) && (uint32_t)key[r] < (uint32_t)p.vocabulary) p.seen[key[r]] = 1;
-        }
     }
     // first place of every digit: of all keys with lower digits, then of the tiles before this one
     int32_t run = 0;
-    const int per = digits / (TOK_WARPS * 32) > 0 ? digits / (TOK_WARPS * 32) : 1, d0 = threadIdx.x * per;
-    for (int i = 0; i < per; ++i) run += d0 + i < digits ? p.total[d0 + i] : 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) run += total[i];
     int32_t s = run;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -202,10 +229,11 @@ k_tok_place(TokPass p)
     __syncthreads();
     s -= run;
     for (int w = 0; w < warp; ++w) s += wsum[w];
-    for (int i = 0; i < per; ++i)
-        if (d0 + i < digits) {
-            tok_smem[d0 + i] = s + p.count[(int64_t)(d0 + i) * p.tiles + blockIdx.x];
-            s += p.total[d0 + i];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (i < per && d0 + i < digits) {
+            tok_smem[d0 + i] = s + ahead[i];
+            s += total[i];
         }
     // counts of the warps before
     const uint16_t *all = reinterpret_cast<const uint16_t *>(tok_smem + digits);
@@ -216,15 +244,117 @@ k_tok_place(TokPass p)
         const int digit = (key[r] >> p.shift) & (digits - 1);
         int32_t at = tok_smem[digit] + rank[r];
         for (int w = 0; w < warp; ++w) at += all[w * digits + digit];
-        p.keys_out[at] = key[r];
-        p.vals_out[at] = p.first ? (int32_t)(base + r * 32 + lane) : __ldg(p.vals + base + r * 32 + lane);
+        if (p.pairs_out) {
+            p.pairs_out[at] = make_int2(key[r], val[r]);
+        } else {
+            p.keys_out[at] = key[r];
+            p.vals_out[at] = val[r];
+        }
+    }
+}
+
+// A batch of up to TOK_SMALL: one block does all of it, keys and positions in shared memory between passes over digits of up to eight bits.
+#define TOK_SMALL 4096
+#define TOK_SMALL_ROUNDS (TOK_SMALL / 1024)
+__global__ void __launch_bounds__(1024)
+k_tok_small(TokPass p, int all_bits)
+{
+    sat_grid_wait();
+    __shared__ uint16_t cnt[32 * 256];      // [digit][warp]
+    __shared__ int32_t keys[TOK_SMALL];
+    __shared__ uint16_t vals[TOK_SMALL];
+    __shared__ int32_t wsum[32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)p.n;
+    const int rounds = (n + 1023) / 1024, base = warp * rounds * 32;   // a warp's keys are side by side
+    int32_t key[TOK_SMALL_ROUNDS];
+    uint16_t val[TOK_SMALL_ROUNDS], rank[TOK_SMALL_ROUNDS];
+#pragma unroll
+    for (int r = 0; r < TOK_SMALL_ROUNDS; ++r) {
+        const int i = base + r * 32 + lane;
+        key[r] = -1;
+        val[r] = (uint16_t)i;
+        if (r < rounds && i < n) {
+            const int32_t t = __ldg(p.tokens + i);
+            const bool outside = (uint32_t)t >= (uint32_t)p.vocabulary;
+            if (outside && t != p.padding) atomicOr(p.status, 8);
+            key[r] = outside || t == p.padding ? p.vocabulary : t;
+        }
+    }
+    const int passes = (all_bits + 7) / 8;
+    for (int k = 0, shift = 0; k < passes; ++k) {
+        const int bits = (all_bits - shift + passes - k - 1) / (passes - k), digits = 1 << bits;
+        for (int i = threadIdx.x; i < 32 * digits; i += 1024) cnt[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < TOK_SMALL_ROUNDS; ++r) {
+            if (r >= rounds) break;
+            const int digit = key[r] < 0 ? digits : (key[r] >> shift) & (digits - 1);
+            const unsigned same = tok_same(digit, bits);
+            const int before = __popc(same & ((1u << lane) - 1));
+            const int had = key[r] < 0 ? 0 : cnt[digit * 32 + warp];
+            __syncwarp();
+            if (key[r] >= 0 && before == 0) cnt[digit * 32 + warp] = (uint16_t)(had + __popc(same));
+            __syncwarp();
+            rank[r] = (uint16_t)(had + before);
+        }
+        __syncthreads();
+        // running sums over [digit][warp]: eight counts a thread
+        int sum = 0;
+        uint16_t mine[8];
+        const int i0 = threadIdx.x * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            mine[i] = i0 < 32 * digits ? cnt[i0 + i] : 0;
+            sum += mine[i];
+        }
+        int run = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int w = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += w;
+        }
+        if (lane == 31) wsum[warp] = run;
+        __syncthreads();
+        int ahead = lane < warp ? wsum[lane] : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) ahead += __shfl_xor_sync(0xffffffffu, ahead, o);
+        run += ahead - sum;
+        if (i0 < 32 * digits) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                cnt[i0 + i] = (uint16_t)run;
+                run += mine[i];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < TOK_SMALL_ROUNDS; ++r) {
+            if (key[r] < 0) continue;
+            const int at = cnt[((key[r] >> shift) & (digits - 1)) * 32 + warp] + rank[r];
+            keys[at] = key[r];
+            vals[at] = val[r];
+        }
+        __syncthreads();
+        shift += bits;
+#pragma unroll
+        for (int r = 0; r < TOK_SMALL_ROUNDS; ++r) {
+            const int i = base + r * 32 + lane;
+            if (r < rounds && i < n) key[r] = keys[i], val[r] = vals[i];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < TOK_SMALL_ROUNDS; ++r) {
+        const int i = base + r * 32 + lane;
+        if (r >= rounds || i >= n) continue;
+        p.keys_out[i] = key[r];
+        p.vals_out[i] = val[r];
     }
 }
 
 static sat_status order_check(sat_ctx *ctx, const sat_token_order *o, const char *who)
 {
     if (!o || o->n < 0 || o->n >= INT32_MAX || !embed_vocabulary_ok(o->vocabulary)) return sat_fail(ctx, SAT_EINVAL, "%s: no order of tokens, or one of bad size", who);
-    if (!o->seen || (o->n > 0 && (!o->tokens || !o->index))) return sat_fail(ctx, SAT_EINVAL, "%s: null array in the order of tokens", who);
+    if (o->n > 0 && (!o->tokens || !o->index)) return sat_fail(ctx, SAT_EINVAL, "%s: null array in the order of tokens", who);
     return SAT_OK;
 }
 
@@ -235,28 +365,32 @@ extern "C" sat_status sat_token_sort(sat_ctx *ctx, const int32_t *tokens, int32_
     const int64_t n = order->n;
     if (n > 0 && !tokens) return sat_fail(ctx, SAT_EINVAL, "sat_token_sort: null tokens");
     ProfScope prof(ctx, SATK_EMBED, 12.0 * (double)n, 0.0);
-    if (n == 0) {
-        SAT_CUDA(ctx, cudaMemsetAsync(order->seen, 0, (size_t)order->vocabulary, ctx->stream));
-        return SAT_OK;
-    }
+    if (n == 0) return SAT_OK;
     int all = 1;   // bits of the largest key, which is `vocabulary`
     while (all < 31 && (order->vocabulary >> all) != 0) ++all;
+    TokPass p = {};
+    p.tokens = tokens, p.n = n, p.vocabulary = order->vocabulary, p.padding = padding, p.status = ctx->d_flag + 1;
+    if (n <= TOK_SMALL) {
+        p.keys_out = order->tokens, p.vals_out = order->index;
+        sat_pdl(ctx->stream, k_tok_small, 1, 1024, 0)(p, all);
+        SAT_LAUNCHED(ctx);
+        return SAT_OK;
+    }
     const int passes = (all + TOK_BITS - 1) / TOK_BITS;
     const int32_t tiles = (int32_t)cdiv64(n, TOK_TILE);
     const size_t counts = ((size_t)tiles + 1) << TOK_BITS;
-    SAT_TRY(sat_ensure(ctx, ctx->buf_tokens, (counts + (passes > 1 ? 2 * (size_t)n : 0)) * sizeof(int32_t)));
-    int32_t *count = (int32_t *)ctx->buf_tokens.p, *tmp = count + counts;
-    TokPass p = {};
-    p.tokens = tokens, p.n = n, p.vocabulary = order->vocabulary, p.padding = padding, p.tiles = tiles, p.count = count, p.seen = order->seen;
-    p.status = ctx->d_flag + 1;
+    SAT_TRY(sat_ensure(ctx, ctx->buf_tokens, counts * sizeof(int32_t) + (passes > 2 ? 2 : passes - 1) * (size_t)n * sizeof(int2)));
+    int32_t *count = (int32_t *)ctx->buf_tokens.p;
+    int2 *tmp = (int2 *)(count + counts);
+    p.keys_out = order->tokens, p.vals_out = order->index;
+    p.tiles = tiles, p.count = count;
     for (int k = 0, shift = 0; k < passes; ++k) {
         p.shift = shift;
         p.bits = (all - shift + passes - k - 1) / (passes - k);
         shift += p.bits;
         p.total = count + ((size_t)tiles << p.bits);
-        p.first = k == 0, p.last = k == passes - 1;
-        const bool to_tmp = ((passes - 1 - k) & 1) != 0;   // the last pass ends in the caller's arrays
-        p.keys_out = to_tmp ? tmp : order->tokens, p.vals_out = to_tmp ? tmp + n : order->index;
+        p.first = k == 0;
+        p.pairs_out = k == passes - 1 ? nullptr : tmp + (k & 1) * n;
         const int digits = 1 << p.bits;
         sat_pdl(ctx->stream, k_tok_count, (unsigned)tiles, TOK_WARPS * 32, (size_t)digits * 4)(p);
         SAT_LAUNCHED(ctx);
@@ -264,169 +398,288 @@ extern "C" sat_status sat_token_sort(sat_ctx *ctx, const int32_t *tokens, int32_
         SAT_LAUNCHED(ctx);
         sat_pdl(ctx->stream, k_tok_place, (unsigned)tiles, TOK_WARPS * 32, (size_t)digits * (4 + 2 * TOK_WARPS))(p);
         SAT_LAUNCHED(ctx);
-        p.keys = p.keys_out, p.vals = p.vals_out;
+        p.pairs = p.pairs_out;
     }
     return SAT_OK;
 }
 
 // =====================================================================================
-// gradient of the table: the sorted positions are cut into runs of EMB_RUN; TPR lanes walk one, a piece of 16 bytes of the row each
+// gradient of the table: the sorted positions are cut into runs of `len`; TPR lanes walk one, a piece of 16 bytes of the row each
 // =====================================================================================
-// A token whose positions lie in one run has its sum written at once; the sums of one that crosses runs go to `part` ([run][2]: 0 where it begins, 1 where
-// it goes on), and k_embed_join adds these up in order.  Further blocks write the rows of tokens that did not occur.
-#define EMB_RUN 32
+// A token belongs to the run that it begins in.  One that crosses a single border is walked to its end by that run, the next one leaves it out.  One that
+// crosses more is long: every run adds up its own part, in `part` ([run][2]: 0 where the token begins, 1 where it goes on), and k_embed_join adds these in
+// order.  Further blocks write the rows of tokens that did not occur.
 #define EMB_AHEAD 8
 struct EmbedBwd {
     const int32_t *tokens, *index;
-    const uint8_t *seen;
     int64_t n;
     int32_t vocabulary, d;
     int64_t ld_g, ld_gt;
     float scale;
     int accumulate;
     float *g_table, *part;
-    int32_t ld_part, slabs;
+    int32_t ld_part, slabs, len;
     int64_t runs;
-    int64_t walk_blocks;   // blocks of the walk; the others write zeros
+    int64_t walk_blocks, zero_blocks;   // blocks of the walk, and those that write zeros, each for zero_rows tokens
+    int32_t zero_rows;
     int *status;
 };
 
-template <typename T>
-__device__ __forceinline__ void embed_put(const EmbedBwd &p, int32_t token, int32_t col, const float (&f)[RowVec<T>::V])
+// the sum of a token's rows, V columns of it, to its place in the table: scaled, or scaled and added
+template <int V>
+__device__ __forceinline__ void embed_put(const EmbedBwd &p, int32_t token, int32_t col, const float (&f)[V])
 {
     float *o = p.g_table + (int64_t)token * p.ld_gt;
 #pragma unroll
-    for (int i = 0; i < RowVec<T>::V; i += 4) {
+    for (int i = 0; i < V; i += 4) {
         const int32_t c = col + i;
         if (c >= p.d) break;
-        float v[4];
-        const bool whole = c + 4 <= p.d;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = f[i + k] * p.scale;
+        float v[4] = {f[i] * p.scale, f[i + 1] * p.scale, f[i + 2] * p.scale, f[i + 3] * p.scale};
         if (p.accumulate) {
-            if (whole) {
-                const float4 old = *reinterpret_cast<const float4 *>(o + c);
-                v[0] += old.x, v[1] += old.y, v[2] += old.z, v[3] += old.w;
-            } else {
-                for (int k = 0; k < 3; ++k)
-                    if (c + k < p.d) v[k] += o[c + k];
-            }
+            float old[4];
+            row_load(o, c, p.d, old);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += old[k];
         }
         row_store(o, c, p.d, v);
     }
 }
 
+// whether the token at border e (a multiple of len with tokens[e - 1] == tokens[e] == t) crosses another border
+__device__ __forceinline__ bool embed_long(const EmbedBwd &p, int64_t e, int32_t t)
+{
+    return (e > p.len && __ldg(p.tokens + e - p.len - 1) == t) || (e + p.len < p.n && __ldg(p.tokens + e + p.len) == t);
+}
+
+// Zeros for the tokens [v0, v0 + zero_rows) that do not occur
+#define EMB_ZERO 2048
+__device__ __forceinline__ int64_t embed_find(const EmbedBwd &p, int64_t lo, int64_t hi, int64_t v)   // the first position in [lo, hi) whose token is v or more
+{
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (__ldg(p.tokens + mid) < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ void embed_zero(const EmbedBwd &p, int64_t v0)
+{
+    __shared__ uint32_t there[EMB_ZERO / 32];
+    __shared__ int64_t ends[2];
+    const int64_t v1 = v0 + p.zero_rows < p.vocabulary ? v0 + p.zero_rows : p.vocabulary;
+    const int lane = threadIdx.x & 31, rows = (int)(v1 - v0);
+    if (threadIdx.x < EMB_ZERO / 32) there[threadIdx.x] = 0;
+    if (threadIdx.x % 32 == 0 && threadIdx.x < 64) ends[threadIdx.x / 32] = embed_find(p, 0, p.n, threadIdx.x ? v1 : v0);
+    __syncthreads();
+    const int64_t p0 = ends[0], p1 = ends[1];
+    if (p1 - p0 <= 8 * (int64_t)rows + 256) {   // few positions: read them all
+        for (int64_t i = p0 + threadIdx.x; i < p1; i += 256) {
+            const int v = (int)(__ldg(p.tokens + i) - v0);
+            if ((uint32_t)v < (uint32_t)rows && (i == p0 || __ldg(p.tokens + i - 1) != v + v0)) atomicOr(there + (v >> 5), 1u << (v & 31));
+        }
+    } else {
+        for (int v = threadIdx.x; v < rows; v += 256) {
+            const int64_t at = embed_find(p, p0, p1, v0 + v);
+            if (at < p1 && __ldg(p.tokens + at) == v0 + v) atomicOr(there + (v >> 5), 1u << (v & 31));
+        }
+    }
+    __syncthreads();
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    const int32_t quads = (p.d + 3) / 4;
+    const int side = quads < 32 ? 32 / quads : 1, mine = quads < 32 ? lane / quads : 0, quad = quads < 32 ? lane % quads : lane;   // narrow rows side by side in a warp
+    for (int w = threadIdx.x >> 5; w * 32 < rows; w += 8) {
+        const uint32_t none = ~there[w] & (rows - w * 32 >= 32 ? 0xffffffffu : (1u << (rows - w * 32)) - 1u);
+        if (none == 0) continue;
+        float *o = p.g_table + (v0 + w * 32) * p.ld_gt;
+        for (int r = mine; r < 32; r += side) {
+            if (!((none >> r) & 1u) || mine >= side) continue;
+            for (int32_t c = 4 * quad; c < p.d; c += 128) row_store(o + (int64_t)r * p.ld_gt, c, p.d, zero);
+        }
+    }
+}
+
 template <typename T, int TPR>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 3)
 k_embed_bwd(EmbedBwd p, const T *__restrict__ g)
 {
     sat_grid_wait();
     constexpr int V = RowVec<T>::V, GROUPS = 256 / TPR;
-    if ((int64_t)blockIdx.x >= p.walk_blocks) {   // 32 tokens a warp
-        const int lane = threadIdx.x & 31;
-        const int64_t v0 = (((int64_t)blockIdx.x - p.walk_blocks) * 8 + (threadIdx.x >> 5)) * 32;
-        unsigned none = __ballot_sync(0xffffffffu, v0 + lane < p.vocabulary && p.seen[v0 + lane < p.vocabulary ? v0 + lane : 0] == 0);
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        while (none) {
-            const int64_t v = v0 + __ffs(none) - 1;
-            none &= none - 1;
-            for (int32_t c = 4 * lane; c < p.d; c += 128) row_store(p.g_table + v * p.ld_gt, c, p.d, zero);
+    const int lane = threadIdx.x & 31, t = lane % TPR;
+    // blocks that walk and blocks that write zeros take turns while there are both
+    int64_t block = blockIdx.x;
+    {
+        const int64_t both = 2 * (p.walk_blocks < p.zero_blocks ? p.walk_blocks : p.zero_blocks);
+        const bool zeros = block < both ? (block & 1) != 0 : p.zero_blocks > p.walk_blocks;
+        block = block < both ? block >> 1 : block - both / 2;
+        if (zeros) {
+            embed_zero(p, block * p.zero_rows);
+            return;
         }
-        return;
     }
-    const int64_t item = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR;   // neighbouring groups: the slabs of a run
+    const unsigned mates = TPR == 32 ? 0xffffffffu : ((1u << (TPR & 31)) - 1u) << (lane - t);
+    const int64_t item = block * GROUPS + threadIdx.x / TPR;   // neighbouring groups: the slabs of a run
     const int64_t run = sat_div(item, p.slabs);
     if (run >= p.runs) return;
-    const int32_t col = ((int32_t)(item - run * p.slabs) * TPR + threadIdx.x % TPR) * V;
-    const int64_t e0 = run * EMB_RUN, e1 = e0 + EMB_RUN < p.n ? e0 + EMB_RUN : p.n;
-    int32_t cur = __ldg(p.tokens + e0);
-    bool goes_on = e0 > 0 && __ldg(p.tokens + e0 - 1) == cur;   // from the run before
+    const int32_t col = ((int32_t)(item - run * p.slabs) * TPR + t) * V;
+    const int64_t e0 = run * p.len, e1 = e0 + p.len < p.n ? e0 + p.len : p.n;
+    const int32_t first = __ldg(p.tokens + e0), last = __ldg(p.tokens + e1 - 1);
+    const bool goes_on = e0 > 0 && __ldg(p.tokens + e0 - 1) == first, leaves = e1 < p.n && __ldg(p.tokens + e1) == last;
+    const bool first_long = goes_on && embed_long(p, e0, first), last_long = leaves && embed_long(p, e1, last);
+    const int64_t end = leaves && !last_long ? (e1 + p.len < p.n ? e1 + p.len : p.n) : e1;   // (the token ends before that)
+    const bool skip = goes_on && !first_long;
     float acc[V] = {};
-    float *part = p.part + run * 2 * p.ld_part + col;
-    for (int64_t e = e0; e < e1; e += EMB_AHEAD) {
-        uint4 raw[EMB_AHEAD];
-        int32_t tok[EMB_AHEAD];
+    int32_t cur = first;
+    bool begun_here = !goes_on;
+    auto put = [&](bool is_last) {   // the sum of `cur`
+        if ((uint32_t)cur >= (uint32_t)p.vocabulary || col >= p.d || (!begun_here && skip)) return;
+        if (!begun_here || (is_last && last_long)) {
+            float *o = p.part + (run * 2 + (begun_here ? 0 : 1)) * p.ld_part + col;
 #pragma unroll
-        for (int u = 0; u < EMB_AHEAD; ++u) {
-            tok[u] = e + u < e1 ? __ldg(p.tokens + e + u) : -1;
-            const int32_t i = e + u < e1 ? __ldg(p.index + e + u) : 0;
-            const bool known = (uint32_t)tok[u] < (uint32_t)p.vocabulary, there = (uint32_t)i < (uint32_t)p.n;   // (the arrays are the caller's)
-            if (known && !there) atomicOr(p.status, 8);
-            raw[u] = known && there ? row_load_raw(g + (int64_t)i * p.ld_g, col, p.d) : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(o + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+        } else {
+            embed_put<V>(p, cur, col, acc);
         }
+    };
+    // Eight rows are on their way at any time.  The lanes hold eight entries each of three batches: the tokens of the one that is added up, the positions of the
+    // one whose rows are asked for in their place one by one, and the one behind that.  What is to be known of an entry is worked out by its lane: where its row
+    // is (none: -1), whether another token begins with it, whether the walk ends before it.
+    const int slot = lane % EMB_AHEAD;
+    uint4 raw[EMB_AHEAD];
+    const T *gc = g + col;
+    const bool inside = col < p.d;
+    auto entries = [&](int64_t e, int32_t &tok, int32_t &idx) {
+        tok = e + slot < end ? __ldg(p.tokens + e + slot) : -1;
+        idx = e + slot < end ? __ldg(p.index + e + slot) : -1;
+        if (e + slot >= e1 && tok != last) tok = -1;   // behind what this run walks
+        if ((uint32_t)tok >= (uint32_t)p.vocabulary || (skip && tok == first)) {
+            idx = -1;
+        } else if ((uint32_t)idx >= (uint32_t)p.n) {   // (the arrays are the caller's)
+            atomicOr(p.status, 8);
+            idx = -1;
+        }
+    };
+    auto fetch = [&](int32_t i) { return i >= 0 && inside ? *reinterpret_cast<const uint4 *>(gc + (int64_t)i * p.ld_g) : make_uint4(0u, 0u, 0u, 0u); };
+    int32_t tok0, tok1, idx1;
+    {
+        int32_t idx0;
+        entries(e0, tok0, idx0);
+        entries(e0 + EMB_AHEAD, tok1, idx1);
+#pragma unroll
+        for (int u = 0; u < EMB_AHEAD; ++u) raw[u] = fetch(__shfl_sync(mates, idx0, u, EMB_AHEAD));
+    }
+    for (int64_t e = e0; e < end; e += EMB_AHEAD) {
+        int32_t tok2, idx2;
+        entries(e + 2 * EMB_AHEAD, tok2, idx2);
+        int32_t left = __shfl_up_sync(mates, tok0, 1, EMB_AHEAD);
+        if (slot == 0) left = cur;
+        const unsigned other = __ballot_sync(mates, tok0 != left) >> (lane & ~(EMB_AHEAD - 1)), none = __ballot_sync(mates, tok0 == -1) >> (lane & ~(EMB_AHEAD - 1));
+        const int count = __ffs((none & ((1u << EMB_AHEAD) - 1u)) | (1u << EMB_AHEAD)) - 1;
 #pragma unroll
         for (int u = 0; u < EMB_AHEAD; ++u) {
-            if (e + u >= e1) break;
-            if (tok[u] != cur) {
-                if ((uint32_t)cur < (uint32_t)p.vocabulary && col < p.d) {
-                    if (goes_on) {
-#pragma unroll
-                        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(part + p.ld_part + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-                    } else {
-                        embed_put<T>(p, cur, col, acc);
-                    }
-                }
-                cur = tok[u];
-                goes_on = false;
+            const uint4 now = raw[u];
+            raw[u] = fetch(__shfl_sync(mates, idx1, u, EMB_AHEAD));
+            if (u >= count) continue;
+            if ((other >> u) & 1u) {
+                put(false);
+                cur = __shfl_sync(mates, tok0, u, EMB_AHEAD);
+                begun_here = true;
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] = 0.f;
             }
             float f[V];
-            RowVec<T>::unpack(raw[u], f);
+            RowVec<T>::unpack(now, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[i] += f[i];
         }
+        if (count < EMB_AHEAD) break;
+        tok0 = tok1, tok1 = tok2, idx1 = idx2;
     }
-    if ((uint32_t)cur >= (uint32_t)p.vocabulary || col >= p.d) return;
-    if (goes_on || (e1 < p.n && __ldg(p.tokens + e1) == cur)) {
-        float *o = part + (goes_on ? p.ld_part : 0);
-#pragma unroll
-        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(o + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-    } else {
-        embed_put<T>(p, cur, col, acc);
-    }
+    put(true);
 }
 
-// A block per border between two runs and 128 columns: where a token crosses the border and begins in the run before it, its sums are added up, eight warps
-// taking every eighth run.
-__global__ void __launch_bounds__(256)
+// The long tokens.  A block looks at EMB_WINDOW borders and 128 columns; a warp adds up a token of up to 32 runs, the block one of more: as many runs at a
+// time as rows of 128 columns or less lie in its warps side by side, these rows' sums in order at the end.
+#define EMB_WINDOW 256
+__global__ void __launch_bounds__(1024)
 k_embed_join(EmbedBwd p)
 {
     sat_grid_wait();
-    __shared__ float4 red[8][32];
+    __shared__ int32_t list[EMB_WINDOW], heavy[EMB_WINDOW];
+    __shared__ int32_t n_list, n_heavy;
+    __shared__ float4 red[1024];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t b = (int64_t)blockIdx.x;                       // border between runs b and b + 1
-    const int64_t at = (b + 1) * EMB_RUN;
-    const int32_t t = __ldg(p.tokens + at);
-    if (__ldg(p.tokens + at - 1) != t || (uint32_t)t >= (uint32_t)p.vocabulary) return;
-    if (__ldg(p.tokens + b * EMB_RUN) == t && b > 0 && __ldg(p.tokens + b * EMB_RUN - 1) == t) return;   // it began earlier
-    const int32_t col = (int32_t)blockIdx.y * 128 + 4 * lane;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (col < p.d) {
-        if (warp == 0) s = __ldcg(reinterpret_cast<const float4 *>(p.part + b * 2 * p.ld_part + col));
-        for (int64_t r = b + 1 + warp; r < p.runs && __ldg(p.tokens + r * EMB_RUN) == t; r += 8) {
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(p.part + (r * 2 + 1) * p.ld_part + col));
-            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-        }
-    }
-    red[warp][lane] = s;
+    if (threadIdx.x == 0) n_list = n_heavy = 0;
     __syncthreads();
-    if (warp == 0 && col < p.d) {
-        for (int w = 1; w < 8; ++w) s.x += red[w][lane].x, s.y += red[w][lane].y, s.z += red[w][lane].z, s.w += red[w][lane].w;
+    const int64_t b0 = (int64_t)blockIdx.x * EMB_WINDOW + 1;
+    if (threadIdx.x < EMB_WINDOW && b0 + threadIdx.x < p.runs) {
+        const int64_t e = (b0 + threadIdx.x) * p.len;
+        const int32_t t = __ldg(p.tokens + e);
+        // its first border, and there is another one
+        if (__ldg(p.tokens + e - 1) == t && (uint32_t)t < (uint32_t)p.vocabulary && !(e > p.len && __ldg(p.tokens + e - p.len - 1) == t) && e + p.len < p.n &&
+            __ldg(p.tokens + e + p.len) == t)
+            list[atomicAdd(&n_list, 1)] = threadIdx.x;   // (in any order: they have nothing to do with one another)
+    }
+    __syncthreads();
+    const int32_t col0 = (int32_t)blockIdx.y * 128, width = p.d - col0 < 128 ? p.d - col0 : 128;
+    auto row = [&](int64_t run, int which, int32_t col) { return __ldcg(reinterpret_cast<const float4 *>(p.part + (run * 2 + which) * p.ld_part + col)); };
+    auto add = [](float4 &s, const float4 &v) { s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w; };
+    for (int i = warp; i < n_list; i += 32) {
+        const int64_t b = b0 + list[i];
+        const int32_t t = __ldg(p.tokens + b * p.len);
+        const bool in = b + lane < p.runs && __ldg(p.tokens + (b + lane) * p.len) == t;
+        const unsigned runs = __ballot_sync(0xffffffffu, in);   // (from the lowest bit up)
+        if (runs == 0xffffffffu) {
+            if (lane == 0) heavy[atomicAdd(&n_heavy, 1)] = list[i];
+            continue;
+        }
+        if (4 * lane >= width) continue;
+        float4 s = row(b - 1, 0, col0 + 4 * lane);
+        const int count = __popc(runs);
+#pragma unroll 4
+        for (int r = 0; r < count; ++r) add(s, row(b + r, 1, col0 + 4 * lane));
         const float f[4] = {s.x, s.y, s.z, s.w};
-        embed_put<float>(p, t, col, f);
+        embed_put<4>(p, t, col0 + 4 * lane, f);
+    }
+    __syncthreads();
+    const int quads = (width + 3) / 4, side = 1024 / quads, mine = threadIdx.x / quads, quad = threadIdx.x % quads;
+    for (int i = 0; i < n_heavy; ++i) {
+        const int64_t b = b0 + heavy[i];
+        const int32_t t = __ldg(p.tokens + b * p.len);
+        int64_t lo = b;   // the first run that does not begin with t
+        for (int n = 1024; n == 1024; lo += n) {
+            const int64_t r = lo + threadIdx.x;
+            n = __syncthreads_count(r < p.runs && __ldg(p.tokens + (r < p.runs ? r : 0) * p.len) == t);
+        }
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (mine < side) {
+            if (mine == 0) s = row(b - 1, 0, col0 + 4 * quad);
+#pragma unroll 8
+            for (int64_t r = b + mine; r < lo; r += side) add(s, row(r, 1, col0 + 4 * quad));
+        }
+        red[threadIdx.x] = s;
+        __syncthreads();
+        int left = side;
+        while (left > 1) {
+            const int half = (left + 1) / 2;
+            if (mine + half < left) add(red[threadIdx.x], red[threadIdx.x + half * quads]);
+            __syncthreads();
+            left = half;
+        }
+        if (mine == 0) {
+            s = red[quad];
+            const float f[4] = {s.x, s.y, s.z, s.w};
+            embed_put<4>(p, t, col0 + 4 * quad, f);
+        }
+        __syncthreads();
     }
 }
 
 template <typename T>
-static void embed_bwd_launch(sat_ctx *ctx, EmbedBwd &p, const void *g)
+static void embed_bwd_launch(sat_ctx *ctx, EmbedBwd &p, int tpr, const void *g)
 {
-    constexpr int V = RowVec<T>::V;
-    const int32_t pieces = (p.d + V - 1) / V;
-    const int tpr = pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
-    p.slabs = (pieces + tpr - 1) / tpr;
     p.walk_blocks = cdiv64(p.runs * p.slabs, 256 / tpr);
-    const unsigned blocks = (unsigned)(p.walk_blocks + (p.accumulate ? 0 : cdiv64(p.vocabulary, 256)));
+    p.zero_blocks = p.accumulate ? 0 : cdiv64(p.vocabulary, p.zero_rows);
+    const unsigned blocks = (unsigned)(p.walk_blocks + p.zero_blocks);
     if (tpr == 8) sat_pdl(ctx->stream, k_embed_bwd<T, 8>, blocks, 256, 0)(p, (const T *)g);
     else if (tpr == 16) sat_pdl(ctx->stream, k_embed_bwd<T, 16>, blocks, 256, 0)(p, (const T *)g);
     else sat_pdl(ctx->stream, k_embed_bwd<T, 32>, blocks, 256, 0)(p, (const T *)g);
@@ -442,22 +695,29 @@ extern "C" sat_status sat_embed_bwd(sat_ctx *ctx, const sat_token_order *order, 
         return sat_fail(ctx, SAT_EINVAL, "sat_embed_bwd: null / misaligned tensor, bad width or leading dimension");
     if (accumulate != 0 && accumulate != 1) return sat_fail(ctx, SAT_EINVAL, "sat_embed_bwd: accumulate is 0 or 1");
     EmbedBwd p = {};
-    p.tokens = order->tokens, p.index = order->index, p.seen = order->seen, p.n = order->n, p.vocabulary = order->vocabulary, p.d = d, p.ld_g = ld_g, p.ld_gt = ld_gt;
-    p.scale = scale, p.accumulate = accumulate, p.g_table = g_table, p.runs = cdiv64(order->n, EMB_RUN), p.ld_part = (d + 7) & ~7;
+    p.tokens = order->tokens, p.index = order->index, p.n = order->n, p.vocabulary = order->vocabulary, p.d = d, p.ld_g = ld_g, p.ld_gt = ld_gt;
+    p.scale = scale, p.accumulate = accumulate, p.g_table = g_table, p.ld_part = (d + 7) & ~7;
     p.status = ctx->d_flag + 1;
     if (p.n == 0 && accumulate) return SAT_OK;
-    if (p.runs * cdiv64(d, 32) >= INT32_MAX) return sat_fail(ctx, SAT_EINVAL, "sat_embed_bwd: too many rows of this width");
-    if (p.runs > 1) {
+    // lanes of a row: as many as it has pieces of 16 bytes; runs: as many as fill the SMs twice with the 24 warps that they hold, of 8 positions at least
+    const int32_t v = 16 / type_bytes(type), pieces = (d + v - 1) / v;
+    const int tpr = pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
+    p.slabs = (pieces + tpr - 1) / tpr;
+    p.len = (int32_t)std::max<int64_t>(8, cdiv64(p.n * p.slabs, (int64_t)ctx->sms * 48 * (32 / tpr)));
+    p.zero_rows = (int32_t)std::min<int64_t>(EMB_ZERO, std::max<int64_t>(32, cdiv64(order->vocabulary, ctx->sms * 8)));
+    p.runs = cdiv64(p.n, p.len);
+    if (p.runs * p.slabs >= INT32_MAX) return sat_fail(ctx, SAT_EINVAL, "sat_embed_bwd: too many rows of this width");
+    if (p.runs > 2) {   // (a long token crosses two borders)
         SAT_TRY(sat_ensure(ctx, ctx->buf_embed, (size_t)p.runs * 2 * p.ld_part * sizeof(float)));
         p.part = (float *)ctx->buf_embed.p;
     }
     ProfScope prof(ctx, SATK_EMBED, (double)type_bytes(type) * p.n * d + 4.0 * (double)order->vocabulary * d, (double)p.n * d);
-    if (type == SAT_F32) embed_bwd_launch<float>(ctx, p, g);
-    else if (type == SAT_BF16) embed_bwd_launch<__nv_bfloat16>(ctx, p, g);
-    else embed_bwd_launch<__half>(ctx, p, g);
+    if (type == SAT_F32) embed_bwd_launch<float>(ctx, p, tpr, g);
+    else if (type == SAT_BF16) embed_bwd_launch<__nv_bfloat16>(ctx, p, tpr, g);
+    else embed_bwd_launch<__half>(ctx, p, tpr, g);
     SAT_LAUNCHED(ctx);
-    if (p.runs > 1) {
-        sat_pdl(ctx->stream, k_embed_join, dim3((unsigned)(p.runs - 1), (unsigned)cdiv64(d, 128)), 256, 0)(p);
+    if (p.runs > 2) {
+        sat_pdl(ctx->stream, k_embed_join, dim3((unsigned)cdiv64(p.runs - 1, EMB_WINDOW), (unsigned)cdiv64(d, 128)), 1024, 0)(p);
         SAT_LAUNCHED(ctx);
     }
     return SAT_OK;

@@ -9,6 +9,7 @@
 #define LOSS_MAX_BLOCKS(ctx) ((ctx)->sms * 6)
 
 #ifdef __CUDACC__
+// NT: threads of the block, a power of two
 template <int NT = 256>
 __device__ __forceinline__ void loss_finish(double thread_sum, double *__restrict__ block_partial, int *__restrict__ ticket, double *total, int overwrite)
 {
@@ -39,6 +40,27 @@ __device__ __forceinline__ void loss_finish(double thread_sum, double *__restric
     if (threadIdx.x == 0) {
         *ticket = 0;   // the next launch on this stream starts from zero again
         if (total) *total = overwrite ? red[0] : *total + red[0];
+    }
+}
+
+// The same where the sums are one thread's of each block, thread 0: any number of whole warps, little shared memory.
+__device__ __forceinline__ void loss_finish_first(double sum, double *__restrict__ block_partial, int *__restrict__ ticket, double *total)
+{
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        block_partial[blockIdx.x] = sum;
+        __threadfence();
+        last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last || threadIdx.x >= 32) return;
+    __threadfence();
+    double s = 0.0;
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += 32) s += __ldcg(block_partial + i);
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (threadIdx.x == 0) {
+        *ticket = 0;
+        *total += s;
     }
 }
 #endif

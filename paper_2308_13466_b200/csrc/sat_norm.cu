@@ -1,51 +1,117 @@
 // Layer norm by rows, forward and backward:
 //     mu = sum x / d,  s = (sum (x - mu)^2 / d + eps)^(-1/2),  xh = (x - mu) s,  y = xh gamma + beta
 //     u = g gamma,  g_x = s (u - sum u / d - xh sum (u xh) / d),  g_gamma = sum over rows g xh,  g_beta = sum over rows g
+#include "sat_ptx.h"
 #include "sat_rows.h"
 
 #include <algorithm>
 
 #define NORM_MAX 16384   // width: a row lies in the registers of one block
 
-// TPR threads hold a row in registers, CH times 16 bytes each.
-#define NORM_THREADS(TPR) ((TPR) > 32 ? (TPR) : 256)   // of a block
+// The work on 16 bytes of a row, by pairs.
+// Forward: x -> x - m0 (zeros behind the row's end), with its sum and that of its squares
+template <int V>
+__device__ __forceinline__ void norm_centre(uint64_t (&v)[V / 2], float m0, int32_t col, int32_t d, uint64_t &a, uint64_t &b)
+{
+    const uint64_t less = f2_all(-m0);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) v[i] = f2_add(v[i], less);
+    if (col + V > d) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) v[i] = f2_pack(col + 2 * i < d ? f2_unpack(v[i]).x : 0.f, col + 2 * i + 1 < d ? f2_unpack(v[i]).y : 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        a = f2_add(a, v[i]);
+        b = f2_fma(v[i], v[i], b);
+    }
+}
+// ... -> y = (x - m0 - m1) s gamma + beta
+template <typename T>
+__device__ __forceinline__ void norm_finish(T *y, int32_t col, int32_t d, const uint64_t (&v)[RowVec<T>::V / 2], float m1, float sd, const uint64_t (&gamma)[RowVec<T>::V / 2],
+                                            const uint64_t (&beta)[RowVec<T>::V / 2])
+{
+    constexpr int V = RowVec<T>::V;
+    const uint64_t less = f2_all(-m1), s = f2_all(sd);
+    uint64_t o[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) o[i] = f2_fma(f2_mul(f2_add(v[i], less), s), gamma[i], beta[i]);
+    float out[V];
+    pair_floats<V>(o, out);
+    row_store(y, col, d, out);
+}
+// Backward: x -> xh, g -> u (both zero behind the row's end, or times zero), with sum u, sum u xh and the columns' sums
+template <int V>
+__device__ __forceinline__ void norm_back(uint64_t (&x)[V / 2], uint64_t (&g)[V / 2], float m, float sd, const uint64_t (&gamma)[V / 2], uint64_t &s1, uint64_t &s2,
+                                          uint64_t (&ag)[V / 2], uint64_t (&ab)[V / 2])
+{
+    const uint64_t less = f2_all(-m), s = f2_all(sd);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        x[i] = f2_mul(f2_add(x[i], less), s);
+        ag[i] = f2_fma(g[i], x[i], ag[i]);
+        ab[i] = f2_add(ab[i], g[i]);
+        g[i] = f2_mul(g[i], gamma[i]);
+        s1 = f2_add(s1, g[i]);
+        s2 = f2_fma(g[i], x[i], s2);
+    }
+}
+// ... -> g_x = s (u - c1 - xh c2)
+template <typename T>
+__device__ __forceinline__ void norm_back_finish(T *gx, int32_t col, int32_t d, const uint64_t (&xh)[RowVec<T>::V / 2], const uint64_t (&u)[RowVec<T>::V / 2], float sd, float c1, float c2)
+{
+    constexpr int V = RowVec<T>::V;
+    const uint64_t s = f2_all(sd), k1 = f2_all(-c1), k2 = f2_all(-c2);
+    uint64_t o[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) o[i] = f2_mul(f2_add(u[i], f2_fma(xh[i], k2, k1)), s);
+    float out[V];
+    pair_floats<V>(o, out);
+    row_store(gx, col, d, out);
+}
 
+// =====================================================================================
+// rows of up to 512 elements: TPR lanes hold one in registers, CH times 16 bytes each
+// =====================================================================================
+
+// (the next row is asked for before this one is worked on)
 template <typename T, int TPR, int CH>
-__global__ void __launch_bounds__(NORM_THREADS(TPR))
+__global__ void __launch_bounds__(256)
 k_norm_fwd(int64_t rows, int32_t d, const T *x, int64_t ld_x, const float *__restrict__ gamma, const float *__restrict__ beta, float eps, T *y,
            int64_t ld_y, float *__restrict__ mean, float *__restrict__ rstd)
 {
     sat_grid_wait();
-    constexpr int V = RowVec<T>::V, NT = NORM_THREADS(TPR), RPB = NT / TPR;
-    __shared__ float2 red[2][32];
+    constexpr int V = RowVec<T>::V, H = V / 2, NT = 256, RPB = NT / TPR;
+    float2 (*none)[32] = nullptr;
     int turn = 0;
     const int t = threadIdx.x % TPR;
     const float inv_d = 1.f / (float)d;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < rows; r0 += (int64_t)gridDim.x * RPB) {
-        const int64_t r = r0 + threadIdx.x / TPR;
-        const bool ok = r < rows;
-        float v[CH][V];
-        float s = 0.f;
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    uint4 raw[CH];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) raw[j] = row_load_raw(x + row * ld_x, row < rows ? (j * TPR + t) * V : d, d);
+    };
+    fetch(r);
+    // (rows that share a warp go on together: its lanes meet in the sums)
+    for (int64_t first = r - (threadIdx.x & 31) / TPR; first < rows; first += step, r += step) {
+        uint64_t v[CH][H], s = 0;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            row_load(x + (ok ? r : 0) * ld_x, ok ? (j * TPR + t) * V : d, d, v[j]);
+            pair_unpack<T>(raw[j], (j * TPR + t) * V, d, v[j]);
 #pragma unroll
-            for (int i = 0; i < V; ++i) s += v[j][i];
+            for (int i = 0; i < H; ++i) s = f2_add(s, v[j][i]);
         }
-        const float m0 = row_sum2<TPR>(s, 0.f, red, turn).x * inv_d;
+        fetch(r + step);
+        const float m0 = row_sum<TPR>(f2_sum(s), none, turn) * inv_d;
         // what the rounding of the mean left is taken off with the squares
-        float a = 0.f, b = 0.f;
+        uint64_t a = 0, b = 0;
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                v[j][i] = (j * TPR + t) * V + i < d ? v[j][i] - m0 : 0.f;
-                a += v[j][i];
-                b = fmaf(v[j][i], v[j][i], b);
-            }
-        const float2 ab = row_sum2<TPR>(a, b, red, turn);
+        for (int j = 0; j < CH; ++j) norm_centre<V>(v[j], m0, (j * TPR + t) * V, d, a, b);
+        const float2 ab = row_sum2<TPR>(f2_sum(a), f2_sum(b), none, turn);
         const float m1 = ab.x * inv_d, var = fmaxf(ab.y * inv_d - m1 * m1, 0.f), sd = 1.f / sqrtf(var + eps);
-        if (!ok) continue;
+        if (r >= rows) continue;
         if (t == 0) {
             if (mean) mean[r] = m0 + m1;
             if (rstd) rstd[r] = sd;
@@ -54,122 +120,276 @@ k_norm_fwd(int64_t rows, int32_t d, const T *x, int64_t ld_x, const float *__res
         for (int j = 0; j < CH; ++j) {
             const int32_t col = (j * TPR + t) * V;
             if (col >= d) continue;
-            float ga[V], be[V];
-            param_load<V>(gamma, col, d, 1.f, ga);
-            param_load<V>(beta, col, d, 0.f, be);
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[j][i] = fmaf((v[j][i] - m1) * sd, ga[i], be[i]);
-            row_store(y + r * ld_y, col, d, v[j]);
+            uint64_t ga[H], be[H];
+            pair_param<V>(gamma, col, d, 1.f, ga);
+            pair_param<V>(beta, col, d, 0.f, be);
+            norm_finish<T>(y + r * ld_y, col, d, v[j], m1, sd, ga, be);
         }
     }
 }
 
-// The sums over the rows: a thread adds up its columns over the block's rows in registers, the block leaves one row of partial sums
-// [g_gamma | g_beta], k_norm_sums adds these up in a fixed order.
+// The sums over the rows: a thread adds up its columns over its rows in registers, the block leaves one row of partial sums [g_gamma | g_beta], k_norm_sums
+// adds these up in a fixed order.
 template <typename T, int TPR, int CH>
-__global__ void __launch_bounds__(NORM_THREADS(TPR))
+__global__ void __launch_bounds__(256, CH * RowVec<T>::V > 8 ? 2 : 3)
 k_norm_bwd(int64_t rows, int32_t d, const T *x, int64_t ld_x, const T *g, int64_t ld_g, const float *__restrict__ gamma,
            const float *__restrict__ mean, const float *__restrict__ rstd, T *gx, int64_t ld_gx, float *__restrict__ part, int32_t ld_part)
 {
     sat_grid_wait();
-    constexpr int V = RowVec<T>::V, NT = NORM_THREADS(TPR), RPB = NT / TPR;
-    __shared__ float2 red[2][32];
+    constexpr int V = RowVec<T>::V, H = V / 2, NT = 256, RPB = NT / TPR;
+    float2 (*none)[32] = nullptr;
     int turn = 0;
     const int t = threadIdx.x % TPR;
     const float inv_d = 1.f / (float)d;
-    float ag[CH][V] = {}, ab[CH][V] = {};
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < rows; r0 += (int64_t)gridDim.x * RPB) {
-        const int64_t r = r0 + threadIdx.x / TPR;
+    uint64_t ag2[CH][H] = {}, ab2[CH][H] = {};
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    for (int64_t first = r - (threadIdx.x & 31) / TPR; first < rows; first += step, r += step) {
         const bool ok = r < rows;
-        float xh[CH][V], u[CH][V];
+        uint4 xr[CH], gr[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int32_t col = ok ? (j * TPR + t) * V : d;
-            row_load(x + (ok ? r : 0) * ld_x, col, d, xh[j]);
-            row_load(g + (ok ? r : 0) * ld_g, col, d, u[j]);
+            xr[j] = row_load_raw(x + r * ld_x, col, d);
+            gr[j] = row_load_raw(g + r * ld_g, col, d);
         }
-        const float m = ok ? __ldg(mean + r) : 0.f, sd = ok ? __ldg(rstd + r) : 0.f;
-        float s1 = 0.f, s2 = 0.f;
+        const float m = ok ? __ldg(mean + r) : 0.f, sd0 = ok ? __ldg(rstd + r) : 0.f;
+        uint64_t xh[CH][H], u[CH][H], s1 = 0, s2 = 0;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int32_t col = (j * TPR + t) * V;
-            float ga[V];
-            param_load<V>(gamma, col, d, 1.f, ga);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                xh[j][i] = ok && col + i < d ? (xh[j][i] - m) * sd : 0.f;
-                ag[j][i] = fmaf(u[j][i], xh[j][i], ag[j][i]);
-                ab[j][i] += u[j][i];
-                u[j][i] *= ga[i];
-                s1 += u[j][i];
-                s2 = fmaf(u[j][i], xh[j][i], s2);
-            }
+            pair_unpack<T>(xr[j], col, d, xh[j]);
+            pair_unpack<T>(gr[j], col, d, u[j]);
+            uint64_t ga[H];
+            pair_param<V>(gamma, col, d, 1.f, ga);
+            norm_back<V>(xh[j], u[j], m, sd0, ga, s1, s2, ag2[j], ab2[j]);
         }
         if (!gx) continue;   // (the same for all threads)
-        const float2 s = row_sum2<TPR>(s1, s2, red, turn);
-        const float c1 = s.x * inv_d, c2 = s.y * inv_d;
+        const float2 s = row_sum2<TPR>(f2_sum(s1), f2_sum(s2), none, turn);
         if (!ok) continue;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int32_t col = (j * TPR + t) * V;
-            if (col >= d) continue;
-#pragma unroll
-            for (int i = 0; i < V; ++i) u[j][i] = sd * (u[j][i] - fmaf(xh[j][i], c2, c1));
-            row_store(gx + r * ld_gx, col, d, u[j]);
+            if (col < d) norm_back_finish<T>(gx + r * ld_gx, col, d, xh[j], u[j], sd0, s.x * inv_d, s.y * inv_d);
         }
     }
     if (!part) return;
     float *out = part + (int64_t)blockIdx.x * 2 * ld_part;
-    if constexpr (RPB == 1) {
+    __shared__ float sum[2][TPR * V];
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
+    for (int j = 0; j < CH; ++j) {
+        float ag[V], ab[V];
+        pair_floats<V>(ag2[j], ag);
+        pair_floats<V>(ab2[j], ab);
+        for (int w = 0; w < RPB; ++w) {   // one group of rows after the other
+            __syncthreads();
+            if (threadIdx.x / TPR == w) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int32_t col = (j * TPR + t) * V + i;
-                if (col < d) out[col] = ag[j][i], out[ld_part + col] = ab[j][i];
-            }
-    } else {
-        __shared__ float sum[2][TPR * V];
-#pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            for (int w = 0; w < RPB; ++w) {   // one group of rows after the other
-                __syncthreads();
-                if (threadIdx.x / TPR == w) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        sum[0][t * V + i] = w ? sum[0][t * V + i] + ag[j][i] : ag[j][i];
-                        sum[1][t * V + i] = w ? sum[1][t * V + i] + ab[j][i] : ab[j][i];
-                    }
+                for (int i = 0; i < V; ++i) {
+                    sum[0][t * V + i] = w ? sum[0][t * V + i] + ag[i] : ag[i];
+                    sum[1][t * V + i] = w ? sum[1][t * V + i] + ab[i] : ab[i];
                 }
             }
-            __syncthreads();
-            for (int c = threadIdx.x; c < 2 * TPR * V; c += NT) {
-                const int which = c / (TPR * V), i = c % (TPR * V), col = j * TPR * V + i;
-                if (col < d) out[which * ld_part + col] = sum[which][i];
-            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * TPR * V; c += NT) {
+            const int which = c / (TPR * V), i = c % (TPR * V), col = j * TPR * V + i;
+            if (col < d) out[which * ld_part + col] = sum[which][i];
         }
     }
 }
 
-// out[c] (+)= sum over b of part[b][c]: 32 columns a block, eight threads a column
+// =====================================================================================
+// wider rows: a block holds one in registers, CH times 16 bytes a thread; the next ones are on their way into a ring in shared memory (cp.async.bulk), so that what an SM
+// has asked for does not depend on its registers.  A slot is asked for again behind the barrier of the row's sums, when all threads have taken their part of it.
+// =====================================================================================
+#define NORM_SLOTS 8
+// gamma and beta in shared memory, or else from the L1, which has the rest of the SM.  Measured, kept against not: gradients of 50000 x 2048 bf16 125 / 225 us, of 16384 x
+// 4096 bf16 85 / 100, of 16000 x 8192 fp32 248 / 266, of 100000 x 1024 fp32 (where they take a slot's room) 227 / 218; 100000 x 1024 fp32 forward 131 / 166.
+#define NORM_KEPT(NT, V, BACK) ((NT) >= 256 || (V) == 8 || !(BACK))
+#define NORM_RING_BLOCKS(NT) ((NT) >= 512 ? 1 : 640 / (NT))   // of an SM
+template <typename T>
+struct NormRing {
+    int64_t rows;
+    int32_t d, slots;
+    const T *x, *g;        // backward: both
+    int64_t ld_x, ld_g, ld_y;
+    const float *gamma, *beta;
+    float eps;
+    T *y;                  // or g_x
+    float *mean, *rstd;    // forward: written, backward: read
+    float *part;
+    int32_t ld_part;
+    int *status;
+};
+template <typename T, int NT, int CH, bool BACK>
+__global__ void __launch_bounds__(NT, NORM_RING_BLOCKS(NT))
+k_norm_ring(NormRing<T> p)
+{
+    constexpr int V = RowVec<T>::V, H = V / 2;
+    constexpr bool KEPT = NORM_KEPT(NT, RowVec<T>::V, BACK);
+    extern __shared__ uint4 norm_smem[];
+    __shared__ uint64_t full[NORM_SLOTS];
+    __shared__ int dead;
+    __shared__ float2 red[2][32];
+    const int tid = threadIdx.x;
+    const int32_t pieces = (p.d + V - 1) / V, stage = (BACK ? 2 : 1) * pieces;   // of 16 bytes
+    if (tid == 0) {
+        for (int i = 0; i < NORM_SLOTS; ++i) mbar_init(full + i, 1);
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    sat_grid_wait();
+    // gamma and beta of rows that leave no room for them in the L1: four elements of a piece, then the next four of all pieces
+    uint4 *gamma_s = norm_smem + p.slots * stage, *beta_s = gamma_s + pieces * (V / 4);
+    for (int32_t i = tid; KEPT && i < pieces; i += NT) {
+        float f[V];
+        param_load<V>(p.gamma, i * V, p.d, 1.f, f);
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) gamma_s[h * pieces + i] = make_uint4(__float_as_uint(f[4 * h]), __float_as_uint(f[4 * h + 1]), __float_as_uint(f[4 * h + 2]), __float_as_uint(f[4 * h + 3]));
+        if (BACK) continue;
+        param_load<V>(p.beta, i * V, p.d, 0.f, f);
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) beta_s[h * pieces + i] = make_uint4(__float_as_uint(f[4 * h]), __float_as_uint(f[4 * h + 1]), __float_as_uint(f[4 * h + 2]), __float_as_uint(f[4 * h + 3]));
+    }
+    auto params = [&](const uint4 *of, const float *at, float other, int32_t piece, uint64_t (&f)[H]) {
+        if (!KEPT) return pair_param<V>(at, piece * V, p.d, other, f);
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+            const uint4 v = of[h * pieces + piece];
+            f[2 * h] = f2_pack(__uint_as_float(v.x), __uint_as_float(v.y)), f[2 * h + 1] = f2_pack(__uint_as_float(v.z), __uint_as_float(v.w));
+        }
+    };
+    __syncthreads();
+    uint32_t issued = 0;
+    auto ask = [&](int64_t r, uint32_t slot) {   // first thread
+        if (r >= p.rows || *(volatile int *)&dead) return;
+        ++issued;
+        mbar_expect_tx(full + slot, (uint32_t)stage * 16);
+        auto copy = [&](const T *from, uint4 *to) {
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(to)), "l"(from), "r"((uint32_t)pieces * 16),
+                         "r"(smem_u32(full + slot))
+                         : "memory");
+        };
+        copy(p.x + r * p.ld_x, norm_smem + slot * stage);
+        if (BACK) copy(p.g + r * p.ld_g, norm_smem + slot * stage + pieces);
+    };
+    if (tid == 0)
+        for (int i = 0; i < p.slots; ++i) ask(blockIdx.x + (int64_t)i * gridDim.x, i);
+    int turn = 0;
+    uint32_t slot = 0, phase = 0;
+    const float inv_d = 1.f / (float)p.d;
+    uint64_t ag[BACK ? CH : 1][H] = {}, ab[BACK ? CH : 1][H] = {};
+    float m_next = 0.f, sd_next = 0.f;
+    auto statistics = [&](int64_t r) {
+        if (BACK && r < p.rows) m_next = __ldg(p.mean + r), sd_next = __ldg(p.rstd + r);
+    };
+    statistics(blockIdx.x);
+    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+        (void)mbar_wait(full + slot, phase, &dead, p.status);   // (having given up, all finish on what is there)
+        const uint4 *from = norm_smem + slot * stage;
+        uint64_t v[CH][H], u[BACK ? CH : 1][H];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int32_t at = j * NT + tid;
+            if (at < pieces) {
+                pair_unpack<T>(from[at], at * V, p.d, v[j]);
+                if (BACK) pair_unpack<T>(from[pieces + at], at * V, p.d, u[j % (BACK ? CH : 1)]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < H; ++i) v[j][i] = u[j % (BACK ? CH : 1)][i] = 0;
+            }
+        }
+        fence_async_smem();   // these loads are done before a later row lands there
+        T *yr = p.y + r * p.ld_y;
+        const int64_t later = r + (int64_t)p.slots * gridDim.x;
+        if constexpr (BACK) {
+            const float m = m_next, sd = sd_next;
+            statistics(r + gridDim.x);
+            uint64_t s1 = 0, s2 = 0;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                if (j * NT + tid >= pieces) break;
+                uint64_t ga[H];
+                params(gamma_s, p.gamma, 1.f, j * NT + tid, ga);
+                norm_back<V>(v[j], u[j], m, sd, ga, s1, s2, ag[j], ab[j]);
+            }
+            const float2 s = row_sum2<NT>(f2_sum(s1), f2_sum(s2), red, turn);
+            if (tid == 0) ask(later, slot);
+            if (p.y) {
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const int32_t col = (j * NT + tid) * V;
+                    if (col < p.d) norm_back_finish<T>(yr, col, p.d, v[j], u[j], sd, s.x * inv_d, s.y * inv_d);
+                }
+            }
+        } else {
+            uint64_t s = 0;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < H; ++i) s = f2_add(s, v[j][i]);
+            const float m0 = row_sum<NT>(f2_sum(s), red, turn) * inv_d;
+            if (tid == 0) ask(later, slot);
+            uint64_t a = 0, b = 0;   // (as in k_norm_fwd)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) norm_centre<V>(v[j], m0, (j * NT + tid) * V, p.d, a, b);
+            const float2 t = row_sum2<NT>(f2_sum(a), f2_sum(b), red, turn);
+            const float m1 = t.x * inv_d, var = fmaxf(t.y * inv_d - m1 * m1, 0.f), sd = 1.f / sqrtf(var + p.eps);
+            if (tid == 0) {
+                if (p.mean) p.mean[r] = m0 + m1;
+                if (p.rstd) p.rstd[r] = sd;
+            }
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int32_t col = (j * NT + tid) * V;
+                if (col >= p.d) break;
+                uint64_t ga[H], be[H];
+                params(gamma_s, p.gamma, 1.f, j * NT + tid, ga);
+                params(beta_s, p.beta, 0.f, j * NT + tid, be);
+                norm_finish<T>(yr, col, p.d, v[j], m1, sd, ga, be);
+            }
+        }
+        if (++slot == (uint32_t)p.slots) slot = 0, phase ^= 1u;
+    }
+    if (tid == 0 && *(volatile int *)&dead) mbar_settle(full, (uint32_t)p.slots, issued);
+    if constexpr (BACK) {
+        if (!p.part) return;
+        float *out = p.part + (int64_t)blockIdx.x * 2 * p.ld_part;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int32_t col = (j * NT + tid) * V;
+            float sum[V];
+            pair_floats<V>(ag[j], sum);
+            row_store_f32<V>(out, col, p.d, sum);
+            pair_floats<V>(ab[j], sum);
+            row_store_f32<V>(out + p.ld_part, col, p.d, sum);
+        }
+    }
+}
+
+// out[c] (+)= sum over b of part[b][c]: eight columns (a sector of memory) a block, 32 threads a column
 __global__ void __launch_bounds__(256)
 k_norm_sums(const float *__restrict__ part, int32_t blocks, int32_t d, int32_t ld_part, int accumulate, float *__restrict__ g_gamma, float *__restrict__ g_beta)
 {
     sat_grid_wait();
-    __shared__ float red[8][32];
-    const int32_t col = (int32_t)blockIdx.x * 32 + (threadIdx.x & 31);
-    const int w = threadIdx.x >> 5;
+    __shared__ float red[32][9];
+    const int c = threadIdx.x & 7, w = threadIdx.x >> 3;
+    const int32_t col = (int32_t)blockIdx.x * 8 + c;
     float *out = blockIdx.y ? g_beta : g_gamma;
     if (!out) return;
     float s = 0.f;
     if (col < d)
-        for (int32_t b = w; b < blocks; b += 8) s += __ldcg(part + ((int64_t)b * 2 + blockIdx.y) * ld_part + col);
-    red[w][threadIdx.x & 31] = s;
+#pragma unroll 8
+        for (int32_t b = w; b < blocks; b += 32) s += __ldcg(part + ((int64_t)b * 2 + blockIdx.y) * ld_part + col);
+    red[w][c] = s;
     __syncthreads();
-    if (w == 0 && col < d) {
-        for (int i = 1; i < 8; ++i) s += red[i][threadIdx.x];
-        out[col] = accumulate ? out[col] + s : s;
-    }
+    const int lane = threadIdx.x & 31, mine = threadIdx.x >> 5;   // a warp per column
+    s = red[lane][mine];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const int32_t to = (int32_t)blockIdx.x * 8 + mine;
+    if (lane == 0 && to < d) out[to] = accumulate ? out[to] + s : s;
 }
 
 template <typename T>
@@ -183,43 +403,82 @@ struct NormArgs {
     float eps;
     T *y;                 // or g_x
     float *mean, *rstd;
-    float *part;          // backward: partial sums of `blocks` blocks
-    int32_t ld_part, blocks;
+    float *g_gamma, *g_beta;
+    int accumulate;
 };
-template <typename T, int TPR, int CH>
-static void norm_go(const NormArgs<T> &a, bool back)
-{
-    constexpr int NT = NORM_THREADS(TPR), RPB = NT / TPR;
-    if (back) {
-        sat_pdl(a.ctx->stream, k_norm_bwd<T, TPR, CH>, (unsigned)a.blocks, NT, 0)(a.rows, a.d, a.x, a.ld_x, a.g, a.ld_g, a.gamma, a.mean, a.rstd, a.y, a.ld_y, a.part,
-                                                                                   a.ld_part);
-    } else {
-        const int64_t blocks = std::min<int64_t>(cdiv64(a.rows, RPB), (int64_t)a.ctx->sms * (2048 / NT));
-        sat_pdl(a.ctx->stream, k_norm_fwd<T, TPR, CH>, (unsigned)blocks, NT, 0)(a.rows, a.d, a.x, a.ld_x, a.gamma, a.beta, a.eps, a.y, a.ld_y, a.mean, a.rstd);
-    }
-}
-// threads of a row: as few as hold it with up to eight (a block: four) pieces of 16 bytes each, so that sums cross few lanes
-static int norm_tpr(int32_t pieces) { return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 256 ? 32 : pieces <= 512 ? 128 : pieces <= 1024 ? 256 : pieces <= 2048 ? 512 : 1024; }
+// room for a row of partial sums of every block
 template <typename T>
-static void norm_launch(const NormArgs<T> &a, bool back)
+static sat_status norm_parts(const NormArgs<T> &a, int32_t blocks, int32_t ld_part, float **part)
 {
-    const int32_t pieces = (a.d + RowVec<T>::V - 1) / RowVec<T>::V;
-    const int tpr = norm_tpr(pieces), ch = (pieces + tpr - 1) / tpr;
-    switch (tpr) {
-    case 8: return norm_go<T, 8, 1>(a, back);
-    case 16: return norm_go<T, 16, 1>(a, back);
-    case 32:
-        if (ch == 1) return norm_go<T, 32, 1>(a, back);
-        if (ch == 2) return norm_go<T, 32, 2>(a, back);
-        if (ch == 3) return norm_go<T, 32, 3>(a, back);
-        if (ch == 4) return norm_go<T, 32, 4>(a, back);
-        if (ch <= 6) return norm_go<T, 32, 6>(a, back);
-        return norm_go<T, 32, 8>(a, back);
-    case 128: return ch <= 3 ? norm_go<T, 128, 3>(a, back) : norm_go<T, 128, 4>(a, back);
-    case 256: return ch <= 3 ? norm_go<T, 256, 3>(a, back) : norm_go<T, 256, 4>(a, back);
-    case 512: return ch <= 3 ? norm_go<T, 512, 3>(a, back) : norm_go<T, 512, 4>(a, back);
-    default: return ch <= 3 ? norm_go<T, 1024, 3>(a, back) : norm_go<T, 1024, 4>(a, back);
+    *part = nullptr;
+    if (!a.g_gamma && !a.g_beta) return SAT_OK;
+    SAT_TRY(sat_ensure(a.ctx, a.ctx->buf_norm, (size_t)blocks * 2 * ld_part * sizeof(float)));
+    *part = (float *)a.ctx->buf_norm.p;
+    return SAT_OK;
+}
+template <typename T>
+static sat_status norm_sums(const NormArgs<T> &a, int32_t blocks, int32_t ld_part, const float *part)
+{
+    if (!part) return SAT_OK;
+    sat_pdl(a.ctx->stream, k_norm_sums, dim3((unsigned)cdiv64(a.d, 8), 2), 256, 0)(part, blocks, a.d, ld_part, a.accumulate, a.g_gamma, a.g_beta);
+    SAT_LAUNCHED(a.ctx);
+    return SAT_OK;
+}
+template <typename T, int TPR, int CH>
+static sat_status norm_rows_go(const NormArgs<T> &a, bool back)
+{
+    constexpr int RPB = 256 / TPR;
+    sat_ctx *ctx = a.ctx;
+    if (!back) {
+        const int64_t blocks = std::min<int64_t>(cdiv64(a.rows, RPB), (int64_t)ctx->sms * 8);
+        sat_pdl(ctx->stream, k_norm_fwd<T, TPR, CH>, (unsigned)blocks, 256, 0)(a.rows, a.d, a.x, a.ld_x, a.gamma, a.beta, a.eps, a.y, a.ld_y, a.mean, a.rstd);
+        SAT_LAUNCHED(ctx);
+        return SAT_OK;
     }
+    // every block is a row of partial sums: as many as the SMs hold, and two rows a thread at least
+    const int32_t blocks = (int32_t)std::min<int64_t>(cdiv64(a.rows, 2 * RPB), (int64_t)ctx->sms * (CH * RowVec<T>::V > 8 ? 2 : 3)), ld_part = (a.d + 7) & ~7;
+    float *part;
+    SAT_TRY(norm_parts(a, blocks, ld_part, &part));
+    sat_pdl(ctx->stream, k_norm_bwd<T, TPR, CH>, (unsigned)blocks, 256, 0)(a.rows, a.d, a.x, a.ld_x, a.g, a.ld_g, a.gamma, (const float *)a.mean, (const float *)a.rstd, a.y, a.ld_y,
+                                                                           part, ld_part);
+    SAT_LAUNCHED(ctx);
+    return norm_sums(a, blocks, ld_part, part);
+}
+template <typename T, int NT, int CH, bool BACK>
+static sat_status norm_ring_go(const NormArgs<T> &a)
+{
+    static PerDeviceOnce set;
+    sat_ctx *ctx = a.ctx;
+    constexpr int room = (NORM_KEPT(NT, RowVec<T>::V, BACK) ? 208 : 128) * 1024 / NORM_RING_BLOCKS(NT);   // of a block; the rest is L1
+    if (set.need(ctx->device)) {
+        SAT_CUDA(ctx, cudaFuncSetAttribute(k_norm_ring<T, NT, CH, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, room));
+        set.mark(ctx->device);
+    }
+    const int32_t pieces = (a.d + RowVec<T>::V - 1) / RowVec<T>::V, stage = (BACK ? 2 : 1) * pieces * 16, params = NORM_KEPT(NT, RowVec<T>::V, BACK) ? (BACK ? 1 : 2) * pieces * RowVec<T>::V * 4 : 0;
+    const int32_t slots = std::min(NORM_SLOTS, (room - params) / stage);   // one at least: 16,384 fp32 elements take 192 KB
+    const int32_t blocks = (int32_t)std::min<int64_t>(a.rows, (int64_t)ctx->sms * NORM_RING_BLOCKS(NT)), ld_part = (a.d + 7) & ~7;
+    float *part = nullptr;
+    if (BACK) SAT_TRY(norm_parts(a, blocks, ld_part, &part));
+    const NormRing<T> p = {a.rows, a.d, slots, a.x, a.g, a.ld_x, a.ld_g, a.ld_y, a.gamma, a.beta, a.eps, a.y, a.mean, a.rstd, part, ld_part, ctx->d_flag + 1};
+    sat_pdl(ctx->stream, k_norm_ring<T, NT, CH, BACK>, (unsigned)blocks, NT, (size_t)slots * stage + params)(p);
+    SAT_LAUNCHED(ctx);
+    return BACK ? norm_sums(a, blocks, ld_part, part) : SAT_OK;
+}
+template <typename T>
+static sat_status norm_launch(const NormArgs<T> &a, bool back)
+{
+    constexpr int CH = 8 / RowVec<T>::V;   // pieces of a thread with 8 elements
+    const int32_t pieces = (a.d + RowVec<T>::V - 1) / RowVec<T>::V;
+    if (pieces <= 8) return norm_rows_go<T, 8, 1>(a, back);
+    if (pieces <= 16 * CH) return norm_rows_go<T, 16, CH>(a, back);
+    if (pieces <= 32 * CH) return norm_rows_go<T, 32, CH>(a, back);
+    if (pieces <= 64 * CH) return norm_rows_go<T, 32, 2 * CH>(a, back);
+    // (16 elements a thread: what a row costs a warp whatever it holds, its part of the sums above all, is then a fifth of the instructions)
+    if (pieces <= 128 * CH) return back ? norm_ring_go<T, 64, 2 * CH, true>(a) : norm_ring_go<T, 64, 2 * CH, false>(a);
+    if (pieces <= 256 * CH) return back ? norm_ring_go<T, 128, 2 * CH, true>(a) : norm_ring_go<T, 128, 2 * CH, false>(a);
+    if (pieces <= 512 * CH) return back ? norm_ring_go<T, 256, 2 * CH, true>(a) : norm_ring_go<T, 256, 2 * CH, false>(a);
+    if (pieces <= 1024 * CH) return back ? norm_ring_go<T, 512, 2 * CH, true>(a) : norm_ring_go<T, 512, 2 * CH, false>(a);
+    return back ? norm_ring_go<T, 1024, 2 * CH, true>(a) : norm_ring_go<T, 1024, 2 * CH, false>(a);
 }
 
 static sat_status norm_check(sat_ctx *ctx, const char *who, int64_t rows, int32_t d, int type)
@@ -231,14 +490,16 @@ static sat_status norm_check(sat_ctx *ctx, const char *who, int64_t rows, int32_
 static bool norm_param_ok(const float *p) { return !p || aligned16(p); }
 
 template <typename T>
-static void norm_fwd_as(sat_ctx *ctx, int64_t rows, int32_t d, const void *x, int32_t ld_x, const float *gamma, const float *beta, float eps, void *y, int32_t ld_y,
-                        float *mean, float *rstd)
+static sat_status norm_as(sat_ctx *ctx, bool back, int64_t rows, int32_t d, const void *x, int32_t ld_x, const void *g, int32_t ld_g, const float *gamma, const float *beta,
+                          float eps, void *y, int32_t ld_y, float *mean, float *rstd, float *g_gamma, float *g_beta, int accumulate)
 {
-    NormArgs<T> a = {};
-    a.ctx = ctx, a.rows = rows, a.d = d, a.x = (const T *)x, a.ld_x = ld_x, a.gamma = gamma, a.beta = beta, a.eps = eps, a.y = (T *)y, a.ld_y = ld_y;
-    a.mean = mean, a.rstd = rstd;
-    norm_launch(a, false);
+    const NormArgs<T> a = {ctx, rows, d, (const T *)x, (const T *)g, ld_x, ld_g, ld_y, gamma, beta, eps, (T *)y, mean, rstd, g_gamma, g_beta, accumulate};
+    return norm_launch(a, back);
 }
+#define NORM_AS(...)                                         \
+    (type == SAT_F32    ? norm_as<float>(__VA_ARGS__)         \
+     : type == SAT_BF16 ? norm_as<__nv_bfloat16>(__VA_ARGS__) \
+                        : norm_as<__half>(__VA_ARGS__))
 
 extern "C" sat_status sat_layernorm_fwd(sat_ctx *ctx, int64_t rows, int32_t d, int type, const void *x, int32_t ld_x, const float *gamma, const float *beta,
                                         float eps, void *y, int32_t ld_y, float *mean, float *rstd)
@@ -250,21 +511,7 @@ extern "C" sat_status sat_layernorm_fwd(sat_ctx *ctx, int64_t rows, int32_t d, i
         return sat_fail(ctx, SAT_EINVAL, "sat_layernorm_fwd: null / misaligned tensor, bad leading dimension or negative eps");
     if (rows == 0) return SAT_OK;
     ProfScope prof(ctx, SATK_NORM, 2.0 * type_bytes(type) * (double)rows * d, 8.0 * (double)rows * d);
-    if (type == SAT_F32) norm_fwd_as<float>(ctx, rows, d, x, ld_x, gamma, beta, eps, y, ld_y, mean, rstd);
-    else if (type == SAT_BF16) norm_fwd_as<__nv_bfloat16>(ctx, rows, d, x, ld_x, gamma, beta, eps, y, ld_y, mean, rstd);
-    else norm_fwd_as<__half>(ctx, rows, d, x, ld_x, gamma, beta, eps, y, ld_y, mean, rstd);
-    SAT_LAUNCHED(ctx);
-    return SAT_OK;
-}
-
-template <typename T>
-static void norm_bwd_as(sat_ctx *ctx, int64_t rows, int32_t d, const void *x, int32_t ld_x, const void *g, int32_t ld_g, const float *gamma, const float *mean,
-                        const float *rstd, void *g_x, int32_t ld_gx, float *part, int32_t ld_part, int32_t blocks)
-{
-    NormArgs<T> a = {};
-    a.ctx = ctx, a.rows = rows, a.d = d, a.x = (const T *)x, a.ld_x = ld_x, a.g = (const T *)g, a.ld_g = ld_g, a.gamma = gamma, a.y = (T *)g_x, a.ld_y = ld_gx;
-    a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd), a.part = part, a.ld_part = ld_part, a.blocks = blocks;
-    norm_launch(a, true);
+    return NORM_AS(ctx, false, rows, d, x, ld_x, nullptr, 0, gamma, beta, eps, y, ld_y, mean, rstd, nullptr, nullptr, 0);
 }
 
 extern "C" sat_status sat_layernorm_bwd(sat_ctx *ctx, int64_t rows, int32_t d, int type, const void *x, int32_t ld_x, const void *g, int32_t ld_g,
@@ -277,30 +524,12 @@ extern "C" sat_status sat_layernorm_bwd(sat_ctx *ctx, int64_t rows, int32_t d, i
         (rows > 0 && (!x || !g || !mean || !rstd || !aligned16(x) || !aligned16(g))))
         return sat_fail(ctx, SAT_EINVAL, "sat_layernorm_bwd: null / misaligned tensor or bad leading dimension");
     if (accumulate != 0 && accumulate != 1) return sat_fail(ctx, SAT_EINVAL, "sat_layernorm_bwd: accumulate is 0 or 1");
-    const bool params = g_gamma || g_beta;
-    if (!g_x && !params) return sat_fail(ctx, SAT_EINVAL, "sat_layernorm_bwd: no result is asked for");
+    if (!g_x && !g_gamma && !g_beta) return sat_fail(ctx, SAT_EINVAL, "sat_layernorm_bwd: no result is asked for");
     if (rows == 0) {
         if (!accumulate && g_gamma) SAT_CUDA(ctx, cudaMemsetAsync(g_gamma, 0, (size_t)d * sizeof(float), ctx->stream));
         if (!accumulate && g_beta) SAT_CUDA(ctx, cudaMemsetAsync(g_beta, 0, (size_t)d * sizeof(float), ctx->stream));
         return SAT_OK;
     }
-    const int32_t pieces = (d + 16 / type_bytes(type) - 1) / (16 / type_bytes(type));
-    const int tpr = norm_tpr(pieces), nt = tpr > 32 ? tpr : 256;
-    const int32_t blocks = (int32_t)std::min<int64_t>(cdiv64(rows, nt / tpr), (int64_t)ctx->sms * std::max(1, 1024 / nt));
-    const int32_t ld_part = round_up4(d);
-    float *part = nullptr;
-    if (params) {
-        SAT_TRY(sat_ensure(ctx, ctx->buf_norm, (size_t)blocks * 2 * ld_part * sizeof(float)));
-        part = (float *)ctx->buf_norm.p;
-    }
     ProfScope prof(ctx, SATK_NORM, (g_x ? 3.0 : 2.0) * type_bytes(type) * (double)rows * d, 14.0 * (double)rows * d);
-    if (type == SAT_F32) norm_bwd_as<float>(ctx, rows, d, x, ld_x, g, ld_g, gamma, mean, rstd, g_x, ld_gx, part, ld_part, blocks);
-    else if (type == SAT_BF16) norm_bwd_as<__nv_bfloat16>(ctx, rows, d, x, ld_x, g, ld_g, gamma, mean, rstd, g_x, ld_gx, part, ld_part, blocks);
-    else norm_bwd_as<__half>(ctx, rows, d, x, ld_x, g, ld_g, gamma, mean, rstd, g_x, ld_gx, part, ld_part, blocks);
-    SAT_LAUNCHED(ctx);
-    if (params) {
-        sat_pdl(ctx->stream, k_norm_sums, dim3((unsigned)cdiv64(d, 32), 2), 256, 0)(part, blocks, d, ld_part, accumulate, g_gamma, g_beta);
-        SAT_LAUNCHED(ctx);
-    }
-    return SAT_OK;
+    return NORM_AS(ctx, true, rows, d, x, ld_x, g, ld_g, gamma, nullptr, 0.f, g_x, ld_gx, const_cast<float *>(mean), const_cast<float *>(rstd), g_gamma, g_beta, accumulate);
 }

@@ -49,18 +49,13 @@ CASES = [(1, 1, "even"), (1, 5000, "even"), (31, 2, "even"), (32, 16, "even"), (
 @pytest.mark.parametrize("n,vocabulary,kind", CASES + [(5000, 2 ** 22 + 5, "even"), (3000, 2 ** 31 - 2, "ends")])
 @pytest.mark.parametrize("padding", [-1, 0])
 def test_order(B, ctx, n, vocabulary, kind, padding):
-    import torch
     rng = np.random.default_rng(n + vocabulary)
     t = rng.choice(np.array([1, 5, 2 ** 30, vocabulary - 1, vocabulary - 2], dtype=np.int32), n) if kind == "ends" else _tokens(rng, n, vocabulary, kind)
     order = B.new_token_order(n, vocabulary)
     B.sat_token_sort(ctx, _ints(t), padding, order)
     B.sat_sync_status(ctx)
-    tokens, index, seen = order._keep
-    if kind == "ends":                                                          # (a list of what is seen that long is looked at in place)
-        want = np.argsort(t, kind="stable")
-        assert np.array_equal(index.cpu().numpy(), want) and np.array_equal(tokens.cpu().numpy(), t[want]) and int(seen.sum(dtype=torch.int64)) == 5
-        return
-    for got, want in zip((tokens, index, seen), ref.token_order(t, padding, vocabulary)):
+    tokens, index = order._keep
+    for got, want in zip((tokens, index), ref.token_order(t, padding, vocabulary)):
         assert np.array_equal(got.cpu().numpy(), want)
 
 
@@ -102,11 +97,10 @@ def test_an_order_that_is_none(B, ctx):
     """The arrays are the caller's: positions that the batch does not have are told apart from others, and nothing is read there."""
     import torch
     order = B.new_token_order(40, 9)
-    tokens, index, seen = order._keep
+    tokens, index = order._keep
     tokens.copy_(_ints(np.sort(np.arange(40) % 9)))
     index.copy_(_ints(np.arange(40)))
     index[7], index[20] = 40, -3
-    seen.fill_(1)
     g, gt = matrix(np.ones((40, 8)), "f32")[0], torch.zeros((9, 8), device="cuda")
     B.sat_embed_bwd(ctx, order, g, 1.0, gt)
     with pytest.raises(B.SatError) as e:
@@ -153,7 +147,8 @@ def test_gradient(B, ctx, n, vocabulary, kind, d, t):
     count = np.bincount(tokens, minlength=vocabulary)[:, None]
     tol = (66 + count / 256) * U * mag
     within(host(gt), want, tol, "gradient")
-    assert guarded(full, d) and bool((gt[order._keep[2] == 0] == 0).all())
+    none = torch.from_numpy(mag.sum(1) == 0).cuda()
+    assert guarded(full, d) and bool((gt[none] == 0).all())
     first = gt.clone()
     B.sat_embed_bwd(ctx, order, g, scale, gt)
     assert torch.equal(first, gt)                                               # the same bits
@@ -161,7 +156,7 @@ def test_gradient(B, ctx, n, vocabulary, kind, d, t):
     B.sat_embed_bwd(ctx, order, g, scale, gt, accumulate=True)
     B.sat_sync_status(ctx)
     within(host(gt), want + 2.5, tol + U * np.abs(want + 2.5), "added")
-    assert guarded(full, d) and bool((gt[order._keep[2] == 0] == 2.5).all())
+    assert guarded(full, d) and bool((gt[none] == 2.5).all())
 
 
 def test_one_order_for_two_tables(B, ctx):
@@ -265,12 +260,12 @@ def test_refusals(B, ctx):
     K = lambda o=order, d=20, ty=0, g=p(out), ld=20, t=p(gt), ldt=20, acc=0: lib.sat_embed_bwd(ctx, None if o is None else C.byref(o), d, ty, g, ld, 1.0, t, ldt, acc)
 
     def changed(**kw):
-        o = B.sat_token_order(order.tokens, order.index, order.seen, order.n, order.vocabulary)
+        o = B.sat_token_order(order.tokens, order.index, order.n, order.vocabulary)
         for k, v in kw.items():
             setattr(o, k, v)
         return o
 
-    for o in (None, changed(tokens=None), changed(index=None), changed(seen=None), changed(n=-1), changed(n=2 ** 31), changed(vocabulary=0), changed(vocabulary=2 ** 31 - 1)):
+    for o in (None, changed(tokens=None), changed(index=None), changed(n=-1), changed(n=2 ** 31), changed(vocabulary=0), changed(vocabulary=2 ** 31 - 1)):
         assert S(o) == B.SAT_EINVAL and K(o=o) == B.SAT_EINVAL
     assert S(order, None) == B.SAT_EINVAL
     for bad in (K(d=0), K(d=21), K(ty=5), K(g=None), K(g=p(out) + 8), K(ld=22), K(t=None), K(t=p(gt) + 4), K(ldt=16), K(acc=3), K(ty=2)):
