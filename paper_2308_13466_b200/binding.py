@@ -12,6 +12,7 @@ import ctypes as C
 import os
 
 import numpy as np
+import torch
 
 from .build import lib_path
 
@@ -551,64 +552,64 @@ _lib.sat_embed_fwd.argtypes = [_P, _L, _P, _I, _I, _I, C.c_int, _P, _I, _F, _P, 
 _lib.sat_token_sort.argtypes = [_P, _P, _I, _P]
 _lib.sat_embed_bwd.argtypes = [_P, _P, _I, C.c_int, _P, _I, _F, _P, _I, C.c_int]
 _lib.sat_distill_grad.argtypes = [_P, _L, _I, C.c_int, _P, _I, _I, _P, _P, _F, _F, _P, _P, _F, _P, _P, _P, _I]
-_ROW_TYPES = {"torch.float32": SAT_F32, "torch.bfloat16": SAT_BF16, "torch.float16": SAT_F16}
+_ROW_TYPES = {torch.float32: SAT_F32, torch.bfloat16: SAT_BF16, torch.float16: SAT_F16}
 
 
-def _row_type(t) -> int:
-    code = _ROW_TYPES.get(str(t.dtype))
-    assert code is not None, "rows are fp32, bf16 or fp16"
-    return code
+def _first(t):
+    """Of a CUDA matrix with contiguous rows of fp32, bf16 or fp16: device, type, and what the others of a call are held to."""
+    dtype = t.dtype
+    dev = t.get_device()
+    assert dev >= 0 and dtype in _ROW_TYPES, "rows are CUDA tensors of fp32, bf16 or fp16"
+    return dev, dtype
 
 
-def _typed(t, like=None):
-    """Pointer and row stride of a CUDA matrix with contiguous rows; of the type and on the device of `like`, where given."""
+def _typed(t, dev, dtype):
+    """Pointer and row stride of such a matrix, of this type and on this device."""
     (r, c), (s0, s1) = t.shape, t.stride()
-    assert t.is_cuda and (s1 == 1 or c <= 1) and (like is None or (t.dtype == like.dtype and t.device == like.device))
+    assert t.dtype is dtype and t.get_device() == dev and (s1 == 1 or c <= 1)
     return t.data_ptr(), s0 if r > 1 else max(s0, c)
 
 
-def _f32(t, count: int, like):
-    """Pointer of a CUDA fp32 tensor of `count` elements without gaps, on the device of `like`; None stays None."""
+def _vec(t, dev, dtype, count: int):
+    """Pointer of a CUDA tensor of `count` elements without gaps, of this type and on this device; None stays None."""
     if t is None:
         return None
-    assert t.device == like.device and (f := t.dtype).itemsize == 4 and f.is_floating_point and t.is_contiguous() and t.numel() == count
-    return t.data_ptr()
-
-
-def _i32(t, count: int, like):
-    """... of an int32 tensor"""
-    if t is None:
-        return None
-    assert t.device == like.device and (f := t.dtype).itemsize == 4 and f.is_signed and not f.is_floating_point and t.is_contiguous() and t.numel() == count
+    assert t.dtype is dtype and t.get_device() == dev and t.numel() == count and t.is_contiguous()
     return t.data_ptr()
 
 
 def sat_layernorm_fwd(ctx, x, gamma, beta, eps: float, y, mean=None, rstd=None):
     """y = (x - mean(x)) / sqrt(var(x) + eps) gamma + beta by rows; mean and rstd [rows] receive what the backward call takes.  y may be x."""
-    rows, d = x.shape
+    (rows, d), (dev, dtype), f = x.shape, _first(x), torch.float32
     assert y.shape == x.shape
-    _check(ctx, _lib.sat_layernorm_fwd(ctx, rows, d, _row_type(x), *_typed(x), _f32(gamma, d, x), _f32(beta, d, x), eps, *_typed(y, x), _f32(mean, rows, x),
-                                       _f32(rstd, rows, x)))
+    st = _lib.sat_layernorm_fwd(ctx, rows, d, _ROW_TYPES[dtype], *_typed(x, dev, dtype), _vec(gamma, dev, f, d), _vec(beta, dev, f, d), eps, *_typed(y, dev, dtype),
+                                _vec(mean, dev, f, rows), _vec(rstd, dev, f, rows))
+    if st:
+        _check(ctx, st)
 
 
 def sat_layernorm_bwd(ctx, x, g, gamma, mean, rstd, g_x=None, g_gamma=None, g_beta=None, accumulate: bool = False):
     """Gradients of sat_layernorm_fwd from that of y: g_x (may be g or x), and g_gamma, g_beta, overwritten or added to."""
-    rows, d = x.shape
+    (rows, d), (dev, dtype), f = x.shape, _first(x), torch.float32
     assert g.shape == x.shape and (g_x is None or g_x.shape == x.shape)
-    _check(ctx, _lib.sat_layernorm_bwd(ctx, rows, d, _row_type(x), *_typed(x), *_typed(g, x), _f32(gamma, d, x), _f32(mean, rows, x), _f32(rstd, rows, x),
-                                       *((None, 0) if g_x is None else _typed(g_x, x)), _f32(g_gamma, d, x), _f32(g_beta, d, x), 1 if accumulate else 0))
+    st = _lib.sat_layernorm_bwd(ctx, rows, d, _ROW_TYPES[dtype], *_typed(x, dev, dtype), *_typed(g, dev, dtype), _vec(gamma, dev, f, d), _vec(mean, dev, f, rows),
+                                _vec(rstd, dev, f, rows), *((None, 0) if g_x is None else _typed(g_x, dev, dtype)), _vec(g_gamma, dev, f, d), _vec(g_beta, dev, f, d),
+                                1 if accumulate else 0)
+    if st:
+        _check(ctx, st)
 
 
 def sat_embed_fwd(ctx, tokens, table, scale: float, padding: int, out):
     """out[i] = scale table[tokens[i]] (tokens: CUDA int32 [n]); a row of zeros where tokens[i] is `padding` (-1: no token pads)."""
-    n, d = out.shape
+    (n, d), (dev, dtype) = out.shape, _first(out)
     assert table.shape[1] == d
-    _check(ctx, _lib.sat_embed_fwd(ctx, n, _i32(tokens, n, out), table.shape[0], padding, d, _row_type(out), *_typed(table, out), scale, *_typed(out)))
+    st = _lib.sat_embed_fwd(ctx, n, _vec(tokens, dev, torch.int32, n), table.shape[0], padding, d, _ROW_TYPES[dtype], *_typed(table, dev, dtype), scale, *_typed(out, dev, dtype))
+    if st:
+        _check(ctx, st)
 
 
 def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
     """Room for the order of n tokens on `device` (default: the current CUDA device)."""
-    import torch
     assert n >= 0 and vocabulary > 0
     device = torch.device("cuda") if device is None else device
     tokens, index = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(2))
@@ -619,26 +620,31 @@ def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
 
 def sat_token_sort(ctx, tokens, padding: int, order: sat_token_order):
     """order <- the positions of tokens (CUDA int32 [n]) by token"""
-    _check(ctx, _lib.sat_token_sort(ctx, _i32(tokens, order.n, order._keep[0]), padding, C.byref(order)))
+    st = _lib.sat_token_sort(ctx, _vec(tokens, order._keep[0].get_device(), torch.int32, order.n), padding, C.byref(order))
+    if st:
+        _check(ctx, st)
 
 
 def sat_embed_bwd(ctx, order: sat_token_order, g, scale: float, g_table, accumulate: bool = False):
     """g_table (CUDA fp32 [vocabulary, d]) (+)= scale times the sum of the rows of g by token"""
-    n, d = g.shape
-    assert n == order.n and g_table.shape == (order.vocabulary, d) and g_table.device == g.device
-    _check(ctx, _lib.sat_embed_bwd(ctx, C.byref(order), d, _row_type(g), *_typed(g), scale, *_rows(g_table), 1 if accumulate else 0))
+    (n, d), (dev, dtype) = g.shape, _first(g)
+    assert n == order.n and g_table.shape == (order.vocabulary, d) and order._keep[0].get_device() == dev
+    st = _lib.sat_embed_bwd(ctx, C.byref(order), d, _ROW_TYPES[dtype], *_typed(g, dev, dtype), scale, *_typed(g_table, dev, torch.float32), 1 if accumulate else 0)
+    if st:
+        _check(ctx, st)
 
 
 def sat_distill_grad(ctx, z, top_ids, top_logits, temperature: float, hard: float, labels, row_weight, weight: float, loss_sum=None, g=None, row_loss=None):
     """Loss between the logits z and a teacher's top logits (CUDA int32 and fp32 [rows, k]) and, with weight `hard`, the labels (CUDA int32 [rows] or
     None); loss_sum (CUDA float64 scalar) += the weighted sum, row_loss [rows] the rows' losses, g the gradient (may be z)."""
-    rows, classes = z.shape
+    (rows, classes), (dev, dtype), f, i = z.shape, _first(z), torch.float32, torch.int32
     k = 0 if top_ids is None else top_ids.shape[1]
-    assert (g is None or g.shape == z.shape) and (loss_sum is None or (loss_sum.device == z.device and loss_sum.dtype.itemsize == 8 and loss_sum.dtype.is_floating_point
-                                                                       and loss_sum.numel() == 1))
-    _check(ctx, _lib.sat_distill_grad(ctx, rows, classes, _row_type(z), *_typed(z), k, _i32(top_ids, rows * k, z), _f32(top_logits, rows * k, z), temperature, hard,
-                                      _i32(labels, rows, z), _f32(row_weight, rows, z), weight, None if loss_sum is None else loss_sum.data_ptr(),
-                                      _f32(row_loss, rows, z), *((None, 0) if g is None else _typed(g, z))))
+    assert g is None or g.shape == z.shape
+    st = _lib.sat_distill_grad(ctx, rows, classes, _ROW_TYPES[dtype], *_typed(z, dev, dtype), k, _vec(top_ids, dev, i, rows * k), _vec(top_logits, dev, f, rows * k), temperature, hard,
+                               _vec(labels, dev, i, rows), _vec(row_weight, dev, f, rows), weight, _vec(loss_sum, dev, torch.float64, 1), _vec(row_loss, dev, f, rows),
+                               *((None, 0) if g is None else _typed(g, dev, dtype)))
+    if st:
+        _check(ctx, st)
 
 
 def sat_dense_tn_static(stream: int, A, Bm, out):

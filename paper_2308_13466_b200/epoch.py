@@ -23,6 +23,22 @@ def _buf(rows: int, d: int, device) -> torch.Tensor:
     return full[:rows, :d]
 
 
+class TokenInputs:
+    """Learned inputs of a partitioned graph: every node has a token, a row of a table is its features.  Holds the tokens in global id order, and the order in
+    which the gradients of the inner rows of all partitions and, behind them, of their halo rows are added up by token; made once for a graph and its tokens."""
+
+    def __init__(self, ep: "SatEpoch", tokens: torch.Tensor, vocabulary: int, padding: int = -1, scale: float = 1.0):
+        assert ep.dims[0] % 4 == 0, "the width of learned inputs is a multiple of 4"
+        lists = [B.sat_part_lists(ep.ctx, m) for m in range(ep.M)]
+        gids = np.concatenate([p["inner_gid"] for p in lists] + [p["halo_gid"] for p in lists])
+        self.tokens, self.vocabulary, self.padding, self.scale = tokens, vocabulary, padding, scale
+        rows = tokens[torch.from_numpy(gids.astype(np.int64)).to(tokens.device)].contiguous()
+        self.order = B.new_token_order(rows.numel(), vocabulary, tokens.device)
+        B.sat_token_sort(ep.ctx, rows, padding, self.order)
+        self.x = _buf(ep.n, ep.dims[0], ep.device)
+        self.g = _buf(ep.n + ep.nb, ep.dims[0], ep.device)
+
+
 class SatEpoch:
     """Holds a context, the partitioned graph, the cache ring and the activation / gradient buffers
     of a GCN with layer widths `dims`, and runs epochs either with one launch set for all
@@ -240,3 +256,54 @@ class SatEpoch:
         if lr is not None:
             keys = [(l, k) for l, p in enumerate(params) for k in p]
             B.sat_sgd_steps(ctx, [params[l][k] for l, k in keys], [self.gat_grads[l][k] for l, k in keys], lr)
+
+    # ---- learned inputs, normalised layers, a teacher ----------------------------------
+    NORM_EPS = 1e-5
+
+    def step_tokens(self, inputs: TokenInputs, params, pred, lr: float | None = None, teacher=None):
+        """One SAT epoch of a network whose nodes have learned inputs and whose hidden rows are normalised, all partitions per launch:
+            x_v = scale table[token_v];  per layer  z = P h W + b;  hidden ones  h = norm(ReLU(z)) gamma + beta, which is what is pushed and pulled;
+        the objective is that of the labels or, with `teacher`, distillation from its top logits.
+        params: dict(table [vocabulary, d0], W, b (lists, a layer each), gamma, beta (lists, a hidden layer each)) of CUDA fp32 tensors; the gradients land in
+        self.token_grads (same keys).  teacher: dict(ids int32 [n, k], logits fp32 [n, k], temperature, hard) of CUDA tensors in partition-major row order;
+        with hard > 0 the labels (int32) count as well.  The inputs of halo nodes are exact, so the table's gradient has their part too; the pulled rows of
+        the other layers are constants of the epoch."""
+        ctx, L, m = self.ctx, self.L, B.SAT_ALL_PARTS
+        dev, f = self.device, torch.float32
+        if not hasattr(self, "token_grads"):
+            self.token_grads = {k: torch.zeros_like(v) if k == "table" else [torch.zeros_like(t) for t in v] for k, v in params.items()}
+            self.normed = [None] + [_buf(self.n, d, dev) for d in self.dims[1:-1]]
+            self.norm_stats = [None] + [tuple(torch.empty(self.n, dtype=f, device=dev) for _ in range(2)) for _ in self.dims[1:-1]]
+        gr = self.token_grads
+        if self._halo_state is not None:
+            self.halo       # an earlier epoch's rows, before this one's push may overwrite them
+        self.loss_sum.zero_()
+        B.sat_embed_fwd(ctx, inputs.tokens, params["table"], inputs.scale, inputs.padding, inputs.x)
+        for l in range(1, L + 1):
+            act = B.SAT_ACT_RELU if l < L else B.SAT_ACT_NONE
+            if l == 1:
+                B.sat_layer_fwd(ctx, m, l, inputs.x, None, params["W"][0], params["b"][0], act | B.SAT_FWD_INPUT_GLOBAL, self.H[l])
+            else:
+                hv = self._halo[:, :self.dims[l - 1]]
+                B.sat_predict(ctx, l - 1, m, pred[l - 2] if pred is not None else None, 0, hv)
+                B.sat_layer_fwd(ctx, m, l, self.normed[l - 1], hv, params["W"][l - 1], params["b"][l - 1], act, self.H[l])
+            if l < L:
+                B.sat_layernorm_fwd(ctx, self.H[l], params["gamma"][l - 1], params["beta"][l - 1], self.NORM_EPS, self.normed[l], *self.norm_stats[l])
+                B.sat_cache_update(ctx, m, l, self.normed[l])
+        if teacher is None:
+            kind = B.SAT_LOSS_SOFTMAX_CE if self.loss == "ce" else B.SAT_LOSS_SIGMOID_BCE
+            B.sat_loss_grad(ctx, m, kind, self.H[L], self.labels, self.loss_sum, self.G[L])
+        else:
+            B.sat_distill_grad(ctx, self.H[L], teacher["ids"], teacher["logits"], teacher["temperature"], teacher["hard"], self.labels if teacher["hard"] > 0 else None,
+                               None, 1.0 / self.n, self.loss_sum, self.G[L])
+        for l in range(L, 0, -1):
+            if l == 1:
+                B.sat_layer_bwd(ctx, m, l, self.G[l], params["W"][0], gr["W"][0], gr["b"][0], 0, inputs.g[:self.n], inputs.g[self.n:] if self.nb else None)
+                break
+            B.sat_layer_bwd(ctx, m, l, self.G[l], params["W"][l - 1], gr["W"][l - 1], gr["b"][l - 1], 0, self.G[l - 1])
+            B.sat_layernorm_bwd(ctx, self.H[l - 1], self.G[l - 1], params["gamma"][l - 2], *self.norm_stats[l - 1], self.G[l - 1], gr["gamma"][l - 2], gr["beta"][l - 2])
+        B.sat_embed_bwd(ctx, inputs.order, inputs.g, inputs.scale, gr["table"])
+        B.sat_cache_commit(ctx)
+        if lr is not None:
+            flat = lambda p: [p["table"]] + [t for k in ("W", "b", "gamma", "beta") for t in p[k]]
+            B.sat_sgd_steps(ctx, flat(params), flat(gr), lr)
