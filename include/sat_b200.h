@@ -598,7 +598,7 @@ sat_status sat_layernorm_bwd(sat_ctx *ctx, int64_t rows, int32_t d, int type, co
  *            token gives a row of zeros too, has no gradient, and sat_sync_status returns SAT_EDATA once.
  *   table    DEVICE [vocabulary x ld_table], of the same type as out
  *
- * sat_token_sort puts the positions of a batch in the order that its gradient is added up in: stable, by token.  The arrays are the caller's (DEVICE), one
+ * sat_token_sort puts the positions of a batch in the order that its gradient is added up in: stable, by token.  The arrays are the caller's (DEVICE, others than the batch's own), one
  * order serves any number of sat_embed_bwd calls, of tables of any width:
  *   tokens [n], index [n]   the tokens in ascending order and where each of them stands in the batch; padding and tokens outside the vocabulary are
  *                           listed last, as the token `vocabulary`

@@ -416,7 +416,7 @@ extern "C" sat_status sat_token_sort(sat_ctx *ctx, const int32_t *tokens, int32_
     CHECK_CTX(ctx);
     SAT_TRY(order_check(ctx, order, "sat_token_sort"));
     const int64_t n = order->n;
-    if (n > 0 && !tokens) return sat_fail(ctx, SAT_EINVAL, "sat_token_sort: null tokens");
+    if (n > 0 && (!tokens || tokens == order->tokens || tokens == order->index)) return sat_fail(ctx, SAT_EINVAL, "sat_token_sort: null tokens, or in the place of their order");
     ProfScope prof(ctx, SATK_EMBED, 12.0 * (double)n, 0.0);
     if (n == 0) return SAT_OK;
     int all = 1;   // bits of the largest key, which is `vocabulary`
@@ -558,6 +558,84 @@ __device__ __forceinline__ void embed_zero(const EmbedBwd &p, int64_t v0)
     }
 }
 
+// The long tokens.  A block looks at EMB_WINDOW borders and 128 columns; a warp adds up a token of up to 32 runs, the block one of more: as many runs at a
+// time as rows of 128 columns or less lie in its warps side by side, these rows' sums in order at the end.
+#define EMB_WINDOW 256
+__global__ void __launch_bounds__(1024)
+k_embed_join(EmbedBwd p)
+{
+    sat_grid_wait();
+    constexpr int NT = 1024;
+    __shared__ int32_t list[EMB_WINDOW], heavy[EMB_WINDOW];
+    __shared__ int32_t n_list, n_heavy;
+    __shared__ float4 red[NT];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) n_list = n_heavy = 0;
+    __syncthreads();
+    const int64_t b0 = (int64_t)blockIdx.x * EMB_WINDOW + 1;
+    if (threadIdx.x < EMB_WINDOW && b0 + threadIdx.x < p.runs) {
+        const int64_t e = (b0 + threadIdx.x) * p.len;
+        const int32_t t = __ldg(p.tokens + e);
+        // its first border, and there is another one
+        if (__ldg(p.tokens + e - 1) == t && (uint32_t)t < (uint32_t)p.vocabulary && !(e > p.len && __ldg(p.tokens + e - p.len - 1) == t) && e + p.len < p.n &&
+            __ldg(p.tokens + e + p.len) == t)
+            list[atomicAdd(&n_list, 1)] = threadIdx.x;   // (in any order: they have nothing to do with one another)
+    }
+    __syncthreads();
+    const int32_t col0 = (int32_t)blockIdx.y * 128, width = p.d - col0 < 128 ? p.d - col0 : 128;
+    auto row = [&](int64_t run, int which, int32_t col) { return __ldcg(reinterpret_cast<const float4 *>(p.part + (run * 2 + which) * p.ld_part + col)); };
+    auto add = [](float4 &s, const float4 &v) { s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w; };
+    for (int i = warp; i < n_list; i += NT / 32) {
+        const int64_t b = b0 + list[i];
+        const int32_t t = __ldg(p.tokens + b * p.len);
+        const bool in = b + lane < p.runs && __ldg(p.tokens + (b + lane) * p.len) == t;
+        const unsigned runs = __ballot_sync(0xffffffffu, in);   // (from the lowest bit up)
+        if (runs == 0xffffffffu) {
+            if (lane == 0) heavy[atomicAdd(&n_heavy, 1)] = list[i];
+            continue;
+        }
+        if (4 * lane >= width) continue;
+        float4 s = row(b - 1, 0, col0 + 4 * lane);
+        const int count = __popc(runs);
+#pragma unroll 4
+        for (int r = 0; r < count; ++r) add(s, row(b + r, 1, col0 + 4 * lane));
+        const float f[4] = {s.x, s.y, s.z, s.w};
+        embed_put<4>(p, t, col0 + 4 * lane, f);
+    }
+    __syncthreads();
+    const int quads = (width + 3) / 4, side = NT / quads, mine = threadIdx.x / quads, quad = threadIdx.x % quads;
+    for (int i = 0; i < n_heavy; ++i) {
+        const int64_t b = b0 + heavy[i];
+        const int32_t t = __ldg(p.tokens + b * p.len);
+        int64_t lo = b;   // the first run that does not begin with t
+        for (int n = NT; n == NT; lo += n) {
+            const int64_t r = lo + threadIdx.x;
+            n = __syncthreads_count(r < p.runs && __ldg(p.tokens + (r < p.runs ? r : 0) * p.len) == t);
+        }
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (mine < side) {
+            if (mine == 0) s = row(b - 1, 0, col0 + 4 * quad);
+#pragma unroll 8
+            for (int64_t r = b + mine; r < lo; r += side) add(s, row(r, 1, col0 + 4 * quad));
+        }
+        red[threadIdx.x] = s;
+        __syncthreads();
+        int left = side;
+        while (left > 1) {
+            const int half = (left + 1) / 2;
+            if (mine + half < left) add(red[threadIdx.x], red[threadIdx.x + half * quads]);
+            __syncthreads();
+            left = half;
+        }
+        if (mine == 0) {
+            s = red[quad];
+            const float f[4] = {s.x, s.y, s.z, s.w};
+            embed_put<4>(p, t, col0 + 4 * quad, f);
+        }
+        __syncthreads();
+    }
+}
+
 template <typename T, int TPR>
 __global__ void __launch_bounds__(256, 3)
 k_embed_bwd(EmbedBwd p, const T *__restrict__ g)
@@ -657,83 +735,6 @@ k_embed_bwd(EmbedBwd p, const T *__restrict__ g)
     put(true);
 }
 
-// The long tokens.  A block looks at EMB_WINDOW borders and 128 columns; a warp adds up a token of up to 32 runs, the block one of more: as many runs at a
-// time as rows of 128 columns or less lie in its warps side by side, these rows' sums in order at the end.
-#define EMB_WINDOW 256
-__global__ void __launch_bounds__(1024)
-k_embed_join(EmbedBwd p)
-{
-    sat_grid_wait();
-    __shared__ int32_t list[EMB_WINDOW], heavy[EMB_WINDOW];
-    __shared__ int32_t n_list, n_heavy;
-    __shared__ float4 red[1024];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) n_list = n_heavy = 0;
-    __syncthreads();
-    const int64_t b0 = (int64_t)blockIdx.x * EMB_WINDOW + 1;
-    if (threadIdx.x < EMB_WINDOW && b0 + threadIdx.x < p.runs) {
-        const int64_t e = (b0 + threadIdx.x) * p.len;
-        const int32_t t = __ldg(p.tokens + e);
-        // its first border, and there is another one
-        if (__ldg(p.tokens + e - 1) == t && (uint32_t)t < (uint32_t)p.vocabulary && !(e > p.len && __ldg(p.tokens + e - p.len - 1) == t) && e + p.len < p.n &&
-            __ldg(p.tokens + e + p.len) == t)
-            list[atomicAdd(&n_list, 1)] = threadIdx.x;   // (in any order: they have nothing to do with one another)
-    }
-    __syncthreads();
-    const int32_t col0 = (int32_t)blockIdx.y * 128, width = p.d - col0 < 128 ? p.d - col0 : 128;
-    auto row = [&](int64_t run, int which, int32_t col) { return __ldcg(reinterpret_cast<const float4 *>(p.part + (run * 2 + which) * p.ld_part + col)); };
-    auto add = [](float4 &s, const float4 &v) { s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w; };
-    for (int i = warp; i < n_list; i += 32) {
-        const int64_t b = b0 + list[i];
-        const int32_t t = __ldg(p.tokens + b * p.len);
-        const bool in = b + lane < p.runs && __ldg(p.tokens + (b + lane) * p.len) == t;
-        const unsigned runs = __ballot_sync(0xffffffffu, in);   // (from the lowest bit up)
-        if (runs == 0xffffffffu) {
-            if (lane == 0) heavy[atomicAdd(&n_heavy, 1)] = list[i];
-            continue;
-        }
-        if (4 * lane >= width) continue;
-        float4 s = row(b - 1, 0, col0 + 4 * lane);
-        const int count = __popc(runs);
-#pragma unroll 4
-        for (int r = 0; r < count; ++r) add(s, row(b + r, 1, col0 + 4 * lane));
-        const float f[4] = {s.x, s.y, s.z, s.w};
-        embed_put<4>(p, t, col0 + 4 * lane, f);
-    }
-    __syncthreads();
-    const int quads = (width + 3) / 4, side = 1024 / quads, mine = threadIdx.x / quads, quad = threadIdx.x % quads;
-    for (int i = 0; i < n_heavy; ++i) {
-        const int64_t b = b0 + heavy[i];
-        const int32_t t = __ldg(p.tokens + b * p.len);
-        int64_t lo = b;   // the first run that does not begin with t
-        for (int n = 1024; n == 1024; lo += n) {
-            const int64_t r = lo + threadIdx.x;
-            n = __syncthreads_count(r < p.runs && __ldg(p.tokens + (r < p.runs ? r : 0) * p.len) == t);
-        }
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (mine < side) {
-            if (mine == 0) s = row(b - 1, 0, col0 + 4 * quad);
-#pragma unroll 8
-            for (int64_t r = b + mine; r < lo; r += side) add(s, row(r, 1, col0 + 4 * quad));
-        }
-        red[threadIdx.x] = s;
-        __syncthreads();
-        int left = side;
-        while (left > 1) {
-            const int half = (left + 1) / 2;
-            if (mine + half < left) add(red[threadIdx.x], red[threadIdx.x + half * quads]);
-            __syncthreads();
-            left = half;
-        }
-        if (mine == 0) {
-            s = red[quad];
-            const float f[4] = {s.x, s.y, s.z, s.w};
-            embed_put<4>(p, t, col0 + 4 * quad, f);
-        }
-        __syncthreads();
-    }
-}
-
 template <typename T>
 static void embed_bwd_launch(sat_ctx *ctx, EmbedBwd &p, int tpr, const void *g)
 {
@@ -759,12 +760,12 @@ extern "C" sat_status sat_embed_bwd(sat_ctx *ctx, const sat_token_order *order, 
     p.scale = scale, p.accumulate = accumulate, p.g_table = g_table, p.ld_part = (d + 7) & ~7;
     p.status = ctx->d_flag + 1;
     if (p.n == 0 && accumulate) return SAT_OK;
-    // lanes of a row: as many as it has pieces of 16 bytes; runs: as many as fill the SMs twice with the 24 warps that they hold, of 8 positions at least
+    // lanes of a row: as many as it has pieces of 16 bytes; runs: as many as fill the SMs four times with the 24 warps that they hold, of 8 positions at least
     const int32_t v = 16 / type_bytes(type), pieces = (d + v - 1) / v;
     const int tpr = pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
     p.slabs = (pieces + tpr - 1) / tpr;
-    p.len = (int32_t)std::max<int64_t>(8, cdiv64(p.n * p.slabs, (int64_t)ctx->sms * 48 * (32 / tpr)));
-    p.zero_rows = (int32_t)std::min<int64_t>(EMB_ZERO, std::max<int64_t>(32, cdiv64(order->vocabulary, ctx->sms * 8)));
+    p.len = (int32_t)std::max<int64_t>(8, cdiv64(p.n * p.slabs, (int64_t)ctx->sms * 96 * (32 / tpr)));
+    p.zero_rows = (int32_t)std::min<int64_t>(EMB_ZERO, std::max<int64_t>(32, cdiv64(order->vocabulary, ctx->sms * 3)));
     p.runs = cdiv64(p.n, p.len);
     if (p.runs * p.slabs >= INT32_MAX) return sat_fail(ctx, SAT_EINVAL, "sat_embed_bwd: too many rows of this width");
     if (p.runs > 2) {   // (a long token crosses two borders)

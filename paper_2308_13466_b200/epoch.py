@@ -85,6 +85,8 @@ class SatEpoch:
         self.H = self.G = self._halo = self._halo_state = self.X_in = self.X = self.labels = self._epoch_key = self._epoch_buf = None
         if hasattr(self, "gat_halo"):
             self.gat_halo = None
+        if hasattr(self, "normed"):
+            self.normed = self.norm_stats = None
 
     # ---- inputs -------------------------------------------------------------------
     def set_inputs(self, X: torch.Tensor, labels_perm: torch.Tensor):

@@ -267,7 +267,7 @@ def test_refusals(B, ctx):
 
     for o in (None, changed(tokens=None), changed(index=None), changed(n=-1), changed(n=2 ** 31), changed(vocabulary=0), changed(vocabulary=2 ** 31 - 1)):
         assert S(o) == B.SAT_EINVAL and K(o=o) == B.SAT_EINVAL
-    assert S(order, None) == B.SAT_EINVAL
+    assert S(order, None) == B.SAT_EINVAL and S(order, order.tokens) == B.SAT_EINVAL and S(order, order.index) == B.SAT_EINVAL
     for bad in (K(d=0), K(d=21), K(ty=5), K(g=None), K(g=p(out) + 8), K(ld=22), K(t=None), K(t=p(gt) + 4), K(ldt=16), K(acc=3), K(ty=2)):
         assert bad == B.SAT_EINVAL
     assert B.sat_launch_count(ctx) == before and bool((gt == 5).all()) and bool((out == 4).all())
