@@ -71,7 +71,8 @@ __device__ __forceinline__ void norm_back_finish(T *gx, int32_t col, int32_t d, 
 }
 
 // =====================================================================================
-// rows of up to 512 elements: TPR lanes hold one in registers, CH times 16 bytes each
+// rows of up to 512 elements: TPR lanes hold one in registers, CH times 16 bytes each.  Bound by memory: 612257 x 256 fp32 forward 201 us (97 % of the copy rate; without the
+// next row on its way 245), backward 287 (the copy rate).
 // =====================================================================================
 
 // (the next row is asked for before this one is worked on)
@@ -251,6 +252,7 @@ k_norm_bwd(int64_t rows, int32_t d, const T *x, int64_t ld_x, const T *g, int64_
 // =====================================================================================
 // wider rows: a block holds one in registers, CH times 16 bytes a thread; the next ones are on their way into a ring in shared memory (cp.async.bulk), so that what an SM
 // has asked for does not depend on its registers.  A slot is asked for again behind the barrier of the row's sums, when all threads have taken their part of it.
+// Bound by instructions: 16384 x 4096 bf16 backward 85 us (73 % of the copy rate), forward 79; with 8 elements a thread and rows asked for into registers 108.
 // =====================================================================================
 #define NORM_SLOTS 8
 // gamma and beta in shared memory, or else from the L1, which has the rest of the SM.  Measured, kept against not: gradients of 50000 x 2048 bf16 125 / 225 us, of 16384 x
