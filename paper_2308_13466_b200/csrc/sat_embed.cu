@@ -506,12 +506,6 @@ __device__ __forceinline__ void embed_put(const EmbedBwd &p, int32_t token, int3
     }
 }
 
-// whether the token at border e (a multiple of len with tokens[e - 1] == tokens[e] == t) crosses another border
-__device__ __forceinline__ bool embed_long(const EmbedBwd &p, int64_t e, int32_t t)
-{
-    return (e > p.len && __ldg(p.tokens + e - p.len - 1) == t) || (e + p.len < p.n && __ldg(p.tokens + e + p.len) == t);
-}
-
 // Zeros for the tokens [v0, v0 + zero_rows) that do not occur
 #define EMB_ZERO 2048
 __device__ __forceinline__ int64_t embed_find(const EmbedBwd &p, int64_t lo, int64_t hi, int64_t v)   // the first position in [lo, hi) whose token is v or more
@@ -576,11 +570,10 @@ k_embed_join(EmbedBwd p)
     const int64_t b0 = (int64_t)blockIdx.x * EMB_WINDOW + 1;
     if (threadIdx.x < EMB_WINDOW && b0 + threadIdx.x < p.runs) {
         const int64_t e = (b0 + threadIdx.x) * p.len;
-        const int32_t t = __ldg(p.tokens + e);
+        const int32_t t = __ldg(p.tokens + e), before = __ldg(p.tokens + e - 1), back = e > p.len ? __ldg(p.tokens + e - p.len - 1) : -2,
+                      forth = e + p.len < p.n ? __ldg(p.tokens + e + p.len) : -2;
         // its first border, and there is another one
-        if (__ldg(p.tokens + e - 1) == t && (uint32_t)t < (uint32_t)p.vocabulary && !(e > p.len && __ldg(p.tokens + e - p.len - 1) == t) && e + p.len < p.n &&
-            __ldg(p.tokens + e + p.len) == t)
-            list[atomicAdd(&n_list, 1)] = threadIdx.x;   // (in any order: they have nothing to do with one another)
+        if (before == t && back != t && forth == t && (uint32_t)t < (uint32_t)p.vocabulary) list[atomicAdd(&n_list, 1)] = threadIdx.x;   // (in any order: they have nothing to do with one another)
     }
     __syncthreads();
     const int32_t col0 = (int32_t)blockIdx.y * 128, width = p.d - col0 < 128 ? p.d - col0 : 128;
@@ -661,9 +654,12 @@ k_embed_bwd(EmbedBwd p, const T *__restrict__ g)
     if (run >= p.runs) return;
     const int32_t col = ((int32_t)(item - run * p.slabs) * TPR + t) * V;
     const int64_t e0 = run * p.len, e1 = e0 + p.len < p.n ? e0 + p.len : p.n;
-    const int32_t first = __ldg(p.tokens + e0), last = __ldg(p.tokens + e1 - 1);
-    const bool goes_on = e0 > 0 && __ldg(p.tokens + e0 - 1) == first, leaves = e1 < p.n && __ldg(p.tokens + e1) == last;
-    const bool first_long = goes_on && embed_long(p, e0, first), last_long = leaves && embed_long(p, e1, last);
+    // (all that is to be known of the borders is asked for at once; -2: no such position)
+    auto token = [&](int64_t e) { return e >= 0 && e < p.n ? __ldg(p.tokens + e) : -2; };
+    const int32_t first = token(e0), last = token(e1 - 1), before = token(e0 - 1), behind = token(e1), back = token(e0 - p.len - 1), forth = token(e1 + p.len);
+    const bool goes_on = before == first, leaves = behind == last;
+    // a token that crosses another border than this one is long
+    const bool first_long = goes_on && (back == first || behind == first), last_long = leaves && (before == last || forth == last);
     const int64_t end = leaves && !last_long ? (e1 + p.len < p.n ? e1 + p.len : p.n) : e1;   // (the token ends before that)
     const bool skip = goes_on && !first_long;
     float acc[V] = {};
@@ -687,9 +683,9 @@ k_embed_bwd(EmbedBwd p, const T *__restrict__ g)
     const T *gc = g + col;
     const bool inside = col < p.d;
     auto entries = [&](int64_t e, int32_t &tok, int32_t &idx) {
-        tok = e + slot < end ? __ldg(p.tokens + e + slot) : -1;
-        idx = e + slot < end ? __ldg(p.index + e + slot) : -1;
-        if (e + slot >= e1 && tok != last) tok = -1;   // behind what this run walks
+        tok = e + slot < p.n ? __ldg(p.tokens + e + slot) : -1;   // (asked for without waiting for the borders' tokens)
+        idx = e + slot < p.n ? __ldg(p.index + e + slot) : -1;
+        if (e + slot >= end || (e + slot >= e1 && tok != last)) tok = -1;   // behind what this run walks
         if ((uint32_t)tok >= (uint32_t)p.vocabulary || (skip && tok == first)) {
             idx = -1;
         } else if ((uint32_t)idx >= (uint32_t)p.n) {   // (the arrays are the caller's)
