@@ -244,6 +244,7 @@ k_tok_place(TokPass p)
         const int digit = (key[r] >> p.shift) & (digits - 1);
         int32_t at = tok_smem[digit] + rank[r];
         for (int w = 0; w < warp; ++w) at += all[w * digits + digit];
+        if ((uint32_t)at >= (uint32_t)p.n) continue;   // (only if somebody has changed the tokens meanwhile)
         if (p.pairs_out) {
             p.pairs_out[at] = make_int2(key[r], val[r]);
         } else {

@@ -1,7 +1,8 @@
 """Embedding lookup, the order of a batch of tokens and the table's gradient, against their definitions.
 
 The order is made of whole numbers and has to be equal, the lookup is one product rounded once.  Gradients: U = 2^-24 is fp32's half step; a token's c
-rows are added 32 at a time, these sums by eight warps and then the eight: below 64 + c / 256 additions one after the other, and two more roundings.
+rows are added in runs of at most 25 positions at these sizes, twice that where it crosses one border, the runs' sums up to 31 one after the other or by 32 threads and more side
+by side: below 64 + c / 256 additions one after the other, and two more roundings.
 """
 import numpy as np
 import pytest
