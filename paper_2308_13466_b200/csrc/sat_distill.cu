@@ -239,16 +239,17 @@ __device__ __forceinline__ DistillSum distill_join_lanes(DistillSum v, float cT)
     return v;
 }
 // Exponents of 2^((z - m) c): z c - o in one operation, o being m c rounded.  What that rounding leaves is the same for all z: a sum and a quotient are
-// multiplied by 2^left, which is exact.  A row whose largest logit is as large as a mask of the type's lowest value (DISTILL_FITS) takes the difference first
-// (`exact`), one thread's part of a row that is masked throughout adds up to zero.
-#define DISTILL_FITS 1e30f
+// multiplied by 2^left.  That keeps the numbers' accuracy while m c is small: below 2^21 half a step of o is 2^-4 at most, far beyond `left` is as large as any
+// exponent, and 2^left no number or none.  So no reference lies below -2 DISTILL_FITS: what a thread has so deep down (logits of -inf, finite masks, or no columns at
+// all) adds up to zero, as it should beside a row's largest logit that is not.  A row whose largest logit times c lies beyond DISTILL_FITS to either side takes the difference first (`exact`).
+#define DISTILL_FITS 1048576.f
 struct DistillScale {
     float c, o, left;
     __device__ __forceinline__ DistillScale(float m, float c_, bool exact = false) : c(c_)
     {
-        const float n = fminf(fmaxf(m, -DISTILL_FITS), DISTILL_FITS);
-        o = exact ? m : n * c_;
-        left = exact ? 0.f : fmaf(n, -c_, o);
+        const float mc = m * c_;
+        o = exact ? m : fmaxf(mc, -2.f * DISTILL_FITS);
+        left = exact || mc < -2.f * DISTILL_FITS ? 0.f : fmaf(m, -c_, mc);
     }
 };
 // 16 bytes of logits: their exponentials, by twos
@@ -353,7 +354,7 @@ struct DistillRow {
             y_among = HARD && en.y >= 0 && ((sh.table[(en.y >> 5) & 255] >> (en.y & 31)) & 1u);
         }
         sum = distill_join_lanes<HARD>(lane < W ? sh.sum[lane] : DistillSum{-INFINITY, 0.f, 0.f}, cT);
-        exact = !(fabsf(sum.m) <= DISTILL_FITS);
+        exact = !(fabsf(sum.m) * (HARD ? fmaxf(cT, LOG2E) : cT) <= DISTILL_FITS);
         if (exact) {   // (the same for the whole block) the sums once more
             const DistillScale cs(sum.m, cT, true), hs(sum.m, LOG2E, true);
             uint64_t s = 0, s1 = 0;
@@ -647,10 +648,10 @@ k_distill_long(Distill p, const T *z, T *g)
                 top = fmaxf(top, fmaxf(RowVec<T>::largest(raw[0]), RowVec<T>::largest(raw[1])));
                 if (top > m) {   // (rare after the first chunks)
                     const DistillScale ns(top, cT), ks(top, LOG2E);
-                    const float f = m == -INFINITY ? 0.f : ex2_fast((m - top) * cT) * ex2_fast(cs.left) * ex2_fast(-ns.left);
+                    const float f = ex2_fast(cs.o - ns.o);
                     s_2 = f2_mul(s_2, f2_pack(f, f));
                     if (HARD) {
-                        const float f1 = m == -INFINITY ? 0.f : ex2_fast((m - top) * LOG2E) * ex2_fast(hs.left) * ex2_fast(-ks.left);
+                        const float f1 = ex2_fast(hs.o - ks.o);
                         s1_2 = f2_mul(s1_2, f2_pack(f1, f1));
                     }
                     cs = ns, hs = ks, m = top;
