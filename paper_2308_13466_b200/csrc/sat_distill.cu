@@ -240,18 +240,19 @@ __device__ __forceinline__ DistillSum distill_join_lanes(DistillSum v, float cT)
 }
 // Exponents of 2^((z - m) c): z c - o in one operation, o being m c rounded.  What that rounding leaves is the same for all z: a sum and a quotient are
 // multiplied by 2^left.  That keeps the numbers' accuracy while m c is small: below 2^21 half a step of o is 2^-4 at most, far beyond `left` is as large as any
-// exponent, and 2^left no number or none.  So no reference lies below -2 DISTILL_FITS: what a thread has so deep down (logits of -inf, finite masks, or no columns at
-// all) adds up to zero, as it should beside a row's largest logit that is not.  A row whose largest logit times c lies beyond DISTILL_FITS to either side takes the difference first (`exact`).
-#define DISTILL_FITS 1048576.f
+// exponent, and 2^left no number or none.  So a thread's reference does not lie below -2 DISTILL_FITS T: what it has so deep down (logits of -inf, finite masks, or no columns at
+// all) adds up to zero, as it should beside a row's largest logit that is not.  A row whose largest logit lies beyond DISTILL_FITS T to either side takes the difference first (`exact`).
+#define DISTILL_FITS 7e5f   // times log2(e): just below 2^20
 struct DistillScale {
     float c, o, left;
     __device__ __forceinline__ DistillScale(float m, float c_, bool exact = false) : c(c_)
     {
-        const float mc = m * c_;
-        o = exact ? m : fmaxf(mc, -2.f * DISTILL_FITS);
-        left = exact || mc < -2.f * DISTILL_FITS ? 0.f : fmaf(m, -c_, mc);
+        o = exact ? m : m * c_;
+        left = exact ? 0.f : fmaf(m, -c_, o);
     }
 };
+// a thread's, at temperature T (1 for the label's term)
+__device__ __forceinline__ DistillScale distill_scale(float m, float T, float c) { return DistillScale(fmaxf(m, -2.f * DISTILL_FITS * T), c); }
 // 16 bytes of logits: their exponentials, by twos
 template <typename T, bool EXACT>
 __device__ __forceinline__ void distill_exp(const uint4 &raw, const DistillScale &sc, uint64_t (&e)[RowVec<T>::V / 2])
@@ -354,7 +355,7 @@ struct DistillRow {
             y_among = HARD && en.y >= 0 && ((sh.table[(en.y >> 5) & 255] >> (en.y & 31)) & 1u);
         }
         sum = distill_join_lanes<HARD>(lane < W ? sh.sum[lane] : DistillSum{-INFINITY, 0.f, 0.f}, cT);
-        exact = !(fabsf(sum.m) * (HARD ? fmaxf(cT, LOG2E) : cT) <= DISTILL_FITS);
+        exact = !(fabsf(sum.m) <= DISTILL_FITS * (HARD ? fminf(p.T, 1.f) : p.T));
         if (exact) {   // (the same for the whole block) the sums once more
             const DistillScale cs(sum.m, cT, true), hs(sum.m, LOG2E, true);
             uint64_t s = 0, s1 = 0;
@@ -528,7 +529,7 @@ k_distill_wide(Distill p, const T *z, T *g)
             sum.m = fmaxf(sum.m, RowVec<T>::largest(raw[j]));
         }
         {
-            const DistillScale cs(sum.m, cT), hs(sum.m, LOG2E);
+            const DistillScale cs = distill_scale(sum.m, p.T, cT), hs = distill_scale(sum.m, 1.f, LOG2E);
             uint64_t s_2 = 0, s1_2 = 0;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
@@ -626,7 +627,7 @@ k_distill_long(Distill p, const T *z, T *g)
             const uint32_t slot0 = slot;
             // sums relative to the largest logit so far
             float m = -INFINITY;
-            DistillScale cs(m, cT), hs(m, LOG2E);
+            DistillScale cs = distill_scale(m, p.T, cT), hs = distill_scale(m, 1.f, LOG2E);
             uint64_t s_2 = 0, s1_2 = 0;
             auto step = [&](uint32_t &s, uint32_t &ph) {
                 if (++s == DISTILL_SLOTS) s = 0, ph ^= 1u;
@@ -647,7 +648,7 @@ k_distill_long(Distill p, const T *z, T *g)
                 }
                 top = fmaxf(top, fmaxf(RowVec<T>::largest(raw[0]), RowVec<T>::largest(raw[1])));
                 if (top > m) {   // (rare after the first chunks)
-                    const DistillScale ns(top, cT), ks(top, LOG2E);
+                    const DistillScale ns = distill_scale(top, p.T, cT), ks = distill_scale(top, 1.f, LOG2E);
                     const float f = ex2_fast(cs.o - ns.o);
                     s_2 = f2_mul(s_2, f2_pack(f, f));
                     if (HARD) {
