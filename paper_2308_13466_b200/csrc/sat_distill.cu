@@ -28,6 +28,71 @@ struct Distill {
     int *status;
 };
 
+// A student that all but agrees with its teacher, at a high temperature.  KL = sum p d + log(s / st), d_j = (t_j - max t) / T - (z_j - max z) / T, is then a difference of numbers that are
+// larger by far, and T^2 brings what their rounding left back to size.  With u = d - sum p d the same is
+//     KL = log(1 + sum p (e^-u - 1 + u) + e^(sum p d) rest / st),     rest: the exponentials of the classes that the teacher does not name,
+// where nothing is negative and nothing cancels; e^-u - 1 + u has its series where u is small, and `rest` is added up by itself.  (A class that is named twice would be
+// in the sum twice: such rows keep what they have.)  Worked out behind the gradient, where little else is in registers, and called: 612257 x 47 with labels 76 us, inlined 82, worked out ahead of
+// the gradient 81 (called 96).  Without it 71, so temperatures of up to DISTILL_NEAR_FROM do: the other form's error, about 2^-21 in KL, is 2^-17 in the loss there.
+// sp has z - max z on entry and is left all zeros, as it is between rows.  `near` is the same for the lanes of a row; all lanes of the warp call.
+#define DISTILL_NEAR_FROM 4.f
+#define DISTILL_NEAR 0.125f   // of KL; beside more than that 2^-21 is small
+template <int TPR>
+__device__ __noinline__ float distill_near(const int32_t *ids, const float *logits, int32_t C, int32_t k, float cT, float inv_T, float *sp, int32_t stride, bool near, float kl)
+{
+    constexpr float TAKEN = -1e30f;   // what a class that the teacher names has in sp afterwards, times the lane's number; as far down logits add nothing to `rest`
+    const int t = threadIdx.x % TPR;
+    auto entry = [&](int32_t e, int32_t &id) {   // its logit; -inf: none
+        id = near && e < k ? __ldg(ids + e) : -1;
+        return (uint32_t)id < (uint32_t)C ? __ldg(logits + e) : -INFINITY;
+    };
+    float tm = -INFINITY, st = 0.f, mean = 0.f, sum = 0.f, rest = 0.f;
+    int32_t id;
+    for (int32_t e0 = 0; e0 < k; e0 += TPR) tm = fmaxf(tm, entry(e0 + t, id));
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, o));
+    for (int32_t e0 = 0; e0 < k; e0 += TPR) {
+        const float gap = entry(e0 + t, id) - tm, w = ex2_fast(gap * cT);
+        if (w > 0.f) st += w, mean = fmaf(w, gap - sp[id], mean);
+    }
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) {
+        st += __shfl_xor_sync(0xffffffffu, st, o);
+        mean += __shfl_xor_sync(0xffffffffu, mean, o);
+    }
+    mean /= st;
+    int twice = 0;
+    for (int32_t e0 = 0; e0 < k; e0 += TPR) {
+        const float gap = entry(e0 + t, id) - tm, w = ex2_fast(gap * cT), x = w > 0.f ? sp[id] : 0.f;
+        __syncwarp();
+        if (w > 0.f) sp[id] = TAKEN * (float)(t + 1);
+        __syncwarp();
+        if (!(w > 0.f)) continue;
+        if (x <= TAKEN || sp[id] != TAKEN * (float)(t + 1)) twice = 1;
+        const float u = (gap - x - mean) * inv_T;
+        if (fabsf(u) < 0.5f) {   // (the next term is 2^-24 of the first at most)
+            const float f = fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 40320.f, -1.f / 5040.f), 1.f / 720.f), -1.f / 120.f), 1.f / 24.f), -1.f / 6.f), 0.5f);
+            sum = fmaf(w, u * u * f, sum);
+        } else {   // (in two factors: a small weight may stand beside a large exponential)
+            const float half = expf(-0.5f * u);
+            sum += w * half * half + w * (u - 1.f);
+        }
+    }
+    __syncwarp();
+    for (int32_t c = t; near && c < C; c += TPR)
+        if (sp[c] > TAKEN) rest += ex2_fast(sp[c] * cT);
+    __syncwarp();
+    for (int32_t c = t; c < stride; c += TPR) sp[c] = 0.f;
+    __syncwarp();
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        rest += __shfl_xor_sync(0xffffffffu, rest, o);
+        twice |= __shfl_xor_sync(0xffffffffu, twice, o);
+    }
+    return near && !twice ? log1pf((sum + expf(mean * inv_T) * rest) / st) : kl;
+}
+
 // Up to 1,024 classes: TPR lanes hold a row in registers, CH times 16 bytes each, and up to NE of the teacher's entries each.  The teacher's probabilities and
 // the label meet their columns in shared memory (`sp`), which is all zeros between rows.  Few lanes a row, since what a row costs whatever its width (two sums
 // and maxima across its lanes, logarithms, quotients) is paid once a warp for its 32 / TPR rows.  Bound by instruction issue: 612257 x 47 fp32 with labels 71 us (16 lanes a row and
@@ -37,13 +102,14 @@ __host__ __device__ constexpr int distill_stride()   // floats of a row's `sp`: 
 {
     return TPR * CH * V + ((TPR * CH * V) % 32 == 0 && TPR < 8 ? 4 * TPR : 0);
 }
-template <typename T, int TPR, int CH, int NE, bool HARD>
+template <typename T, int TPR, int CH, int NE, bool HARD, bool NEAR>
 __global__ void __launch_bounds__(256, CH * RowVec<T>::V > 16 ? 2 : NE > 4 ? 3 : 4)
 k_distill_rows(Distill p, const T *z, T *g)
 {
     sat_grid_wait();
     constexpr int V = RowVec<T>::V, H = V / 2, RPW = 32 / TPR, STRIDE = distill_stride<TPR, CH, V>();
     extern __shared__ float4 distill_smem[];
+    __shared__ float2 kept[NEAR ? 256 / TPR : 1];   // KL and the label's term of a row that distill_near takes
     const int lane = threadIdx.x & 31, t = lane % TPR;
     const unsigned mates = TPR == 32 ? 0xffffffffu : ((1u << (TPR & 31)) - 1u) << (lane - t);
     float *sp = reinterpret_cast<float *>(distill_smem) + (threadIdx.x / TPR) * STRIDE;
@@ -149,63 +215,84 @@ k_distill_rows(Distill p, const T *z, T *g)
             if (HARD) s1 += __shfl_xor_sync(0xffffffffu, s1, o);
         }
         const bool soft_on = some && soft > 0.f, hard_on = HARD && y >= 0, dead = w == 0.f || !(soft_on || hard_on);
-        if (ok && t == 0 && (p.row_loss || p.loss_sum)) {
-            float loss = 0.f;
-            if (!dead) {
-                if (soft_on) loss = soft * p.T * p.T * (num * rcp_fast(st) * inv_T + (__logf(s) - __logf(st)));
-                if (hard_on) loss += p.hard * (__logf(s1) - (zy - m));
-            }
+        bool near = false, nears = false;   // nears: one of the warp's rows
+        auto put = [&](float kl, float label) {
+            const float loss = (1.f - p.hard) * p.T * p.T * kl + label;
             if (p.row_loss) p.row_loss[r] = loss;
-            if (p.loss_sum) acc += (double)w * (double)loss;
-        }
-        if (!g) continue;   // (the same for all threads)
-        const float a = soft_on ? w * soft * p.T : 0.f, b = hard_on ? w * p.hard : 0.f;
-        const float aq = a * rcp_fast(s), ap = soft_on ? a * rcp_fast(st) : 0.f, bq = HARD ? b * rcp_fast(s1) : 0.f;
-        const uint64_t aq_2 = f2_pack(aq, aq), bq_2 = f2_pack(bq, bq);
-        // a class that is named more than once: whose tag is found says that others are there, and then one adds after the other
-#pragma unroll
-        for (int e = 0; e < NE; ++e) {
-            if (e * TPR >= p.k) break;
-            const bool mine = id[e] >= 0 && soft_on;
-            const float val = ap * te[e], old = mine ? sp[id[e]] : 0.f;
-            __syncwarp();
-            if (mine) sp[id[e]] = __int_as_float(t);
-            __syncwarp();
-            const bool twice = __any_sync(0xffffffffu, mine && __float_as_int(sp[mine ? id[e] : 0]) != t);
-            __syncwarp();
-            if (mine) sp[id[e]] = twice ? old : old + val;
-            __syncwarp();
-            if (twice)
-                for (int i = 0; i < TPR; ++i) {
-                    if (mine && t == i) sp[id[e]] += val;
-                    __syncwarp();
-                }
-        }
-        if (HARD) {
-            if (hard_on && t == 0) sp[y] += b;
-            __syncwarp();
-        }
-#pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            const int32_t col = (j * TPR + t) * V;
-            if (col >= p.C) break;
-            float o[V];
-#pragma unroll
-            for (int i = 0; i < V; i += 4) {
-                float4 *at = reinterpret_cast<float4 *>(sp + col + i);
-                const float4 q = *at;
-                *at = make_float4(0.f, 0.f, 0.f, 0.f);
-                uint64_t out[2] = {f2_pack(-q.x, -q.y), f2_pack(-q.z, -q.w)};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {   // (exponentials once more: kept, they would take the registers of half of the warps)
-                    const uint64_t xx = x[j][i / 2 + h];
-                    if (HARD) out[h] = f2_fma(bq_2, f2_ex2(f2_mul(xx, c1_2)), out[h]);
-                    out[h] = f2_fma(aq_2, f2_ex2(f2_mul(xx, cT_2)), out[h]);
-                    const float2 f = f2_unpack(out[h]);
-                    o[i + 2 * h] = dead ? 0.f : f.x, o[i + 2 * h + 1] = dead ? 0.f : f.y;
-                }
+            if (p.loss_sum) acc += (double)(p.weight * (p.row_weight ? __ldg(p.row_weight + r) : 1.f)) * (double)loss;
+        };
+        if ((p.row_loss || p.loss_sum) && (NEAR || (ok && t == 0))) {
+            const float kl = soft_on && !dead ? num * rcp_fast(st) * inv_T + logf(s * rcp_fast(st)) : 0.f, label = hard_on && !dead ? p.hard * (logf(s1) - (zy - m)) : 0.f;
+            if (NEAR) {
+                near = ok && soft_on && !dead && kl < DISTILL_NEAR;
+                nears = __any_sync(0xffffffffu, near);
+                if (t == 0 && near) kept[threadIdx.x / TPR] = make_float2(kl, label);
             }
-            if (ok) row_store(g + r * p.ld_g, col, p.C, o);
+            if (t == 0 && ok && !near) put(kl, label);
+        }
+        if (!g) {   // (the same for all threads)
+            if (!NEAR || !nears) continue;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < H; ++i)
+                    if ((j * TPR + t) * V < p.C) *reinterpret_cast<float2 *>(sp + (j * TPR + t) * V + 2 * i) = f2_unpack(x[j][i]);
+        } else {
+            const float a = soft_on ? w * soft * p.T : 0.f, b = hard_on ? w * p.hard : 0.f;
+            const float aq = a * rcp_fast(s), ap = soft_on ? a * rcp_fast(st) : 0.f, bq = HARD ? b * rcp_fast(s1) : 0.f;
+            const uint64_t aq_2 = f2_pack(aq, aq), bq_2 = f2_pack(bq, bq);
+            // a class that is named more than once: whose tag is found says that others are there, and then one adds after the other
+#pragma unroll
+            for (int e = 0; e < NE; ++e) {
+                if (e * TPR >= p.k) break;
+                const bool mine = id[e] >= 0 && soft_on;
+                const float val = ap * te[e], old = mine ? sp[id[e]] : 0.f;
+                __syncwarp();
+                if (mine) sp[id[e]] = __int_as_float(t);
+                __syncwarp();
+                const bool twice = __any_sync(0xffffffffu, mine && __float_as_int(sp[mine ? id[e] : 0]) != t);
+                __syncwarp();
+                if (mine) sp[id[e]] = twice ? old : old + val;
+                __syncwarp();
+                if (twice)
+                    for (int i = 0; i < TPR; ++i) {
+                        if (mine && t == i) sp[id[e]] += val;
+                        __syncwarp();
+                    }
+            }
+            if (HARD) {
+                if (hard_on && t == 0) sp[y] += b;
+                __syncwarp();
+            }
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int32_t col = (j * TPR + t) * V;
+                if (col >= p.C) break;
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; i += 4) {
+                    float4 *at = reinterpret_cast<float4 *>(sp + col + i);
+                    const float4 q = *at;
+                    const float2 x0 = f2_unpack(x[j][i / 2]), x1 = f2_unpack(x[j][i / 2 + 1]);
+                    *at = NEAR && nears ? make_float4(x0.x, x0.y, x1.x, x1.y) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    uint64_t out[2] = {f2_pack(-q.x, -q.y), f2_pack(-q.z, -q.w)};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {   // (exponentials once more: kept, they would take the registers of half of the warps)
+                        const uint64_t xx = x[j][i / 2 + h];
+                        if (HARD) out[h] = f2_fma(bq_2, f2_ex2(f2_mul(xx, c1_2)), out[h]);
+                        out[h] = f2_fma(aq_2, f2_ex2(f2_mul(xx, cT_2)), out[h]);
+                        const float2 f = f2_unpack(out[h]);
+                        o[i + 2 * h] = dead ? 0.f : f.x, o[i + 2 * h + 1] = dead ? 0.f : f.y;
+                    }
+                }
+                if (ok) row_store(g + r * p.ld_g, col, p.C, o);
+            }
+        }
+        if (NEAR && nears) {
+            __syncwarp();
+            const float2 had = kept[threadIdx.x / TPR];
+            const float kl = distill_near<TPR>(p.ids + r * p.k, p.logits + r * p.k, p.C, p.k, cT, 1.f / p.T, sp, STRIDE, near, had.x);
+            if (t == 0 && near) put(kl, had.y);
         }
         __syncwarp();
     }
@@ -321,6 +408,7 @@ struct DistillShared {
         if (threadIdx.x == 0) twice = 0;
     }
 };
+#define DISTILL_TELLS(NT) ((NT) - 32)   // the thread that works out a row's loss: of the last warp, which has no entries unless there are many (the first: 1.3 % of 8192 x 50001 bf16)
 template <int NT>
 __device__ __forceinline__ void distill_sync() { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); }
 
@@ -423,7 +511,8 @@ struct DistillRow {
     __device__ __forceinline__ void finish(const Distill &p, DistillShared<NT> &sh, int64_t r, float cT, T *gr, double &acc) const
     {
         const int tid = threadIdx.x;
-        if (tid >= DistillShared<NT>::K || (tid != 0 && en.id < 0)) return;
+        const bool tells = tid == DISTILL_TELLS(NT);
+        if (!tells && (tid >= DistillShared<NT>::K || (tid != 0 && en.id < 0))) return;
         if (en.id >= 0) sh.table[(en.id >> 5) & 255] = 0;
         float2 ts = make_float2(0.f, 0.f);
 #pragma unroll
@@ -443,12 +532,12 @@ struct DistillRow {
             gr[c] = RowVec<T>::to(o);
         };
         if (en.id >= 0) column(en.id, sh.e[tid], sh.twice != 0, zc);
-        if (tid != 0) return;
-        if (HARD && en.y >= 0) column(en.y, 0.f, y_among, zy);
+        if (HARD && tid == 0 && en.y >= 0) column(en.y, 0.f, y_among, zy);
+        if (!tells) return;
         float loss = 0.f;
         if (!dead) {
-            if (soft_on) loss = (1.f - p.hard) * p.T * p.T * (ts.y * rcp_fast(ts.x) / p.T + (__logf(sum.s) - __logf(ts.x)));
-            if (hard_on) loss += p.hard * (__logf(sum.s1) - (zy - sum.m));
+            if (soft_on) loss = (1.f - p.hard) * p.T * p.T * (ts.y * rcp_fast(ts.x) / p.T + (logf(sum.s) - logf(ts.x)));
+            if (hard_on) loss += p.hard * (logf(sum.s1) - (zy - sum.m));
         }
         if (p.row_loss) p.row_loss[r] = loss;
         if (p.loss_sum) acc += (double)en.w * (double)loss;
@@ -561,7 +650,7 @@ k_distill_wide(Distill p, const T *z, T *g)
         row.finish(p, sh[turn], r, cT, gr, acc);
     }
     if (STAGED && tid == 0 && *(volatile int *)&dead) mbar_settle(&full, 1, issued);
-    if (p.loss_sum) loss_finish_first(acc, p.block_partial, p.ticket, p.loss_sum);
+    if (p.loss_sum) loss_finish_first<DISTILL_TELLS(NT)>(acc, p.block_partial, p.ticket, p.loss_sum);
 }
 
 // Longer rows come through shared memory, in chunks of a piece a thread and a ring of as many slots as two blocks an SM have room for; one warp asks for them
@@ -703,15 +792,15 @@ k_distill_long(Distill p, const T *z, T *g)
     }
     __syncwarp();
     __syncthreads();
-    if (p.loss_sum) loss_finish_first(acc, p.block_partial, p.ticket, p.loss_sum);
+    if (p.loss_sum) loss_finish_first<DISTILL_TELLS(NT)>(acc, p.block_partial, p.ticket, p.loss_sum);
 }
 
-template <typename T, int TPR, int CH, int NE, bool HARD>
+template <typename T, int TPR, int CH, int NE, bool HARD, bool NEAR = false>
 static void distill_rows_go(sat_ctx *ctx, const Distill &p, const T *z, T *g)
 {
     const int resident = CH * RowVec<T>::V > 16 ? 2 : NE > 4 ? 3 : 4;   // blocks of an SM: all of them at work from the beginning to the end
     const unsigned blocks = (unsigned)std::min<int64_t>(cdiv64(p.rows, 256 / TPR), (int64_t)ctx->sms * resident);
-    sat_pdl(ctx->stream, k_distill_rows<T, TPR, CH, NE, HARD>, blocks, 256, (256 / TPR) * distill_stride<TPR, CH, RowVec<T>::V>() * sizeof(float))(p, z, g);
+    sat_pdl(ctx->stream, k_distill_rows<T, TPR, CH, NE, HARD, NEAR>, blocks, 256, (256 / TPR) * distill_stride<TPR, CH, RowVec<T>::V>() * sizeof(float))(p, z, g);
 }
 template <typename T, int NT, int CH, bool HARD, bool STAGED>
 static sat_status distill_wide_go(sat_ctx *ctx, const Distill &p, const T *z, T *g)
@@ -744,6 +833,13 @@ static sat_status distill_launch(sat_ctx *ctx, const Distill &p, const T *z, T *
             set.mark(ctx->device);
         }
         sat_pdl(ctx->stream, k_distill_long<T, HARD>, (unsigned)std::min<int64_t>(p.rows, ctx->sms * 2), DISTILL_LONG_NT + 32, smem)(p, z, g);
+        return SAT_OK;
+    }
+    if (p.T > DISTILL_NEAR_FROM && (p.row_loss || p.loss_sum)) {   // (fewer shapes of this one)
+        if (pieces > 32 * CH) distill_rows_go<T, 32, 2 * CH, 8, HARD, true>(ctx, p, z, g);
+        else if (pieces > 16 * CH || p.k > 64) distill_rows_go<T, 32, CH, 8, HARD, true>(ctx, p, z, g);
+        else if (pieces > 4 * CH || p.k > 16) distill_rows_go<T, 16, CH, 4, HARD, true>(ctx, p, z, g);
+        else distill_rows_go<T, 4, CH, 4, HARD, true>(ctx, p, z, g);
         return SAT_OK;
     }
     // the fewest lanes that hold the row and, with four entries each, the teacher's (two, where that is enough: more warps fit)

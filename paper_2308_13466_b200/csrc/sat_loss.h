@@ -43,11 +43,12 @@ __device__ __forceinline__ void loss_finish(double thread_sum, double *__restric
     }
 }
 
-// The same where the sums are one thread's of each block, thread 0: any number of whole warps, little shared memory.
+// The same where the sums are one thread's of each block, `who`: any number of whole warps, little shared memory.
+template <int who>
 __device__ __forceinline__ void loss_finish_first(double sum, double *__restrict__ block_partial, int *__restrict__ ticket, double *total)
 {
     __shared__ int last;
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == who) {
         block_partial[blockIdx.x] = sum;
         __threadfence();
         last = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
