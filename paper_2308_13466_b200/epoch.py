@@ -7,6 +7,8 @@ steps in between.  It contains no arithmetic of its own.
 """
 from __future__ import annotations
 
+import weakref
+
 import numpy as np
 import torch
 
@@ -29,14 +31,28 @@ class TokenInputs:
 
     def __init__(self, ep: "SatEpoch", tokens: torch.Tensor, vocabulary: int, padding: int = -1, scale: float = 1.0):
         assert ep.dims[0] % 4 == 0, "the width of learned inputs is a multiple of 4"
-        lists = [B.sat_part_lists(ep.ctx, m) for m in range(ep.M)]
-        gids = np.concatenate([p["inner_gid"] for p in lists] + [p["halo_gid"] for p in lists])
+        assert tuple(tokens.shape) == (ep.n,) and tokens.dtype is torch.int32, "a token (int32) per node"
+        self.gids, self.d, self._for = self._rows(ep), ep.dims[0], weakref.WeakSet([ep])
         self.tokens, self.vocabulary, self.padding, self.scale = tokens, vocabulary, padding, scale
-        rows = tokens[torch.from_numpy(gids.astype(np.int64)).to(tokens.device)].contiguous()
+        rows = tokens[torch.from_numpy(self.gids.astype(np.int64)).to(tokens.device)].contiguous()
         self.order = B.new_token_order(rows.numel(), vocabulary, tokens.device)
         B.sat_token_sort(ep.ctx, rows, padding, self.order)
         self.x = _buf(ep.n, ep.dims[0], ep.device)
         self.g = _buf(ep.n + ep.nb, ep.dims[0], ep.device)
+
+    @staticmethod
+    def _rows(ep: "SatEpoch") -> np.ndarray:
+        """The nodes behind the rows of the gradient: inner rows of all partitions, then their halo rows"""
+        lists = [B.sat_part_lists(ep.ctx, m) for m in range(ep.M)]
+        return np.concatenate([p["inner_gid"] for p in lists] + [p["halo_gid"] for p in lists])
+
+    def fits(self, ep: "SatEpoch") -> bool:
+        """Made for the graph, the partitions and the input width of `ep` (looked up once per SatEpoch)"""
+        if ep not in self._for:
+            if self.d != ep.dims[0] or len(self.tokens) != ep.n or len(self.gids) != ep.n + ep.nb or not np.array_equal(self.gids, self._rows(ep)):
+                return False
+            self._for.add(ep)
+        return True
 
 
 class SatEpoch:
@@ -262,6 +278,36 @@ class SatEpoch:
     # ---- learned inputs, normalised layers, a teacher ----------------------------------
     NORM_EPS = 1e-5
 
+    def _token_check(self, inputs: TokenInputs, params, pred, teacher):
+        """What an epoch of step_tokens is refused for, before any of it has run: the library takes pointers, and a push without its commit would leave half an epoch."""
+        L, d = self.L, self.dims
+        assert inputs.fits(self), "learned inputs of another graph, other partitions or another width"
+        shapes = dict(table=[(inputs.vocabulary, d[0])], W=[(d[l], d[l + 1]) for l in range(L)], b=[(x,) for x in d[1:]], gamma=[(x,) for x in d[1:-1]], beta=[(x,) for x in d[1:-1]])
+        for name, want in shapes.items():
+            have = [params[name]] if name == "table" else params[name]
+            assert len(have) >= len(want), f"{name}: a tensor per layer"
+            for t, shape in zip(have, want):
+                assert tuple(t.shape) == shape and t.dtype is torch.float32 and t.device == self.device and (name == "table" or t.is_contiguous()), f"{name}: fp32 {shape} on {self.device}"
+        assert pred is None or len(pred) >= L - 1, "a predictor (or None) per hidden layer"
+        hard = 1.0 if teacher is None else teacher["hard"]
+        if teacher is not None:
+            ids, logits = teacher["ids"], teacher["logits"]
+            assert ids.dim() == 2 and len(ids) == self.n and ids.shape == logits.shape and ids.dtype is torch.int32 and logits.dtype is torch.float32, "teacher: ids int32 and logits fp32 [n, k]"
+            assert all(t.device == self.device and t.is_contiguous() for t in (ids, logits)) and ids.shape[1] <= 256, f"teacher: up to 256 entries a row, on {self.device}"
+            assert 0 <= hard <= 1 and 1e-3 <= teacher["temperature"] <= 1e3, "teacher: 0 <= hard <= 1, 0.001 <= temperature <= 1000"
+        if hard > 0:
+            assert self.labels is not None and (teacher is None or (self.labels.dtype is torch.int32 and tuple(self.labels.shape) == (self.n,))), "labels (set_inputs), beside a teacher int32 [n]"
+
+    def _token_room(self, params):
+        """token_grads in the shapes of the parameters, made anew where those are others than the last time; normalised rows and their statistics"""
+        layout = {k: v.shape if k == "table" else [t.shape for t in v] for k, v in params.items()}
+        if getattr(self, "_token_layout", None) != layout:
+            self.token_grads = {k: torch.zeros_like(v) if k == "table" else [torch.zeros_like(t) for t in v] for k, v in params.items()}
+            self._token_layout = layout
+        if getattr(self, "normed", None) is None:
+            self.normed = [None] + [_buf(self.n, d, self.device) for d in self.dims[1:-1]]
+            self.norm_stats = [None] + [tuple(torch.empty(self.n, dtype=torch.float32, device=self.device) for _ in range(2)) for _ in self.dims[1:-1]]
+
     def step_tokens(self, inputs: TokenInputs, params, pred, lr: float | None = None, teacher=None):
         """One SAT epoch of a network whose nodes have learned inputs and whose hidden rows are normalised, all partitions per launch:
             x_v = scale table[token_v];  per layer  z = P h W + b;  hidden ones  h = norm(ReLU(z)) gamma + beta, which is what is pushed and pulled;
@@ -271,11 +317,8 @@ class SatEpoch:
         with hard > 0 the labels (int32) count as well.  The inputs of halo nodes are exact, so the table's gradient has their part too; the pulled rows of
         the other layers are constants of the epoch."""
         ctx, L, m = self.ctx, self.L, B.SAT_ALL_PARTS
-        dev, f = self.device, torch.float32
-        if not hasattr(self, "token_grads"):
-            self.token_grads = {k: torch.zeros_like(v) if k == "table" else [torch.zeros_like(t) for t in v] for k, v in params.items()}
-            self.normed = [None] + [_buf(self.n, d, dev) for d in self.dims[1:-1]]
-            self.norm_stats = [None] + [tuple(torch.empty(self.n, dtype=f, device=dev) for _ in range(2)) for _ in self.dims[1:-1]]
+        self._token_check(inputs, params, pred, teacher)
+        self._token_room(params)
         gr = self.token_grads
         if self._halo_state is not None:
             self.halo       # an earlier epoch's rows, before this one's push may overwrite them
