@@ -34,11 +34,13 @@ class TokenInputs:
         assert tuple(tokens.shape) == (ep.n,) and tokens.dtype is torch.int32, "a token (int32) per node"
         self.gids, self.d, self._for = self._rows(ep), ep.dims[0], weakref.WeakSet([ep])
         self.tokens, self.vocabulary, self.padding, self.scale = tokens, vocabulary, padding, scale
-        rows = tokens[torch.from_numpy(self.gids.astype(np.int64)).to(tokens.device)].contiguous()
-        self.order = B.new_token_order(rows.numel(), vocabulary, tokens.device)
-        B.sat_token_sort(ep.ctx, rows, padding, self.order)
-        self.x = _buf(ep.n, ep.dims[0], ep.device)
-        self.g = _buf(ep.n + ep.nb, ep.dims[0], ep.device)
+        ep.stream.wait_stream(torch.cuda.current_stream(ep.device))             # (the tokens may just have been made on it)
+        with torch.cuda.stream(ep.stream):                                      # what is made here is the library's, whose stream this is
+            rows = tokens[torch.from_numpy(self.gids.astype(np.int64)).to(tokens.device)].contiguous()
+            self.order = B.new_token_order(rows.numel(), vocabulary, tokens.device)
+            B.sat_token_sort(ep.ctx, rows, padding, self.order)
+            self.x = _buf(ep.n, ep.dims[0], ep.device)
+            self.g = _buf(ep.n + ep.nb, ep.dims[0], ep.device)
 
     @staticmethod
     def _rows(ep: "SatEpoch") -> np.ndarray:
@@ -318,11 +320,12 @@ class SatEpoch:
         the other layers are constants of the epoch."""
         ctx, L, m = self.ctx, self.L, B.SAT_ALL_PARTS
         self._token_check(inputs, params, pred, teacher)
-        self._token_room(params)
+        with torch.cuda.stream(self.stream):
+            self._token_room(params)
+            self.loss_sum.zero_()
         gr = self.token_grads
         if self._halo_state is not None:
             self.halo       # an earlier epoch's rows, before this one's push may overwrite them
-        self.loss_sum.zero_()
         B.sat_embed_fwd(ctx, inputs.tokens, params["table"], inputs.scale, inputs.padding, inputs.x)
         for l in range(1, L + 1):
             act = B.SAT_ACT_RELU if l < L else B.SAT_ACT_NONE

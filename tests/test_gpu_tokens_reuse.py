@@ -79,3 +79,34 @@ def test_inputs_of_another_epoch_object(B):
     finally:
         for ep in (a, b, c):
             ep.close()
+
+
+def test_called_on_another_stream(B):
+    """The library's stream is the one that was current when the SatEpoch was made; what the calls make by themselves goes there, also from another one that is busy."""
+    import torch
+    from paper_2308_13466_b200.epoch import TokenInputs
+    wl, rng = make_workload("tiny"), np.random.default_rng(3)
+    p, ids = _params(rng, wl, 40), rng.integers(0, 40, wl.n).astype(np.int32)
+    tokens, a, b = dev(ids), _epoch(B, wl), _epoch(B, wl)
+    try:
+        one = TokenInputs(a, tokens, 40)
+        for _ in range(2):
+            a.step_tokens(one, p, None)
+        side, busy = torch.cuda.Stream(), torch.zeros((4096, 4096), device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(30):
+                busy = busy @ busy
+            late = dev(ids)[:] + 0                                              # tokens that are there only when `side` has got that far
+            two = TokenInputs(b, late, 40)
+            for _ in range(2):
+                for _ in range(30):
+                    busy = busy @ busy
+                b.step_tokens(two, p, None)
+        torch.cuda.synchronize()
+        for x, y in zip((*one.order._keep, a.loss_sum, *_flat(a.token_grads)), (*two.order._keep, b.loss_sum, *_flat(b.token_grads))):
+            assert torch.equal(x, y)
+        B.sat_sync_status(b.ctx)
+    finally:
+        a.close()
+        b.close()
