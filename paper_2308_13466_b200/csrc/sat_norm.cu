@@ -432,9 +432,13 @@ k_norm_sums(const float *__restrict__ part, int32_t blocks, int32_t d, int32_t l
     float *out = blockIdx.y ? g_beta : g_gamma;
     if (!out) return;
     float s = 0.f;
-    if (col < d)
+    for (int32_t b0 = w; col < d && b0 < blocks; b0 += 32 * 64) {   // (64 at a time: as with a block's rows)
+        const int32_t b1 = b0 + 32 * 64 < blocks ? b0 + 32 * 64 : blocks;
+        float some = 0.f;
 #pragma unroll 8
-        for (int32_t b = w; b < blocks; b += 32) s += __ldcg(part + ((int64_t)b * 2 + blockIdx.y) * ld_part + col);
+        for (int32_t b = b0; b < b1; b += 32) some += __ldcg(part + ((int64_t)b * 2 + blockIdx.y) * ld_part + col);
+        s += some;
+    }
     red[w][c] = s;
     __syncthreads();
     const int lane = threadIdx.x & 31, mine = threadIdx.x >> 5;   // a warp per column
@@ -459,6 +463,13 @@ struct NormArgs {
     float *g_gamma, *g_beta;
     int accumulate;
 };
+// Blocks of a backward pass: `resident` of them, or as many times that as leave a thread no more than NORM_CHAIN rows.  A thread's sums are additions one after the other, in which many small
+// terms would be lost beside a large sum; partial sums of blocks meet in shorter chains.  (Up to 7 million narrow rows nothing changes.)
+#define NORM_CHAIN 512
+static int32_t norm_blocks(int64_t rows, int32_t rows_of_block, int32_t resident)   // rows_of_block: side by side
+{
+    return resident * (int32_t)std::max<int64_t>(1, cdiv64(rows, (int64_t)resident * rows_of_block * NORM_CHAIN));
+}
 // room for a row of partial sums of every block
 template <typename T>
 static sat_status norm_parts(const NormArgs<T> &a, int32_t blocks, int32_t ld_part, float **part)
@@ -497,7 +508,7 @@ static sat_status norm_rows_go(const NormArgs<T> &a, bool back)
         return SAT_OK;
     }
     // every block is a row of partial sums: as many as the SMs hold, and two rows a thread at least
-    const int32_t blocks = (int32_t)std::min<int64_t>(cdiv64(a.rows, 2 * RPB), (int64_t)ctx->sms * (CH * RowVec<T>::V > 8 ? 2 : 3)), ld_part = (a.d + 7) & ~7;
+    const int32_t blocks = (int32_t)std::min<int64_t>(cdiv64(a.rows, 2 * RPB), norm_blocks(a.rows, RPB, ctx->sms * (CH * RowVec<T>::V > 8 ? 2 : 3))), ld_part = (a.d + 7) & ~7;
     float *part;
     SAT_TRY(norm_parts(a, blocks, ld_part, &part));
     sat_pdl(ctx->stream, k_norm_bwd<T, TPR, CH>, (unsigned)blocks, 256, 0)(a.rows, a.d, a.x, a.ld_x, a.g, a.ld_g, a.gamma, (const float *)a.mean, (const float *)a.rstd, a.y, a.ld_y,
@@ -517,7 +528,7 @@ static sat_status norm_ring_go(const NormArgs<T> &a)
     }
     const int32_t pieces = (a.d + RowVec<T>::V - 1) / RowVec<T>::V, stage = (BACK ? 2 : 1) * pieces * 16, params = NORM_KEPT(NT, RowVec<T>::V, BACK) ? (BACK ? 1 : 2) * pieces * RowVec<T>::V * 4 : 0;
     const int32_t slots = std::min(NORM_SLOTS, (room - params) / stage);   // one at least: 16,384 fp32 elements take 192 KB
-    const int32_t blocks = (int32_t)std::min<int64_t>(a.rows, (int64_t)ctx->sms * NORM_RING_BLOCKS(NT)), ld_part = (a.d + 7) & ~7;
+    const int32_t resident = ctx->sms * NORM_RING_BLOCKS(NT), blocks = (int32_t)std::min<int64_t>(a.rows, BACK ? norm_blocks(a.rows, 1, resident) : resident), ld_part = (a.d + 7) & ~7;
     float *part = nullptr;
     if (BACK) SAT_TRY(norm_parts(a, blocks, ld_part, &part));
     const NormRing<T> p = {a.rows, a.d, slots, a.x, a.g, a.ld_x, a.ld_g, a.ld_y, a.gamma, a.beta, a.eps, a.y, a.mean, a.rstd, part, ld_part, norm_last_of(a, blocks, ld_part, part), ctx->d_flag + 1};
