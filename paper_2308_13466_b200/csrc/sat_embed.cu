@@ -1,5 +1,5 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens:
-//     out[i] = scale table[t_i]            g_table[v] (+)= scale sum of g[i] over the i with t_i = v, in ascending order of i
+//     out[i] = scale table[t_i]            g_table[v] (+)= scale sum of g[i] over the i with t_i = v, in a fixed order: ascending i within a run of positions, then the runs
 // The tokens are sorted once (sat_token_sort: keys of 32 bits, by digits, stable), the gradient then walks them in that order.
 #include "sat_rows.h"
 
@@ -472,6 +472,7 @@ extern "C" sat_status sat_token_sort(sat_ctx *ctx, const int32_t *tokens, int32_
 // order.  Further blocks write the rows of tokens that did not occur.  Bound by memory: 65536 x 1024 bf16 into 131072 rows 117 us (4.7 TB/s), 1300000 x 100 fp32 into 612257 rows
 // 179 (4.8 TB/s: rows of 400 bytes at random places, fetched by 64 bytes).  Four rows on their way and four blocks an SM: no faster.
 #define EMB_AHEAD 8
+#define EMB_LEN 256
 struct EmbedBwd {
     const int32_t *tokens, *index;
     int64_t n;
@@ -610,8 +611,15 @@ k_embed_join(EmbedBwd p)
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         if (mine < side) {
             if (mine == 0) s = row(b - 1, 0, col0 + 4 * quad);
+            float4 all = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int64_t r0 = b + mine; r0 < lo; r0 += 64 * side) {   // (64 at a time: shorter chains of additions)
+                const int64_t r1 = r0 + 64 * side < lo ? r0 + 64 * side : lo;
 #pragma unroll 8
-            for (int64_t r = b + mine; r < lo; r += side) add(s, row(r, 1, col0 + 4 * quad));
+                for (int64_t r = r0; r < r1; r += side) add(s, row(r, 1, col0 + 4 * quad));
+                add(all, s);
+                s = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            s = all;
         }
         red[threadIdx.x] = s;
         __syncthreads();
@@ -758,11 +766,12 @@ extern "C" sat_status sat_embed_bwd(sat_ctx *ctx, const sat_token_order *order, 
     p.scale = scale, p.accumulate = accumulate, p.g_table = g_table, p.ld_part = (d + 7) & ~7;
     p.status = ctx->d_flag + 1;
     if (p.n == 0 && accumulate) return SAT_OK;
-    // lanes of a row: as many as it has pieces of 16 bytes; runs: as many as fill the SMs four times with the 24 warps that they hold, of 8 positions at least
+    // lanes of a row: as many as it has pieces of 16 bytes; runs: as many as fill the SMs four times with the 24 warps that they hold, of 8 positions at least and EMB_LEN at most (a run's sum
+    // is additions one after the other)
     const int32_t v = 16 / type_bytes(type), pieces = (d + v - 1) / v;
     const int tpr = pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
     p.slabs = (pieces + tpr - 1) / tpr;
-    p.len = (int32_t)std::max<int64_t>(8, cdiv64(p.n * p.slabs, (int64_t)ctx->sms * 96 * (32 / tpr)));
+    p.len = (int32_t)std::min<int64_t>(EMB_LEN, std::max<int64_t>(8, cdiv64(p.n * p.slabs, (int64_t)ctx->sms * 96 * (32 / tpr))));
     p.zero_rows = (int32_t)std::min<int64_t>(EMB_ZERO, std::max<int64_t>(32, cdiv64(order->vocabulary, ctx->sms * 3)));
     p.runs = cdiv64(p.n, p.len);
     if (p.runs * p.slabs >= INT32_MAX) return sat_fail(ctx, SAT_EINVAL, "sat_embed_bwd: too many rows of this width");
