@@ -5,13 +5,17 @@ import numpy as np
 import pytest
 import torch
 
-import paper_2308_13466_b200.binding as B
-from paper_2308_13466_b200.epoch import SatEpoch, TokenInputs
-
 DIMS, N, HALO, WORDS = [8, 6, 5, 3], 12, 4, 20
 
 
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    import __graft_entry__
+    __graft_entry__.build()
+
+
 def _epoch(n=N, nb=HALO, dims=DIMS):
+    from paper_2308_13466_b200.epoch import SatEpoch
     ep = SatEpoch.__new__(SatEpoch)
     ep.ctx, ep.device, ep.n, ep.nb, ep.M, ep.dims, ep.L = None, torch.device("cpu"), n, nb, 1, list(dims), len(dims) - 1
     ep.labels, ep.loss = torch.zeros(n, dtype=torch.int32), "ce"
@@ -19,6 +23,7 @@ def _epoch(n=N, nb=HALO, dims=DIMS):
 
 
 def _inputs(ep, gids=None):
+    from paper_2308_13466_b200.epoch import TokenInputs
     it = TokenInputs.__new__(TokenInputs)
     it.gids = np.arange(ep.n + ep.nb, dtype=np.int32) % ep.n if gids is None else gids
     it.tokens, it.vocabulary, it.padding, it.scale, it.d, it._for = torch.zeros(ep.n, dtype=torch.int32), WORDS, -1, 1.0, ep.dims[0], weakref.WeakSet()
@@ -41,6 +46,7 @@ class Ran(Exception):
 @pytest.fixture
 def library(monkeypatch):
     """Calls of the library raise Ran; the lists of a partition are those of _inputs."""
+    import paper_2308_13466_b200.binding as B
     for name in B.EXPORTS:
         def call(*a, **kw):
             raise Ran(name)
