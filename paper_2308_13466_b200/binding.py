@@ -12,7 +12,6 @@ import ctypes as C
 import os
 
 import numpy as np
-import torch
 
 from .build import lib_path
 
@@ -552,11 +551,19 @@ _lib.sat_embed_fwd.argtypes = [_P, _L, _P, _I, _I, _I, C.c_int, _P, _I, _F, _P, 
 _lib.sat_token_sort.argtypes = [_P, _P, _I, _P]
 _lib.sat_embed_bwd.argtypes = [_P, _P, _I, C.c_int, _P, _I, _F, _P, _I, C.c_int]
 _lib.sat_distill_grad.argtypes = [_P, _L, _I, C.c_int, _P, _I, _I, _P, _P, _F, _F, _P, _P, _F, _P, _P, _P, _I]
-_ROW_TYPES = {torch.float32: SAT_F32, torch.bfloat16: SAT_BF16, torch.float16: SAT_F16}
+torch, _ROW_TYPES = None, {}   # once a tensor has come: host arrays alone need no torch
+
+
+def _need_torch():
+    global torch
+    import torch
+    _ROW_TYPES.update({torch.float32: SAT_F32, torch.bfloat16: SAT_BF16, torch.float16: SAT_F16})
 
 
 def _first(t):
-    """Of a CUDA matrix with contiguous rows of fp32, bf16 or fp16: device, type, and what the others of a call are held to."""
+    """Of a CUDA matrix with contiguous rows of fp32, bf16 or fp16: device and type, which the others of a call are held to."""
+    if torch is None:
+        _need_torch()
     dtype = t.dtype
     dev = t.get_device()
     assert dev >= 0 and dtype in _ROW_TYPES, "rows are CUDA tensors of fp32, bf16 or fp16"
@@ -610,6 +617,7 @@ def sat_embed_fwd(ctx, tokens, table, scale: float, padding: int, out):
 
 def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
     """Room for the order of n tokens on `device` (default: the current CUDA device)."""
+    _need_torch()
     assert n >= 0 and vocabulary > 0
     device = torch.device("cuda") if device is None else device
     tokens, index = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(2))
