@@ -551,6 +551,7 @@ _lib.sat_embed_fwd.argtypes = [_P, _L, _P, _I, _I, _I, C.c_int, _P, _I, _F, _P, 
 _lib.sat_token_sort.argtypes = [_P, _P, _I, _P]
 _lib.sat_embed_bwd.argtypes = [_P, _P, _I, C.c_int, _P, _I, _F, _P, _I, C.c_int]
 _lib.sat_distill_grad.argtypes = [_P, _L, _I, C.c_int, _P, _I, _I, _P, _P, _F, _F, _P, _P, _F, _P, _P, _P, _I]
+_MOST = 2 ** 31 - 1
 torch, _ROW_TYPES = None, {}   # once a tensor has come: host arrays alone need no torch
 
 
@@ -573,8 +574,9 @@ def _first(t):
 def _typed(t, dev, dtype):
     """Pointer and row stride of such a matrix, of this type and on this device."""
     (r, c), (s0, s1) = t.shape, t.stride()
-    assert t.dtype is dtype and t.get_device() == dev and (s1 == 1 or c <= 1)
-    return t.data_ptr(), s0 if r > 1 else max(s0, c)
+    ld = s0 if r > 1 else max(s0, c)
+    assert t.dtype is dtype and t.get_device() == dev and (s1 == 1 or c <= 1) and c <= _MOST and ld <= _MOST   # (ctypes would cut them to 32 bits)
+    return t.data_ptr(), ld
 
 
 def _vec(t, dev, dtype, count: int):
@@ -609,7 +611,7 @@ def sat_layernorm_bwd(ctx, x, g, gamma, mean, rstd, g_x=None, g_gamma=None, g_be
 def sat_embed_fwd(ctx, tokens, table, scale: float, padding: int, out):
     """out[i] = scale table[tokens[i]] (tokens: CUDA int32 [n]); a row of zeros where tokens[i] is `padding` (-1: no token pads)."""
     (n, d), (dev, dtype) = out.shape, _first(out)
-    assert table.shape[1] == d
+    assert table.shape[1] == d and table.shape[0] <= _MOST and -_MOST <= padding <= _MOST
     st = _lib.sat_embed_fwd(ctx, n, _vec(tokens, dev, torch.int32, n), table.shape[0], padding, d, _ROW_TYPES[dtype], *_typed(table, dev, dtype), scale, *_typed(out, dev, dtype))
     if st:
         _check(ctx, st)
@@ -618,7 +620,7 @@ def sat_embed_fwd(ctx, tokens, table, scale: float, padding: int, out):
 def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
     """Room for the order of n tokens on `device` (default: the current CUDA device)."""
     _need_torch()
-    assert n >= 0 and vocabulary > 0
+    assert n >= 0 and 0 < vocabulary <= _MOST
     device = torch.device("cuda") if device is None else device
     tokens, index = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(2))
     order = sat_token_order(tokens.data_ptr(), index.data_ptr(), n, vocabulary)
@@ -628,6 +630,7 @@ def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
 
 def sat_token_sort(ctx, tokens, padding: int, order: sat_token_order):
     """order <- the positions of tokens (CUDA int32 [n]) by token"""
+    assert -_MOST <= padding <= _MOST
     st = _lib.sat_token_sort(ctx, _vec(tokens, order._keep[0].get_device(), torch.int32, order.n), padding, C.byref(order))
     if st:
         _check(ctx, st)
@@ -647,7 +650,7 @@ def sat_distill_grad(ctx, z, top_ids, top_logits, temperature: float, hard: floa
     None); loss_sum (CUDA float64 scalar) += the weighted sum, row_loss [rows] the rows' losses, g the gradient (may be z)."""
     (rows, classes), (dev, dtype), f, i = z.shape, _first(z), torch.float32, torch.int32
     k = 0 if top_ids is None else top_ids.shape[1]
-    assert g is None or g.shape == z.shape
+    assert (g is None or g.shape == z.shape) and k <= _MOST
     st = _lib.sat_distill_grad(ctx, rows, classes, _ROW_TYPES[dtype], *_typed(z, dev, dtype), k, _vec(top_ids, dev, i, rows * k), _vec(top_logits, dev, f, rows * k), temperature, hard,
                                _vec(labels, dev, i, rows), _vec(row_weight, dev, f, rows), weight, _vec(loss_sum, dev, torch.float64, 1), _vec(row_loss, dev, f, rows),
                                *((None, 0) if g is None else _typed(g, dev, dtype)))
