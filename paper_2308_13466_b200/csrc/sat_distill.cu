@@ -835,7 +835,7 @@ static sat_status distill_launch(sat_ctx *ctx, const Distill &p, const T *z, T *
         sat_pdl(ctx->stream, k_distill_long<T, HARD>, (unsigned)std::min<int64_t>(p.rows, ctx->sms * 2), DISTILL_LONG_NT + 32, smem)(p, z, g);
         return SAT_OK;
     }
-    if (p.T > DISTILL_NEAR_FROM && (p.row_loss || p.loss_sum)) {   // (fewer shapes of this one)
+    if (p.T > DISTILL_NEAR_FROM) {   // (fewer shapes of this one; the same with and without losses, so that a gradient is the same bits)
         if (pieces > 32 * CH) distill_rows_go<T, 32, 2 * CH, 8, HARD, true>(ctx, p, z, g);
         else if (pieces > 16 * CH || p.k > 64) distill_rows_go<T, 32, CH, 8, HARD, true>(ctx, p, z, g);
         else if (pieces > 4 * CH || p.k > 16) distill_rows_go<T, 16, CH, 4, HARD, true>(ctx, p, z, g);

@@ -147,3 +147,17 @@ def test_rows_that_are_no_numbers(B, ctx):
     for r in np.flatnonzero(~bad & (np.arange(40) != 25)):
         kl, tol = _near(host(zt)[r], ids[r], logits[r].astype(np.float32).astype(np.float64), 20.0)
         assert abs(host(losses)[r] - 400 * kl) <= 400 * tol + 4 * U * 400 * kl
+
+
+@pytest.mark.parametrize("classes,k", [(7, 5), (47, 8), (47, 30), (200, 40), (900, 200), (1500, 30)])
+@pytest.mark.parametrize("T", [4.0, 5.0])
+def test_the_gradient_does_not_depend_on_what_else_is_asked_for(B, ctx, classes, k, T):
+    import torch
+    rng = np.random.default_rng(classes)
+    z, ids, logits, labels = _students(rng, 50, classes, k, "similar")
+    zt, (g, alone) = matrix(z, "f32")[0], (room(50, classes, "f32")[0] for _ in range(2))
+    args = (_dev(ids, np.int32), _dev(logits), T, 0.5, _dev(labels, np.int32), None, 0.02)
+    B.sat_distill_grad(ctx, zt, *args, torch.zeros(1, dtype=torch.float64, device="cuda"), g, torch.empty(50, device="cuda"))
+    B.sat_distill_grad(ctx, zt, *args, None, alone)
+    B.sat_sync_status(ctx)
+    assert torch.equal(g, alone)
