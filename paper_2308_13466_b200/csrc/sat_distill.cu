@@ -653,10 +653,9 @@ k_distill_wide(Distill p, const T *z, T *g)
     if (p.loss_sum) loss_finish_first<DISTILL_TELLS(NT)>(acc, p.block_partial, p.ticket, p.loss_sum);
 }
 
-// Longer rows come through shared memory, in chunks of a piece a thread and a ring of as many slots as two blocks an SM have room for; one warp asks for them
-// (cp.async.bulk).  A row that the ring holds is read once: its chunks stay until the gradient has been worked out of them, and those of the next row follow
-// into the slots that become free.  One that it does not hold comes twice, the second time from the L2 for the most part.
-// 2048 x 131072 fp32: 536 us (4.0 TB/s).
+// Longer rows, which no ring holds, come through shared memory in chunks of a piece a thread, with as many slots as two blocks an SM have room for; one warp asks for them
+// (cp.async.bulk).  Where a gradient is asked for they come twice, the second time from the L2 for the most part.
+// 2048 x 131072 fp32: 530 us (4.1 TB/s).
 #define DISTILL_LONG_NT 512
 #define DISTILL_SLOTS 13
 template <typename T, bool HARD>
@@ -678,13 +677,12 @@ k_distill_long(Distill p, const T *z, T *g)
     __syncthreads();
     sat_grid_wait();
     const int32_t pieces = (p.C + V - 1) / V, chunks = (pieces + CHUNK - 1) / CHUNK;
-    const bool once = chunks <= DISTILL_SLOTS || !g;
     double acc = 0.0;
     if (tid >= NT) {
         if (lane == 0) {
             uint32_t slot = 0, turn = 0, issued = 0;
             for (int64_t r = blockIdx.x; r < p.rows && !*(volatile int *)&dead; r += gridDim.x)
-                for (int32_t i = 0; i < (once ? chunks : 2 * chunks); ++i) {
+                for (int32_t i = 0; i < (g ? 2 * chunks : chunks); ++i) {
                     const int32_t c = i < chunks ? i : i - chunks, here = pieces - c * CHUNK < CHUNK ? pieces - c * CHUNK : CHUNK;
                     if (turn > 0 && !mbar_wait<64>(empty + slot, (turn - 1) & 1u, &dead, p.status)) break;
                     mbar_expect_tx(full + slot, (uint32_t)here * 16);
@@ -713,7 +711,6 @@ k_distill_long(Distill p, const T *z, T *g)
             distill_known(p, row.en);
             row.zc = row.en.id >= 0 ? RowVec<T>::from(zr[row.en.id]) : 0.f;
             row.zy = row.en.y >= 0 ? RowVec<T>::from(zr[row.en.y]) : 0.f;
-            const uint32_t slot0 = slot;
             // sums relative to the largest logit so far
             float m = -INFINITY;
             DistillScale cs = distill_scale(m, p.T, cT), hs = distill_scale(m, 1.f, LOG2E);
@@ -732,7 +729,7 @@ k_distill_long(Distill p, const T *z, T *g)
                     (void)mbar_wait(full + slot, phase, &dead, p.status);   // (having given up, all finish on what is there)
                     if (piece < pieces) raw[u] = ring[slot * CHUNK + tid];
                     if (piece == pieces - 1 && p.C % V) raw[u] = RowVec<T>::cut(raw[u], p.C % V);
-                    if (!once || !g) release(slot);
+                    release(slot);
                     step(slot, phase);
                 }
                 top = fmaxf(top, fmaxf(RowVec<T>::largest(raw[0]), RowVec<T>::largest(raw[1])));
@@ -757,7 +754,6 @@ k_distill_long(Distill p, const T *z, T *g)
             if (g) {
                 const DistillScale gs(row.sum.m, cT), gh(row.sum.m, LOG2E);
                 const float af = row.aq * ex2_fast(gs.left), bf = HARD ? row.bq * ex2_fast(gh.left) : 0.f;
-                uint32_t at = once ? slot0 : slot;
                 const bool other = row.dead || row.exact;   // (its chunks are taken off all the same)
                 if (other) row.other_rows(p, zr, gr, cT);
                 for (int32_t c = 0; c < chunks; c += 2) {
@@ -766,14 +762,10 @@ k_distill_long(Distill p, const T *z, T *g)
                     for (int u = 0; u < 2; ++u) {
                         raw[u] = make_uint4(0u, 0u, 0u, 0u);
                         if (c + u >= chunks) break;
-                        if (!once) (void)mbar_wait(full + at, phase, &dead, p.status);
-                        if ((c + u) * CHUNK + tid < pieces) raw[u] = ring[at * CHUNK + tid];
-                        release(at);
-                        if (once) {
-                            if (++at == DISTILL_SLOTS) at = 0;
-                        } else {
-                            step(at, phase);
-                        }
+                        (void)mbar_wait(full + slot, phase, &dead, p.status);
+                        if ((c + u) * CHUNK + tid < pieces) raw[u] = ring[slot * CHUNK + tid];
+                        release(slot);
+                        step(slot, phase);
                     }
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
@@ -784,7 +776,6 @@ k_distill_long(Distill p, const T *z, T *g)
                         row_store(gr, piece * V, p.C, o);
                     }
                 }
-                if (!once) slot = at;
             }
             distill_sync<NT>();
             row.finish(p, sh[which], r, cT, gr, acc);
@@ -820,7 +811,7 @@ static sat_status distill_launch(sat_ctx *ctx, const Distill &p, const T *z, T *
     constexpr int V = RowVec<T>::V, CH = 16 / V;   // 16 elements a lane
     const int32_t pieces = (p.C + V - 1) / V;
     if (pieces > 32 * 2 * CH) {
-        // a block whose registers hold the row in four pieces a thread, or in eight, staged; or the ring
+        // a block whose registers hold the row in four pieces a thread, or in eight, staged; or the ring, which holds less than the last of these
         if (pieces <= 128 * 4 && p.k <= 128) return distill_wide_go<T, 128, 4, HARD, false>(ctx, p, z, g);
         if (pieces <= 256 * 4) return distill_wide_go<T, 256, 4, HARD, false>(ctx, p, z, g);
         if (pieces <= 512 * 4) return distill_wide_go<T, 512, 4, HARD, false>(ctx, p, z, g);
