@@ -26,6 +26,8 @@ __device__ __forceinline__ void norm_centre(uint64_t (&v)[V / 2], float m0, int3
         b = f2_fma(v[i], v[i], b);
     }
 }
+// (what rounding leaves of a constant row may be below zero; a row that is no number keeps that)
+__device__ __forceinline__ float norm_variance(float v) { return v < 0.f ? 0.f : v; }
 // ... -> y = (x - m0 - m1) s gamma + beta
 template <typename T>
 __device__ __forceinline__ void norm_finish(T *y, int32_t col, int32_t d, const uint64_t (&v)[RowVec<T>::V / 2], float m1, float sd, const uint64_t (&gamma)[RowVec<T>::V / 2],
@@ -111,7 +113,7 @@ k_norm_fwd(int64_t rows, int32_t d, const T *x, int64_t ld_x, const float *__res
 #pragma unroll
         for (int j = 0; j < CH; ++j) norm_centre<V>(v[j], m0, (j * TPR + t) * V, d, a, b);
         const float2 ab = row_sum2<TPR>(f2_sum(a), f2_sum(b), none, turn);
-        const float m1 = ab.x * inv_d, var = fmaxf(ab.y * inv_d - m1 * m1, 0.f), sd = 1.f / sqrtf(var + eps);
+        const float m1 = ab.x * inv_d, var = norm_variance(ab.y * inv_d - m1 * m1), sd = 1.f / sqrtf(var + eps);
         if (r >= rows) continue;
         if (t == 0) {
             if (mean) mean[r] = m0 + m1;
@@ -387,7 +389,7 @@ k_norm_ring(NormRing<T> p)
 #pragma unroll
             for (int j = 0; j < CH; ++j) norm_centre<V>(v[j], m0, (j * NT + tid) * V, p.d, a, b);
             const float2 t = row_sum2<NT>(f2_sum(a), f2_sum(b), red, turn);
-            const float m1 = t.x * inv_d, var = fmaxf(t.y * inv_d - m1 * m1, 0.f), sd = 1.f / sqrtf(var + p.eps);
+            const float m1 = t.x * inv_d, var = norm_variance(t.y * inv_d - m1 * m1), sd = 1.f / sqrtf(var + p.eps);
             if (tid == 0) {
                 if (p.mean) p.mean[r] = m0 + m1;
                 if (p.rstd) p.rstd[r] = sd;
