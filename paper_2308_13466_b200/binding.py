@@ -127,6 +127,7 @@ def sat_create(device: int = 0, stream: int = 0):
     st = _lib.sat_create(C.byref(ctx), C.c_int(device), C.c_void_p(stream))
     if st != SAT_OK:
         raise SatError(st, "sat_create failed")
+    ctx.device = device
     return ctx
 
 
@@ -561,13 +562,14 @@ def _need_torch():
     _ROW_TYPES.update({torch.float32: SAT_F32, torch.bfloat16: SAT_BF16, torch.float16: SAT_F16})
 
 
-def _first(t):
-    """Of a CUDA matrix with contiguous rows of fp32, bf16 or fp16: device and type, which the others of a call are held to."""
+def _first(ctx, t):
+    """Of a CUDA matrix with contiguous rows of fp32, bf16 or fp16: device and type, which the others of a call are held to.  The device is the context's."""
     if torch is None:
         _need_torch()
     dtype = t.dtype
     dev = t.get_device()
     assert dev >= 0 and dtype in _ROW_TYPES, "rows are CUDA tensors of fp32, bf16 or fp16"
+    assert dev == getattr(ctx, "device", dev), "tensors on another device than the context's"
     return dev, dtype
 
 
@@ -589,7 +591,7 @@ def _vec(t, dev, dtype, count: int):
 
 def sat_layernorm_fwd(ctx, x, gamma, beta, eps: float, y, mean=None, rstd=None):
     """y = (x - mean(x)) / sqrt(var(x) + eps) gamma + beta by rows; mean and rstd [rows] receive what the backward call takes.  y may be x."""
-    (rows, d), (dev, dtype), f = x.shape, _first(x), torch.float32
+    (rows, d), (dev, dtype), f = x.shape, _first(ctx, x), torch.float32
     assert y.shape == x.shape
     st = _lib.sat_layernorm_fwd(ctx, rows, d, _ROW_TYPES[dtype], *_typed(x, dev, dtype), _vec(gamma, dev, f, d), _vec(beta, dev, f, d), eps, *_typed(y, dev, dtype),
                                 _vec(mean, dev, f, rows), _vec(rstd, dev, f, rows))
@@ -599,7 +601,7 @@ def sat_layernorm_fwd(ctx, x, gamma, beta, eps: float, y, mean=None, rstd=None):
 
 def sat_layernorm_bwd(ctx, x, g, gamma, mean, rstd, g_x=None, g_gamma=None, g_beta=None, accumulate: bool = False):
     """Gradients of sat_layernorm_fwd from that of y: g_x (may be g or x), and g_gamma, g_beta, overwritten or added to."""
-    (rows, d), (dev, dtype), f = x.shape, _first(x), torch.float32
+    (rows, d), (dev, dtype), f = x.shape, _first(ctx, x), torch.float32
     assert g.shape == x.shape and (g_x is None or g_x.shape == x.shape)
     st = _lib.sat_layernorm_bwd(ctx, rows, d, _ROW_TYPES[dtype], *_typed(x, dev, dtype), *_typed(g, dev, dtype), _vec(gamma, dev, f, d), _vec(mean, dev, f, rows),
                                 _vec(rstd, dev, f, rows), *((None, 0) if g_x is None else _typed(g_x, dev, dtype)), _vec(g_gamma, dev, f, d), _vec(g_beta, dev, f, d),
@@ -610,7 +612,7 @@ def sat_layernorm_bwd(ctx, x, g, gamma, mean, rstd, g_x=None, g_gamma=None, g_be
 
 def sat_embed_fwd(ctx, tokens, table, scale: float, padding: int, out):
     """out[i] = scale table[tokens[i]] (tokens: CUDA int32 [n]); a row of zeros where tokens[i] is `padding` (-1: no token pads)."""
-    (n, d), (dev, dtype) = out.shape, _first(out)
+    (n, d), (dev, dtype) = out.shape, _first(ctx, out)
     assert table.shape[1] == d and table.shape[0] <= _MOST and -_MOST <= padding <= _MOST
     st = _lib.sat_embed_fwd(ctx, n, _vec(tokens, dev, torch.int32, n), table.shape[0], padding, d, _ROW_TYPES[dtype], *_typed(table, dev, dtype), scale, *_typed(out, dev, dtype))
     if st:
@@ -631,14 +633,16 @@ def new_token_order(n: int, vocabulary: int, device=None) -> sat_token_order:
 def sat_token_sort(ctx, tokens, padding: int, order: sat_token_order):
     """order <- the positions of tokens (CUDA int32 [n]) by token"""
     assert -_MOST <= padding <= _MOST
-    st = _lib.sat_token_sort(ctx, _vec(tokens, order._keep[0].get_device(), torch.int32, order.n), padding, C.byref(order))
+    dev = order._keep[0].get_device()
+    assert dev == getattr(ctx, "device", dev), "tensors on another device than the context's"
+    st = _lib.sat_token_sort(ctx, _vec(tokens, dev, torch.int32, order.n), padding, C.byref(order))
     if st:
         _check(ctx, st)
 
 
 def sat_embed_bwd(ctx, order: sat_token_order, g, scale: float, g_table, accumulate: bool = False):
     """g_table (CUDA fp32 [vocabulary, d]) (+)= scale times the sum of the rows of g by token"""
-    (n, d), (dev, dtype) = g.shape, _first(g)
+    (n, d), (dev, dtype) = g.shape, _first(ctx, g)
     assert n == order.n and g_table.shape == (order.vocabulary, d) and order._keep[0].get_device() == dev
     st = _lib.sat_embed_bwd(ctx, C.byref(order), d, _ROW_TYPES[dtype], *_typed(g, dev, dtype), scale, *_typed(g_table, dev, torch.float32), 1 if accumulate else 0)
     if st:
@@ -648,7 +652,7 @@ def sat_embed_bwd(ctx, order: sat_token_order, g, scale: float, g_table, accumul
 def sat_distill_grad(ctx, z, top_ids, top_logits, temperature: float, hard: float, labels, row_weight, weight: float, loss_sum=None, g=None, row_loss=None):
     """Loss between the logits z and a teacher's top logits (CUDA int32 and fp32 [rows, k]) and, with weight `hard`, the labels (CUDA int32 [rows] or
     None); loss_sum (CUDA float64 scalar) += the weighted sum, row_loss [rows] the rows' losses, g the gradient (may be z)."""
-    (rows, classes), (dev, dtype), f, i = z.shape, _first(z), torch.float32, torch.int32
+    (rows, classes), (dev, dtype), f, i = z.shape, _first(ctx, z), torch.float32, torch.int32
     k = 0 if top_ids is None else top_ids.shape[1]
     assert (g is None or g.shape == z.shape) and k <= _MOST
     st = _lib.sat_distill_grad(ctx, rows, classes, _ROW_TYPES[dtype], *_typed(z, dev, dtype), k, _vec(top_ids, dev, i, rows * k), _vec(top_logits, dev, f, rows * k), temperature, hard,

@@ -48,22 +48,54 @@ class Rows:
         return True
 
 
-def test_numbers_beyond_32_bits(B, monkeypatch):
-    import torch
-    calls = []
+@pytest.fixture
+def calls(B, monkeypatch):
+    """The row operators' entry points take note of a call and do nothing."""
+    seen = []
     for name in ("sat_layernorm_fwd", "sat_layernorm_bwd", "sat_embed_fwd", "sat_token_sort", "sat_embed_bwd", "sat_distill_grad"):
         class Fake:
             def __call__(self, *a, name=name):
-                calls.append(name)
+                seen.append(name)
                 return 0
         monkeypatch.setattr(B._lib, name, Fake(), raising=False)
+    return seen
+
+
+def _calls(B, ctx):
+    import torch
+    ints = lambda *s: Rows(s, dtype=torch.int32)
+    B.new_token_order(0, 1, "cpu")
+    order = B.sat_token_order(1 << 20, 1 << 20, 4, 9)
+    order._keep = (ints(4), ints(4))
+    return [lambda: B.sat_layernorm_fwd(ctx, Rows((4, 8)), None, None, 1e-5, Rows((4, 8))), lambda: B.sat_layernorm_bwd(ctx, Rows((4, 8)), Rows((4, 8)), None, Rows((4,)), Rows((4,)), Rows((4, 8))),
+            lambda: B.sat_embed_fwd(ctx, ints(4), Rows((9, 8)), 1.0, -1, Rows((4, 8))), lambda: B.sat_token_sort(ctx, ints(4), 2 ** 31 - 1, order),
+            lambda: B.sat_embed_bwd(ctx, order, Rows((4, 8)), 1.0, Rows((9, 8))),
+            lambda: B.sat_distill_grad(ctx, Rows((4, 8)), ints(4, 2), Rows((4, 2)), 1.0, 0.0, None, None, 1.0, None, Rows((4, 8)))]
+
+
+def test_tensors_of_another_device(B, calls):
+    """The context's device is the one that kernels run on: memory of another is not theirs."""
+    import ctypes
+    ctx = ctypes.c_void_p(1 << 20)
+    ctx.device = 0
+    here = _calls(B, ctx)
+    for call in here:
+        call()
+    assert len(calls) == len(here)
+    ctx.device = 1
+    for call in here:
+        with pytest.raises(AssertionError):
+            call()
+    assert len(calls) == len(here)
+
+
+def test_numbers_beyond_32_bits(B, calls):
+    import torch
     i32, big = torch.int32, 2 ** 32
     ints = lambda *s: Rows(s, dtype=i32)
     order = B.sat_token_order(1 << 20, 1 << 20, 4, 9)
     order._keep = (ints(4), ints(4))
-    ok = [lambda: B.sat_layernorm_fwd(None, Rows((4, 8)), None, None, 1e-5, Rows((4, 8))), lambda: B.sat_embed_fwd(None, ints(4), Rows((9, 8)), 1.0, -1, Rows((4, 8))),
-          lambda: B.sat_token_sort(None, ints(4), 2 ** 31 - 1, order), lambda: B.sat_embed_bwd(None, order, Rows((4, 8)), 1.0, Rows((9, 8))),
-          lambda: B.sat_distill_grad(None, Rows((4, 8)), ints(4, 2), Rows((4, 2)), 1.0, 0.0, None, None, 1.0, None, Rows((4, 8)))]
+    ok = _calls(B, None)
     for call in ok:
         call()
     assert len(calls) == len(ok)
