@@ -583,7 +583,7 @@ enum { SAT_F32 = 0, SAT_BF16 = 1, SAT_F16 = 2 };
  *     mu = mean(x), s = (mean((x - mu)^2) + eps)^(-1/2), xh = (x - mu) s, y = xh gamma + beta
  *   gamma, beta  DEVICE [d], 16-byte aligned; NULL: ones, zeros
  *   mean, rstd   DEVICE [rows], written with mu and s for the backward call; either may be NULL
- * y may be x.  A row with an infinity or a NaN becomes NaN, no other row does.  Magnitudes up to 2^60 / d are taken without overflow of the squares.
+ * y may be x.  A row with an infinity or a NaN becomes NaN, and so do its mean and rstd; no other row does.  Magnitudes up to 2^60 / d are taken without overflow of the squares.
  *
  * Backward, from the same x and gamma, what the forward call left in mean and rstd, and g = gradient with respect to y:
  *     u = g gamma, g_x = s (u - mean(u) - xh mean(u xh)), g_gamma (+)= sum over the rows of g xh, g_beta (+)= sum over the rows of g

@@ -32,8 +32,9 @@ struct Distill {
 // larger by far, and T^2 brings what their rounding left back to size.  With u = d - sum p d the same is
 //     KL = log(1 + sum p (e^-u - 1 + u) + e^(sum p d) rest / st),     rest: the exponentials of the classes that the teacher does not name,
 // where nothing is negative and nothing cancels; e^-u - 1 + u has its series where u is small, and `rest` is added up by itself.  (A class that is named twice would be
-// in the sum twice: such rows keep what they have.)  Worked out behind the gradient, where little else is in registers, and called: 612257 x 47 with labels 76 us, inlined 82, worked out ahead of
-// the gradient 81 (called 96).  Without it 71, so temperatures of up to DISTILL_NEAR_FROM do: the other form's error, about 2^-21 in KL, is 2^-17 in the loss there.
+// in the sum twice: such rows keep what they have.)  Worked out behind the gradient, where little else is in registers, and called (612257 x 47 with labels, four lanes a row and two entries a
+// lane: 76 us, inlined 82, ahead of the gradient 81, called there 96, not at all 70.5).  With the fewer shapes that there are of it 84 us, and 244 for 111 of 1000000 x 16 whose rows all take it; so temperatures of up
+// to DISTILL_NEAR_FROM do without: the other form's error, about 2^-21 in KL, is 2^-17 in the loss there.
 // sp has z - max z on entry and is left all zeros, as it is between rows.  `near` is the same for the lanes of a row; all lanes of the warp call.
 #define DISTILL_NEAR_FROM 4.f
 #define DISTILL_NEAR 0.125f   // of KL; beside more than that 2^-21 is small
@@ -545,7 +546,7 @@ struct DistillRow {
 };
 
 // Rows of up to CH pieces of 16 bytes a thread: they stay in registers as they lie in memory.  Where few blocks share an SM (STAGED) the next row comes into
-// shared memory meanwhile (cp.async.bulk).  The sums, their join and the gradient take turns: 8192 x 50001 bf16 379 us (4.3 TB/s; not staged 389), of which the exponentials are
+// shared memory meanwhile (cp.async.bulk).  The sums, their join and the gradient take turns: 8192 x 50001 bf16 374 us (4.4 TB/s; not staged 389), of which the exponentials are
 // 182; 16384 x 4000 bf16 62 us (4.3 TB/s), 32768 x 2000 fp32 100 (5.3).
 template <typename T, int NT, int CH, bool HARD, bool STAGED>
 __global__ void __launch_bounds__(NT, 1024 / NT)

@@ -73,8 +73,9 @@ __device__ __forceinline__ void norm_back_finish(T *gx, int32_t col, int32_t d, 
 }
 
 // =====================================================================================
-// rows of up to 512 elements: TPR lanes hold one in registers, CH times 16 bytes each.  Bound by memory: 612257 x 256 fp32 forward 201 us (97 % of the copy rate; without the
-// next row on its way 245), backward 287 (the copy rate).
+// rows of up to 512 elements: TPR lanes hold one in registers, CH times 16 bytes each.  Bound by memory: 612257 x 256 fp32 forward 198 to 214 us (91 to 98 % of the copy rate, from one GPU to
+// another; without the next row on its way 245), backward 287 to 295 (the copy rate).  Rows of 9 to 16 pieces of 16 bytes leave half of the lanes' room empty (610000 x 50 fp32: 40 and 43 % of the copy rate), rows of 16 bits
+// lie on twice the lanes that they need with 16 elements each (400000 x 256 bf16: 60 and 67 %).
 // =====================================================================================
 
 // (the next row is asked for before this one is worked on)
@@ -254,7 +255,8 @@ k_norm_bwd(int64_t rows, int32_t d, const T *x, int64_t ld_x, const T *g, int64_
 // =====================================================================================
 // wider rows: a block holds one in registers, CH times 16 bytes a thread; the next ones are on their way into a ring in shared memory (cp.async.bulk), so that what an SM
 // has asked for does not depend on its registers.  A slot is asked for again behind the barrier of the row's sums, when all threads have taken their part of it.
-// Bound by instructions: 16384 x 4096 bf16 backward 85 us (73 % of the copy rate), forward 79; with 8 elements a thread and rows asked for into registers 108.
+// 16384 x 4096 bf16 backward 85 us (73 % of the copy rate; with 8 elements a thread and rows asked for into registers 108): instructions, and a barrier a row; forward 79 (53 %): two barriers a row, and two blocks an SM to
+// fill their waits.
 // =====================================================================================
 #define NORM_SLOTS 8
 // gamma and beta in shared memory, or else from the L1, which has the rest of the SM.  Measured, kept against not: gradients of 50000 x 2048 bf16 125 / 225 us, of 16384 x

@@ -93,3 +93,19 @@ def test_threads_without_columns(B, ctx, classes, k, t):
     for T in TEMPERATURES:
         for hard in (0.0, 0.4):
             _check(B, ctx, z, ids, logits, T, hard, labels if hard else None, t)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [0.001, 0.02, 300.0, 1000.0])
+@pytest.mark.parametrize("classes,k", [(60, 20), (1100, 200), (5003, 64), (20000, 64), (70000, 30)])
+def test_the_ends_of_the_temperatures(B, ctx, classes, k, T, t):
+    rng = np.random.default_rng(classes)
+    z, logits, labels = 2 * rng.normal(size=(8, classes)), 3 * rng.normal(size=(8, k)), rng.integers(0, classes, 8)
+    z[1] += 600.0                                                               # near, and behind, what a product with log2(e) / T takes at the lowest of them
+    z[2] -= 900.0
+    z[3] *= 1e4
+    z[4:7, classes // 2:] = np.array([-np.inf, -1e5, -1e30])[:, None]
+    ids = np.stack([rng.permutation(classes // 2)[:k] for _ in z])
+    labels[4:7] = ids[4:7, 0]
+    for hard in (0.0, 0.4):
+        _check(B, ctx, z, ids, logits, T, hard, labels if hard else None, t)
